@@ -243,6 +243,73 @@ int zr_impute(void* out, int64_t ld, int32_t rows, int32_t cols, int32_t axis,
               const int32_t* keep_idx, int32_t n_keep, int policy, const void* prev,
               int dtype, void* stream);
 
+/* ---- Block-scaled values: activation checkpoints in 8 bits, products of 8- and 4-bit operands ----
+ *
+ * A matrix [rows x n] is held in blocks of 32 neighbouring values of a row (the axis that products sum over), a power of
+ * two for each block and 8 or 4 bits for each value:
+ *   value = element * 2^e.   With a = max |x| over the block, e is the smallest integer with a <= top * 2^e, within
+ *   [-127, 127], and the element is x * 2^-e rounded to nearest, ties to even, on the grid of its format: no value is
+ *   clipped (unless e is limited), each is off by at most half a step of the grid.
+ *   ZR_MX_E4M3  8 bits, 4 of exponent, 3 of mantissa; top 448.  Half a step: at most 2^-4 of the value.
+ *   ZR_MX_E2M1  4 bits, 2 of exponent, 1 of mantissa; top 6.
+ *   ZR_MX_INT8  8-bit integers in 64ths; top 127/64.  Half a step: 2^-7 of 2^e, i.e. at most a 126th of a.  The closest one
+ *               for activations of like size; no product instruction takes it (zr_mx_linear_fwd: ZR_ERR_DTYPE).
+ *   A block that holds a NaN or an infinity stands for NaN in all of its values.
+ * Storage: elements [rows x ldq bytes], zr_mx_row_bytes(n, format) of them used (whole groups of 128 values, E2M1 with the
+ * even value in the low half of a byte; zeros behind the n-th); scales [rows x lds bytes], zr_mx_scale_bytes(n) of them used: e + 127
+ * as a byte, 255 for NaN, in groups of 16 blocks with block b of a group at byte 4 (b % 4) + b / 4, zeros
+ * behind the last block.  Both 16-byte aligned, ldq and lds multiples of 16 (else SHAPE).  zr_mx_quantize writes all of
+ * it; a matrix from elsewhere must hold the zeros too.  (The two size functions: pure host, 0 on bad arguments.) */
+typedef enum { ZR_MX_E4M3 = 0, ZR_MX_E2M1 = 1, ZR_MX_INT8 = 2 } zr_mx_format;
+size_t zr_mx_row_bytes(int32_t n, int format);
+size_t zr_mx_scale_bytes(int32_t n);
+
+/* src [rows x cols] (ld, dtype) into blocks along `axis`:
+ *  axis 1: along a row; q holds `rows` rows of cols values.  The checkpoint of an activation X[M x K], or a shard stored
+ *          [out x in].
+ *  axis 0: along a column; q holds the transpose, `cols` rows of `rows` values.  A shard stored [in x out].
+ *  keep_idx (NULL: all, n_keep is ignored): only these indices of the block axis, side by side in ascending order (the
+ *  pruned input of Sec. 3.1, or the weight rows that go with it); rows of q then hold n_keep values.
+ *  One launch.  Errors: NULL, SHAPE, INDEX, DTYPE (dtype or format), LIMIT, HIP. */
+int zr_mx_quantize(const void* src, int64_t ld, int32_t rows, int32_t cols, int axis, const int32_t* keep_idx, int32_t n_keep,
+                   int dtype, int format, void* q, int64_t ldq, void* scales, int64_t lds, void* stream);
+
+/* out [rows x n] (ldo, dtype): the values that a matrix in blocks stands for, rounded to dtype (bf16 holds them exactly,
+ * but for magnitudes below 2^-126).  One launch.  Errors: NULL, SHAPE, DTYPE, LIMIT, HIP. */
+int zr_mx_dequantize(const void* q, int64_t ldq, const void* scales, int64_t lds, int32_t rows, int32_t n, int format,
+                     void* out, int64_t ldo, int dtype, void* stream);
+
+/* zr_resized_linear_fwd with both operands in blocks along the contraction:
+ *  DROP_K: Y = X[:,S] W[S,:]          Wq [N x n_keep]: zr_mx_quantize of the shard's kept rows (axis 0 of [K x N])
+ *  DROP_N: Y[:,S] = X W[:,S]; Y[:,P] imputed by `policy`
+ *                                     Wq [N x K]: the whole shard, put into blocks once; kept rows are picked in flight
+ *  keep_idx NULL: nothing is pruned, n_keep is ignored.
+ *  X [M x K] (ldx, dtype) is put into blocks of x_format by the call, into Xq / Xs, which then hold the checkpoint for
+ *  zr_resized_linear_bwd_mx ([M x n_keep] in DROP_K, [M x K] in DROP_N; the bits of zr_mx_quantize).  With M <= 16 they
+ *  may both be NULL: nothing is kept, and the product does it in its one launch.  X NULL: Xq / Xs are the input.
+ *  x_format ZR_MX_E4M3 or ZR_MX_E2M1; w_format the same or ZR_MX_E2M1.  dtype: of X, Y and prev_Y.
+ *  Sums are fp32, rounded once.  bf16 results with an 8-bit operand: the matrix instruction cuts every product at 2^-13 of the
+ *  largest of its group of eight, 1e-5 of a result's size on the whole; fp32 results are multiplied in bf16 instead (exact factors).
+ *  prev_Y as for zr_resized_linear_fwd.  Launches: 1, +1 if Xq / Xs are written, +1 for AVERAGE.
+ *  Errors: NULL, SHAPE, INDEX, DTYPE, MODE, POLICY, LIMIT, HIP. */
+int zr_mx_linear_fwd(const void* X, int64_t ldx, void* Xq, int64_t ldxq, void* Xs, int64_t ldxs, int x_format,
+                     const void* Wq, int64_t ldwq, const void* Ws, int64_t ldws, int w_format,
+                     void* Y, int64_t ldy, int32_t M, int32_t K, int32_t N, const int32_t* keep_idx, int32_t n_keep,
+                     int mode, int dtype, int policy, const void* prev_Y, void* stream);
+
+/* zr_resized_linear_bwd from a checkpoint of X in blocks (any format): Xq / Xs hold [M x n_keep] in DROP_K (the kept columns) and
+ * [M x K] in DROP_N, as zr_mx_quantize and zr_mx_linear_fwd leave them.  W, dY, dX, dW, lists, policies and errors as
+ * there; dX and dW are the gradients at the values that the checkpoint stands for.
+ *  workspace: needed for dW (NULL otherwise allowed), 16-byte aligned, at least zr_mx_bwd_workspace_bytes: the checkpoint's
+ *  values go there ([M x width], width = the held columns rounded up to 64), and what is left serves as
+ *  zr_resized_linear_bwd's scratch.  Errors also: NULL without it, SHAPE if it is too small or not aligned. */
+size_t zr_mx_bwd_workspace_bytes(int32_t M, int32_t K, int32_t N, int32_t n_keep, int mode, int dtype);
+int zr_resized_linear_bwd_mx(const void* Xq, int64_t ldxq, const void* Xs, int64_t ldxs, int x_format,
+                             const void* W, int64_t ldw, const void* dY, int64_t lddy,
+                             void* dX, int64_t lddx, void* dW, int64_t lddw, int32_t M, int32_t K, int32_t N,
+                             const int32_t* keep_idx, int32_t n_keep, int mode, int w_layout, int dtype, int policy,
+                             const void* prev_dX, const void* prev_dW, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Weight-variation scores (Sec. 3.2 "Priority Pruning"; Algorithm 1):
  *   scores[i] = mean over the slice's elements of |W_t - W_prev|, for every index
  *   i of the pruned axis of W[K x N] (columns for ZR_DROP_N, rows for ZR_DROP_K;

@@ -12,7 +12,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libzr.so")
 SOURCES = ["zr_api.hip", "zr_select.hip", "zr_impute.hip", "zr_gemm.hip", "zr_gemm_fast.hip", "zr_gemm_pair.hip", "zr_gemm_f32.hip", "zr_compact.hip", "zr_priority.hip",
-           "zr_probe.hip"]
+           "zr_probe.hip", "zr_mx_api.hip", "zr_mx_quant.hip", "zr_mx_gemm.hip"]
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

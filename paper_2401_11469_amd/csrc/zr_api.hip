@@ -317,30 +317,45 @@ int zr_resized_linear_fwd(const void* X, int64_t ldx, const void* W, int64_t ldw
     return launch_gemm(d, s);
 }
 
-int zr_resized_linear_bwd(const void* X, int64_t ldx, const void* W, int64_t ldw,
-                          const void* dY, int64_t lddy,
-                          void* dX, int64_t lddx, void* dW, int64_t lddw,
-                          int32_t M, int32_t K, int32_t N,
-                          const int32_t* keep_idx, int32_t n_keep,
-                          int mode, int w_layout, int dtype, int policy,
-                          const void* prev_dX, const void* prev_dW,
-                          void* workspace, size_t workspace_bytes, int workspace_flags, void* stream)
+}  // extern "C"
+
+namespace zr {
+
+int check_linear_bwd(const void* X, int64_t ldx, const void* W, int64_t ldw, const void* dY, int64_t lddy,
+                     const void* dX, int64_t lddx, const void* dW, int64_t lddw, int32_t M, int32_t K, int32_t N,
+                     const int32_t* keep_idx, int32_t n_keep, int mode, int w_layout, int dtype, int policy,
+                     const void* prev_dX, const void* prev_dW, bool x_kept)
 {
     if (!dY || (!dX && !dW)) return ZR_ERR_NULL;
     if ((dX && !W) || (dW && !X)) return ZR_ERR_NULL;
-    int st = check_common(M, K, N, keep_idx, n_keep, mode, dtype, policy);
+    const int st = check_common(M, K, N, keep_idx, n_keep, mode, dtype, policy);
     if (st != ZR_OK) return st;
     if (w_layout != ZR_W_KN && w_layout != ZR_W_NK) return ZR_ERR_MODE;
     const bool kn = w_layout == ZR_W_KN;
     if (lddy < N) return ZR_ERR_SHAPE;
     if (dX && (ldw < (kn ? N : K) || lddx < K)) return ZR_ERR_SHAPE;
-    if (dW && (ldx < K || lddw < (kn ? N : K))) return ZR_ERR_SHAPE;
+    if (dW && (ldx < (x_kept ? n_keep : K) || lddw < (kn ? N : K))) return ZR_ERR_SHAPE;
     const bool full = n_keep == (mode == ZR_DROP_N ? N : K);
     if (policy == ZR_IMPUTE_SAME && !full) {
         if (dW && !prev_dW) return ZR_ERR_POLICY;
         if (dX && mode == ZR_DROP_K && !prev_dX) return ZR_ERR_POLICY;
     }
-    hipStream_t s = (hipStream_t)stream;
+    return ZR_OK;
+}
+
+int resized_linear_bwd(const void* X, int64_t ldx, const void* W, int64_t ldw,
+                       const void* dY, int64_t lddy,
+                       void* dX, int64_t lddx, void* dW, int64_t lddw,
+                       int32_t M, int32_t K, int32_t N,
+                       const int32_t* keep_idx, int32_t n_keep,
+                       int mode, int w_layout, int dtype, int policy,
+                       const void* prev_dX, const void* prev_dW,
+                       void* workspace, size_t workspace_bytes, int workspace_flags, bool x_kept, hipStream_t s)
+{
+    int st = check_linear_bwd(X, ldx, W, ldw, dY, lddy, dX, lddx, dW, lddw, M, K, N, keep_idx, n_keep, mode, w_layout, dtype, policy, prev_dX, prev_dW, x_kept);
+    if (st != ZR_OK) return st;
+    const bool kn = w_layout == ZR_W_KN;
+    const bool full = n_keep == (mode == ZR_DROP_N ? N : K);
     const int32_t* S = full ? nullptr : keep_idx;
     const bool same = !full && policy == ZR_IMPUTE_SAME;       // fused into the scatter epilogues
     const bool post = !full && policy == ZR_IMPUTE_AVERAGE;    // sums in the epilogue, then mean and fill
@@ -363,7 +378,7 @@ int zr_resized_linear_bwd(const void* X, int64_t ldx, const void* W, int64_t ldw
         const int wr = kn ? K : N, wc = kn ? N : K;
         auto dx_clear = [&](const void* p, int rows, int cols, int64_t ld) { return clear(dX, M, K, lddx, p, rows, cols, ld); };
         auto dw_clear = [&](const void* p, int rows, int cols, int64_t ld) { return clear(dW, wr, wc, lddw, p, rows, cols, ld); };
-        return dx_clear(dW, wr, wc, lddw) && dx_clear(X, M, K, ldx) && dx_clear(dY, M, N, lddy) && dx_clear(same ? prev_dW : nullptr, wr, wc, lddw) &&
+        return dx_clear(dW, wr, wc, lddw) && dx_clear(X, M, x_kept ? n_keep : K, ldx) && dx_clear(dY, M, N, lddy) && dx_clear(same ? prev_dW : nullptr, wr, wc, lddw) &&
                dw_clear(W, wr, wc, ldw) && dw_clear(dY, M, N, lddy) && dw_clear(same ? prev_dX : nullptr, M, K, lddx);
     };
 
@@ -375,7 +390,9 @@ int zr_resized_linear_bwd(const void* X, int64_t ldx, const void* W, int64_t ldw
 
     // one extraction serves both products: X[:,S] (DROP_K, used by dW) or dY[:,S] (DROP_N)
     Extract ex{false, 0};
-    if (mode == ZR_DROP_K) {
+    if (x_kept) {
+        // X holds the kept columns already
+    } else if (mode == ZR_DROP_K) {
         if (dW) ex = plan_extract(X, ldx, M, K, n_keep, dtype, workspace, workspace_bytes);
         // the forward call of this layer left X[:,S] at the same place (same plan, same sizes)
         const bool reuse = (workspace_flags & ZR_WS_HOLDS_FORWARD) != 0;
@@ -394,7 +411,7 @@ int zr_resized_linear_bwd(const void* X, int64_t ldx, const void* W, int64_t ldw
     // (in DROP_K the start of the buffer may hold the forward call's X[:,S] even when this call
     // extracts nothing itself)
     give_split_scratch(d, workspace, workspace_bytes,
-                       extraction_bytes(M, mode == ZR_DROP_K ? K : N, n_keep, dtype, workspace, workspace_bytes));
+                       x_kept ? 0 : extraction_bytes(M, mode == ZR_DROP_K ? K : N, n_keep, dtype, workspace, workspace_bytes));
     if (dX) {
         d.out = dX; d.ldo = lddx; d.I = M;
         d.B = weight_dx(W, ldw, K, N, mode, w_layout, S);
@@ -423,8 +440,9 @@ int zr_resized_linear_bwd(const void* X, int64_t ldx, const void* W, int64_t ldw
         d.out = dW; d.ldo = lddw; d.C = M;
         d.prev = same ? prev_dW : nullptr;
         const Operand xs = (mode == ZR_DROP_K)
-            ? (ex.use ? operand(workspace, ex.width, false, nullptr, nullptr, M, ex.width)
-                      : operand(X, ldx, false, nullptr, S, M, K))
+            ? (x_kept ? operand(X, ldx, false, nullptr, nullptr, M, (int)ldx)
+               : ex.use ? operand(workspace, ex.width, false, nullptr, nullptr, M, ex.width)
+                        : operand(X, ldx, false, nullptr, S, M, K))
             : operand(X, ldx, false, nullptr, nullptr, M, K);
         const Operand dys = (mode == ZR_DROP_N)
             ? (ex.use ? operand(workspace, ex.width, false, nullptr, nullptr, M, ex.width)
@@ -459,6 +477,23 @@ int zr_resized_linear_bwd(const void* X, int64_t ldx, const void* W, int64_t ldw
         if (st != ZR_OK) return st;
     }
     return ZR_OK;
+}
+
+}  // namespace zr
+
+extern "C" {
+
+int zr_resized_linear_bwd(const void* X, int64_t ldx, const void* W, int64_t ldw,
+                          const void* dY, int64_t lddy,
+                          void* dX, int64_t lddx, void* dW, int64_t lddw,
+                          int32_t M, int32_t K, int32_t N,
+                          const int32_t* keep_idx, int32_t n_keep,
+                          int mode, int w_layout, int dtype, int policy,
+                          const void* prev_dX, const void* prev_dW,
+                          void* workspace, size_t workspace_bytes, int workspace_flags, void* stream)
+{
+    return resized_linear_bwd(X, ldx, W, ldw, dY, lddy, dX, lddx, dW, lddw, M, K, N, keep_idx, n_keep, mode, w_layout, dtype, policy,
+                              prev_dX, prev_dW, workspace, workspace_bytes, workspace_flags, false, (hipStream_t)stream);
 }
 
 int zr_priority_scores(const void* W_t, const void* W_prev, int64_t ld, int32_t K, int32_t N, int mode,

@@ -242,6 +242,19 @@ inline double two_groups(int n1, double t1, int n2, double t2, int slots)
     return std::max(T, hi);
 }
 
+// zr_resized_linear_bwd on arguments of its own kind; x_kept (DROP_K): X holds the kept columns side by side, [M x ldx] with
+// zeros behind the last, ldx a multiple of 64.
+int resized_linear_bwd(const void* X, int64_t ldx, const void* W, int64_t ldw, const void* dY, int64_t lddy,
+                       void* dX, int64_t lddx, void* dW, int64_t lddw, int32_t M, int32_t K, int32_t N,
+                       const int32_t* keep_idx, int32_t n_keep, int mode, int w_layout, int dtype, int policy,
+                       const void* prev_dX, const void* prev_dW, void* workspace, size_t workspace_bytes,
+                       int workspace_flags, bool x_kept, hipStream_t stream);
+// its argument checks alone
+int check_linear_bwd(const void* X, int64_t ldx, const void* W, int64_t ldw, const void* dY, int64_t lddy,
+                     const void* dX, int64_t lddx, const void* dW, int64_t lddw, int32_t M, int32_t K, int32_t N,
+                     const int32_t* keep_idx, int32_t n_keep, int mode, int w_layout, int dtype, int policy,
+                     const void* prev_dX, const void* prev_dW, bool x_kept);
+
 inline int hip_status(hipError_t e) { return e == hipSuccess ? ZR_OK : ZR_ERR_HIP; }
 
 }  // namespace zr

@@ -1,0 +1,658 @@
+// The product of two matrices in blocks (zr_mx.h has the format):
+//     Y[m, j] = sum_c X[m, c] W[j, c],   both operands with the contraction contiguous,
+// on the matrix instruction that takes 4- and 8-bit elements with a scale per 32 of them
+// (16 x 16 x 128, one step of a row is 64 or 128 bytes).
+#include <type_traits>
+
+#include "zr_mx.h"
+
+namespace zr {
+
+namespace {
+
+typedef int v8i __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+constexpr int E4 = ZR_MX_E4M3, E2 = ZR_MX_E2M1;
+constexpr int step_bytes(int fmt) { return fmt == E2 ? 64 : 128; }       // 128 elements of a row
+
+struct PArgs {
+    const uint8_t *xq, *xs, *wq, *ws;
+    int64_t ldxq, ldxs, ldwq, ldws;
+    const int32_t* w_rows;
+    int w_extent, M, J, steps;          // steps of 128
+    void* Y;
+    int64_t ldy;
+    int N;
+    const void* prev;
+    int vec;                            // 16-byte accesses fit Y and prev
+    int tiles_i, tiles_j;
+    const void* raw;                    // X as it arrives
+    int64_t ldraw;
+    const int32_t* raw_cols;
+    int raw_extent, C;
+};
+
+// global memory -> LDS, 16 bytes a lane to 64 x 16 bytes from a wavefront-uniform address; from inline assembly, so
+// that the compiler's waits for LDS reads do not count it: every wait for it is written out (wait_vm)
+__device__ __forceinline__ void to_lds16(const void* gptr, uint32_t lds_uniform)
+{
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" :: "v"(gptr), "s"(lds_uniform) : "memory");
+}
+// (and for the LDS reads, so that no read of a stage is under way when the barrier behind lets others write there)
+template <int N> __device__ __forceinline__ void wait_vm()
+{
+    static_assert(N >= 0 && N < 64, "vmcnt is a 6-bit field");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(N) : "memory");
+}
+
+template <class T> __device__ __forceinline__ T to_out(float f);
+template <> __device__ __forceinline__ float to_out<float>(float f) { return f; }
+template <> __device__ __forceinline__ uint16_t to_out<uint16_t>(float f)
+{
+    union { __bf16 h; uint16_t u; } x;
+    x.h = (__bf16)f;                    // v_cvt_pk_bf16_f32: to nearest even
+    return x.u;
+}
+
+// One lane's 128-deep share of a row: 32 elements.
+struct Frag { uint4 lo, hi; };
+__device__ __forceinline__ v8i as_v8(const Frag& f)
+{
+    v8i v;
+    v[0] = f.lo.x; v[1] = f.lo.y; v[2] = f.lo.z; v[3] = f.lo.w;
+    v[4] = f.hi.x; v[5] = f.hi.y; v[6] = f.hi.z; v[7] = f.hi.w;
+    return v;
+}
+
+template <int FA, int FB, int OP>
+__device__ __forceinline__ f32x4 mma(const Frag& a, uint32_t sa, const Frag& b, uint32_t sb, f32x4 c)
+{
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(as_v8(a), as_v8(b), c, FA == E2 ? 4 : 0, FB == E2 ? 4 : 0, OP, (int)sa, OP, (int)sb);
+}
+
+// Wide products.  The 8-bit form of the instruction adds up groups of eight products after cutting each at 2^-13 of the
+// group's largest (read off the hardware with two-term sums); rounded to bf16 that is lost in the rounding (1e-5 of a
+// result's size, against 2^-9), but an fp32 result would show it.  For fp32 results with an 8-bit operand the elements,
+// scaled, are turned into bf16 (exact: at most 4 significant bits) and multiplied by the bf16 instruction, whose sums are fp32.
+// Eight elements (8 bytes, or 4 in .x) -> bf16
+template <int F> __device__ __forceinline__ bf16x8 widen8(uint2 r, float scale)
+{
+    bf16x8 o;
+    bf16x2 p[4];
+    if constexpr (F == E2) {
+        p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(r.x, scale, 0);
+        p[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(r.x, scale, 1);
+        p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(r.x, scale, 2);
+        p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(r.x, scale, 3);
+    } else {
+        p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(r.x, scale, false);
+        p[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(r.x, scale, true);
+        p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(r.y, scale, false);
+        p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(r.y, scale, true);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { o[2 * i] = p[i].x; o[2 * i + 1] = p[i].y; }
+    return o;
+}
+
+// Which 32 of a step's 128 elements lane group g holds.  8-bit: 16 g .. + 15 and 64 + 16 g .. + 15 (the instruction's
+// own order); 4-bit: 32 g .. + 31, but in wide products, where both operands have to agree, as for 8-bit.
+// The scale of block g goes with lane group g either way; a wide product needs those of blocks g / 2 and 2 + g / 2.
+
+// ---------------------------------------------------------------------------
+// Results of one strip of a tile, laid out in LDS, to Y: plain, or the kept columns at their places and the imputed
+// value in the others.  A scattering tile owns the original columns from its first kept one (0 for the first tile) up to
+// the next tile's first (all for the last).
+// ---------------------------------------------------------------------------
+constexpr int WIN = 1024;       // original columns per pass
+
+template <class T, int BN, int ROWS, int NT, class ROWOF>
+__device__ void store_strip(const PArgs& g, const T* Cs, int cp, uint16_t* tab, const int* sidx, int j0, int cols_valid,
+                            int start, int end, int tid, ROWOF row_of)
+{
+    constexpr int PER = 16 / (int)sizeof(T);
+    T* Y = (T*)g.Y;
+    const T* prev = (const T*)g.prev;
+    if (!g.w_rows) {
+        if (g.vec) {
+            for (int u = tid; u < ROWS * (BN / PER); u += NT) {
+                const int r = u / (BN / PER), c = u % (BN / PER) * PER, row = row_of(r);
+                if (row >= g.M || c >= cols_valid) continue;
+                T* o = Y + (size_t)row * (size_t)g.ldy + j0 + c;
+                if (c + PER <= cols_valid) *(uint4*)o = *(const uint4*)(Cs + r * cp + c);
+                else
+                    for (int e = 0; c + e < cols_valid; ++e) o[e] = Cs[r * cp + c + e];
+            }
+        } else {
+            for (int u = tid; u < ROWS * BN; u += NT) {
+                const int r = u / BN, c = u % BN, row = row_of(r);
+                if (row < g.M && c < cols_valid) Y[(size_t)row * (size_t)g.ldy + j0 + c] = Cs[r * cp + c];
+            }
+        }
+        return;
+    }
+    for (int base = start / PER * PER; base < end; base += WIN) {
+        const int span = min(WIN, end - base);
+        __syncthreads();
+        for (int u = tid; u < WIN; u += NT) tab[u] = 0xffffu;
+        __syncthreads();
+        for (int u = tid; u < cols_valid; u += NT) {
+            const int p = sidx[u] - base;
+            if (p >= 0 && p < WIN) tab[p] = (uint16_t)u;
+        }
+        __syncthreads();
+        if (g.vec) {
+            const int nch = (span + PER - 1) / PER;
+            for (int u = tid; u < ROWS * nch; u += NT) {
+                const int r = u / nch, c = u - r * nch, row = row_of(r), p = base + c * PER;
+                if (row >= g.M) continue;
+                const size_t off = (size_t)row * (size_t)g.ldy + p;
+                const bool whole = p >= start && p + PER <= end;
+                union { uint4 v; T e[PER]; } x;
+                x.v = make_uint4(0u, 0u, 0u, 0u);
+                if (prev) {
+                    if (whole) x.v = *(const uint4*)(prev + off);
+                    else {
+#pragma unroll
+                        for (int e = 0; e < PER; ++e)
+                            if (p + e >= start && p + e < end) x.e[e] = prev[off + e];
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < PER; ++e) {
+                    const int k = tab[c * PER + e];
+                    const T y = Cs[r * cp + (k & (BN - 1))];
+                    x.e[e] = k == 0xffff ? x.e[e] : y;
+                }
+                if (whole) *(uint4*)(Y + off) = x.v;
+                else {
+#pragma unroll
+                    for (int e = 0; e < PER; ++e)
+                        if (p + e >= start && p + e < end) Y[off + e] = x.e[e];
+                }
+            }
+        } else {
+            for (int u = tid; u < ROWS * span; u += NT) {
+                const int r = u / span, c = u - r * span, row = row_of(r), p = base + c;
+                if (row >= g.M || p < start) continue;
+                const size_t off = (size_t)row * (size_t)g.ldy + p;
+                const int k = tab[c];
+                Y[off] = k != 0xffff ? Cs[r * cp + k] : prev ? prev[off] : T(0);
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Tiles of BM x BN on WM x WN wavefronts.  The contraction travels in steps of 128 through a ring of LDS stages, straight
+// from memory; the scales of four steps at a time, into two places of their own.
+// ---------------------------------------------------------------------------
+template <int FA, int FB, int BM, int BN, int WM, int WN> struct Shape {
+    static constexpr int NW = WM * WN, NT = 64 * NW, TM = BM / WM / 16, TN = BN / WN / 16;
+    static constexpr int BA = step_bytes(FA), BB = step_bytes(FB);
+    static constexpr int A_BYTES = BM * BA, STAGE = BM * BA + BN * BB, SCALES = (BM + BN) * 16;
+    static constexpr int FIT = (160 * 1024 - 2 * SCALES) / STAGE;
+    static constexpr int NS = FIT < 4 ? FIT : 4;
+    static constexpr int RING = NS * STAGE + 2 * SCALES;
+    static constexpr int NA = A_BYTES / 1024 / NW, NB = BN * BB / 1024 / NW, NL = NA + NB;
+    static_assert(NS >= 2 && NA * NW * 1024 == A_BYTES && NB * NW * 1024 == BN * BB && NA > 0 && NB > 0, "loads do not divide over the wavefronts");
+    static constexpr int SINST = SCALES / 1024;             // instructions for the scales of four steps, one a wavefront at most
+    static_assert(SINST <= NW && NW % SINST == 0, "scales");
+};
+// rows of a strip of the epilogue: as many 16-row groups of every wavefront row as leave room
+template <class T, int BM, int BN, int WM> constexpr int strip_groups()
+{
+    int sg = BM / WM / 16;
+    while (16 * WM * sg * (BN + 16 / (int)sizeof(T)) * (int)sizeof(T) > 139 * 1024) sg /= 2;
+    return sg;
+}
+template <class T, int FA, int FB, int BM, int BN, int WM, int WN> constexpr int tile_lds()
+{
+    const int ep = 16 * WM * strip_groups<T, BM, BN, WM>() * (BN + 16 / (int)sizeof(T)) * (int)sizeof(T) + WIN * 2 + BN * 4;
+    const int ring = Shape<FA, FB, BM, BN, WM, WN>::RING;
+    return ep > ring ? ep : ring;
+}
+
+template <int FA, int FB, int BM, int BN, int WM, int WN, bool WIDE, class T>
+__global__ __launch_bounds__(64 * WM * WN) void mx_kernel(const PArgs g)
+{
+    typedef Shape<FA, FB, BM, BN, WM, WN> S;
+    constexpr int NW = S::NW, NT = S::NT, TM = S::TM, TN = S::TN, BA = S::BA, BB = S::BB, NS = S::NS;
+    extern __shared__ __align__(16) uint8_t smem[];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+
+    // workgroups go round-robin to the 8 XCDs: each gets a contiguous range of tiles, in groups of 4 tile rows
+    int ti, tj;
+    {
+        const int lin = (int)((blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8);
+        if (lin >= g.tiles_i * g.tiles_j) return;
+        constexpr int GI = 4;
+        const int grp = lin / (GI * g.tiles_j), in_rows = min(GI, g.tiles_i - grp * GI), within = lin - grp * GI * g.tiles_j;
+        ti = grp * GI + within % in_rows;
+        tj = within / in_rows;
+    }
+    const int i0 = ti * BM, j0 = tj * BN;
+    const int KT = g.steps;
+
+    // what this lane fetches: rows past the ends are the last one again (their results are not stored)
+    const uint8_t *pa[S::NA], *pb[S::NB], *psc;
+    {
+        constexpr int RA = 1024 / BA, RB = 1024 / BB;       // rows of one instruction
+        const int ra = lane / (BA / 16), rb = lane / (BB / 16);
+#pragma unroll
+        for (int q = 0; q < S::NA; ++q) {
+            const int r = RA * (wave + NW * q) + ra;
+            const int chunk = (lane % (BA / 16)) ^ ((r >> 1) & (BA / 16 - 1));
+            pa[q] = g.xq + (size_t)min(i0 + r, g.M - 1) * (size_t)g.ldxq + chunk * 16;
+        }
+#pragma unroll
+        for (int q = 0; q < S::NB; ++q) {
+            const int r = RB * (wave + NW * q) + rb;
+            const int chunk = (lane % (BB / 16)) ^ ((r >> 1) & (BB / 16 - 1));
+            int j = min(j0 + r, g.J - 1);
+            if (g.w_rows) j = clamp_idx(g.w_rows[j], g.w_extent);
+            pb[q] = g.wq + (size_t)j * (size_t)g.ldwq + chunk * 16;
+        }
+        const int r = 64 * (wave % S::SINST) + lane;        // tile rows of A, then of B
+        if (r < BM) psc = g.xs + (size_t)min(i0 + r, g.M - 1) * (size_t)g.ldxs;
+        else {
+            int j = min(j0 + r - BM, g.J - 1);
+            if (g.w_rows) j = clamp_idx(g.w_rows[j], g.w_extent);
+            psc = g.ws + (size_t)j * (size_t)g.ldws;
+        }
+    }
+    const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)smem);
+    const uint32_t sc0 = lds0 + NS * S::STAGE;
+    // requests stage s into ring slot `slot`; with the first of four steps go their scales
+    auto issue = [&](int s, int slot) {
+        if ((s & 3) == 0) to_lds16(psc + (s >> 2) * 16, sc0 + ((s >> 2) & 1) * S::SCALES + (wave % S::SINST) * 1024);
+        const uint32_t base = lds0 + slot * S::STAGE;
+#pragma unroll
+        for (int q = 0; q < S::NA; ++q) to_lds16(pa[q] + (size_t)s * BA, base + (wave + NW * q) * 1024);
+#pragma unroll
+        for (int q = 0; q < S::NB; ++q) to_lds16(pb[q] + (size_t)s * BB, base + S::A_BYTES + (wave + NW * q) * 1024);
+    };
+
+    const int wr = wave / WN * (TM * 16), wc = wave % WN * (TN * 16);
+    const int r16 = lane & 15, lg = lane >> 4;
+    auto frag = [&](const uint8_t* tile, int row, auto fmt) {
+        constexpr int F = decltype(fmt)::value;
+        Frag f;
+        f.hi = make_uint4(0u, 0u, 0u, 0u);
+        const int sw = (row >> 1) & (step_bytes(F) / 16 - 1);
+        const uint8_t* p = tile + row * step_bytes(F);
+        if constexpr (F == E4) {
+            f.lo = *(const uint4*)(p + ((lg ^ sw) << 4));
+            f.hi = *(const uint4*)(p + (((lg + 4) ^ sw) << 4));
+        } else if constexpr (!WIDE) {
+            f.lo = *(const uint4*)(p + ((lg ^ sw) << 4));
+        } else {
+            const uint2 a = *(const uint2*)(p + (((lg >> 1) ^ sw) << 4) + (lg & 1) * 8);
+            const uint2 b = *(const uint2*)(p + ((((lg >> 1) + 2) ^ sw) << 4) + (lg & 1) * 8);
+            f.lo = make_uint4(a.x, a.y, b.x, b.y);
+        }
+        return f;
+    };
+
+    f32x4 acc[TM][TN];
+#pragma unroll
+    for (int a = 0; a < TM; ++a)
+#pragma unroll
+        for (int b = 0; b < TN; ++b) acc[a][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    for (int s = 0; s < NS - 1; ++s)
+        if (s < KT) issue(s, s);
+    wait_vm<0>();
+    __builtin_amdgcn_s_barrier();
+
+    uint32_t sa[TM][WIDE ? 2 : 1], sb[TN][WIDE ? 2 : 1];
+    int slot = 0;
+    auto step = [&](int s, auto sub) {
+        constexpr int U = decltype(sub)::value;
+        const uint8_t* st = smem + slot * S::STAGE;
+        if constexpr (U == 0) {
+            const uint8_t* sc = smem + NS * S::STAGE + ((s >> 2) & 1) * S::SCALES;
+#pragma unroll
+            for (int h = 0; h < (WIDE ? 2 : 1); ++h) {
+                const int o = WIDE ? ((lg >> 1) + 2 * h) * 4 : lg * 4;
+#pragma unroll
+                for (int a = 0; a < TM; ++a) sa[a][h] = *(const uint32_t*)(sc + (wr + a * 16 + r16) * 16 + o);
+#pragma unroll
+                for (int b = 0; b < TN; ++b) sb[b][h] = *(const uint32_t*)(sc + (BM + wc + b * 16 + r16) * 16 + o);
+            }
+        }
+        const bool more = s + NS - 1 < KT;
+        if (more) issue(s + NS - 1, slot == 0 ? NS - 1 : slot - 1);
+        Frag fb[TN];
+#pragma unroll
+        for (int b = 0; b < TN; ++b) fb[b] = frag(st + S::A_BYTES, wc + b * 16 + r16, std::integral_constant<int, FB>());
+        if constexpr (!WIDE) {
+#pragma unroll
+            for (int a = 0; a < TM; ++a) {
+                const Frag fa = frag(st, wr + a * 16 + r16, std::integral_constant<int, FA>());
+#pragma unroll
+                for (int b = 0; b < TN; ++b) acc[a][b] = mma<FA, FB, U>(fa, sa[a][0], fb[b], sb[b][0], acc[a][b]);
+            }
+        } else {
+            auto piece = [&](const Frag& f, int u, auto fmt, const uint32_t (&sc)[2]) {
+                constexpr int F = decltype(fmt)::value;
+                const uint4 v = F == E2 || u < 2 ? f.lo : f.hi;
+                uint2 r;
+                if constexpr (F == E2) r = make_uint2(u == 0 ? v.x : u == 1 ? v.y : u == 2 ? v.z : v.w, 0u);
+                else r = (u & 1) ? make_uint2(v.z, v.w) : make_uint2(v.x, v.y);
+                return widen8<F>(r, mx_scale((sc[u >> 1] >> (8 * U)) & 255));
+            };
+            Frag fa[TM];
+#pragma unroll
+            for (int a = 0; a < TM; ++a) fa[a] = frag(st, wr + a * 16 + r16, std::integral_constant<int, FA>());
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                bf16x8 wb[TN];
+#pragma unroll
+                for (int b = 0; b < TN; ++b) wb[b] = piece(fb[b], u, std::integral_constant<int, FB>(), sb[b]);
+#pragma unroll
+                for (int a = 0; a < TM; ++a) {
+                    const bf16x8 wa = piece(fa[a], u, std::integral_constant<int, FA>(), sa[a]);
+#pragma unroll
+                    for (int b = 0; b < TN; ++b) acc[a][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wa, wb[b], acc[a][b], 0, 0, 0);
+                }
+            }
+        }
+        // stage s + 1 has landed when only the requests of s + 2 .. s + NS - 1 are out
+        if (more) {
+            constexpr int SC = (U + 2 <= 4 && 4 <= U + NS - 1) ? 1 : 0;       // scales go with the first of the next four
+            wait_vm<S::NL * (NS - 2) + SC>();
+        } else wait_vm<0>();
+        __builtin_amdgcn_s_barrier();
+        slot = slot + 1 == NS ? 0 : slot + 1;
+    };
+    for (int s = 0; s < KT; s += 4) {
+        step(s, std::integral_constant<int, 0>());
+        if (s + 1 < KT) step(s + 1, std::integral_constant<int, 1>());
+        if (s + 2 < KT) step(s + 2, std::integral_constant<int, 2>());
+        if (s + 3 < KT) step(s + 3, std::integral_constant<int, 3>());
+    }
+    __syncthreads();
+
+    // results: strips of 16 SG rows of every wavefront row through LDS
+    constexpr int SG = strip_groups<T, BM, BN, WM>(), ROWS = 16 * WM * SG, CP = BN + 16 / (int)sizeof(T);
+    T* Cs = (T*)smem;
+    uint16_t* tab = (uint16_t*)(smem + ROWS * CP * sizeof(T));
+    int* sidx = (int*)(tab + WIN);
+    const int cols_valid = min(BN, g.J - j0);
+    int start = 0, end = 0;
+    if (g.w_rows) {
+        for (int u = tid; u < cols_valid; u += NT) sidx[u] = clamp_idx(g.w_rows[j0 + u], g.N);
+        start = j0 == 0 ? 0 : clamp_idx(g.w_rows[j0], g.N);
+        end = j0 + BN >= g.J ? g.N : clamp_idx(g.w_rows[j0 + BN], g.N);
+    }
+#pragma unroll
+    for (int a0 = 0; a0 < TM; a0 += SG) {
+        if (a0) __syncthreads();
+#pragma unroll
+        for (int a = a0; a < a0 + SG; ++a)
+#pragma unroll
+            for (int b = 0; b < TN; ++b) {
+                T* c = Cs + (wave / WN * (16 * SG) + (a - a0) * 16 + 4 * lg) * CP + wc + b * 16 + r16;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) c[i * CP] = to_out<T>(acc[a][b][i]);
+            }
+        __syncthreads();
+        store_strip<T, BN, ROWS, NT>(g, Cs, CP, tab, sidx, j0, cols_valid, start, end, tid, [&](int r) {
+            return i0 + r / (16 * SG) * (TM * 16) + a0 * 16 + r % (16 * SG);
+        });
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Few rows of X (up to 16 MT): the weight is read once, straight into registers, and that is the time.  A workgroup has 16 rows
+// of W; its wavefronts split the contraction and add up in LDS, in their order.  RAW: X arrives in its own type and
+// each wavefront puts the part that it needs into blocks itself.
+// ---------------------------------------------------------------------------
+constexpr int FEW_WAVES = 8;
+
+template <int FA, int FB, int MT, bool WIDE, bool RAW, class T>
+__global__ __launch_bounds__(64 * FEW_WAVES) void mx_few_kernel(const PArgs g)
+{
+    constexpr int NT = 64 * FEW_WAVES, BA = step_bytes(FA), BB = step_bytes(FB);
+    __shared__ f32x4 part[FEW_WAVES][MT][64];
+    __shared__ int sidx[16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r16 = lane & 15, lg = lane >> 4;
+    const int j0 = blockIdx.x * 16, cols_valid = min(16, g.J - j0);
+    int j = min(j0 + r16, g.J - 1);
+    if (g.w_rows) j = clamp_idx(g.w_rows[j], g.w_extent);
+    const uint8_t* wq = g.wq + (size_t)j * (size_t)g.ldwq;
+    const uint8_t* ws = g.ws + (size_t)j * (size_t)g.ldws;
+
+    // this lane's 32 elements of a step (see the order above)
+    auto frag = [&](const uint8_t* p, auto fmt) {
+        constexpr int F = decltype(fmt)::value;
+        Frag f;
+        f.hi = make_uint4(0u, 0u, 0u, 0u);
+        if constexpr (F == E4) {
+            f.lo = *(const uint4*)(p + lg * 16);
+            f.hi = *(const uint4*)(p + 64 + lg * 16);
+        } else if constexpr (!WIDE) {
+            f.lo = *(const uint4*)(p + lg * 16);
+        } else {
+            const uint2 a = *(const uint2*)(p + lg * 8), b = *(const uint2*)(p + 32 + lg * 8);
+            f.lo = make_uint4(a.x, a.y, b.x, b.y);
+        }
+        return f;
+    };
+    // the scale bytes of step s that this lane needs: of block lg, or (wide) of blocks lg / 2 and 2 + lg / 2
+    struct Sc { uint32_t a, b; };
+    auto scales = [&](const uint8_t* p, int s) {
+        Sc c;
+        const uint8_t* q = p + (s >> 2) * 16 + (s & 3);
+        c.a = q[(WIDE ? lg >> 1 : lg) * 4];
+        c.b = WIDE ? q[((lg >> 1) + 2) * 4] : 0;
+        return c;
+    };
+    f32x4 acc[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    auto multiply = [&](const Frag& fa, Sc sa, const Frag& fb, Sc sb, f32x4 c) {
+        if constexpr (!WIDE) return mma<FA, FB, 0>(fa, sa.a, fb, sb.a, c);
+        else {
+            auto piece = [](const Frag& f, int u, auto fmt, Sc sc) {
+                constexpr int F = decltype(fmt)::value;
+                const uint4 v = F == E2 || u < 2 ? f.lo : f.hi;
+                uint2 r;
+                if constexpr (F == E2) r = make_uint2(u == 0 ? v.x : u == 1 ? v.y : u == 2 ? v.z : v.w, 0u);
+                else r = (u & 1) ? make_uint2(v.z, v.w) : make_uint2(v.x, v.y);
+                return widen8<F>(r, mx_scale(u < 2 ? sc.a : sc.b));
+            };
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(piece(fa, u, std::integral_constant<int, FA>(), sa),
+                                                            piece(fb, u, std::integral_constant<int, FB>(), sb), c, 0, 0, 0);
+            return c;
+        }
+    };
+
+    const int s_lo = g.steps * wave / FEW_WAVES, s_hi = g.steps * (wave + 1) / FEW_WAVES;
+    constexpr int U = 4;
+    for (int s0 = s_lo; s0 < s_hi; s0 += U) {
+        Frag fb[U];
+        Sc sb[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int s = min(s0 + u, s_hi - 1);
+            fb[u] = frag(wq + (size_t)s * BB, std::integral_constant<int, FB>());
+            sb[u] = scales(ws, s);
+        }
+        if constexpr (!RAW) {
+#pragma unroll
+            for (int t = 0; t < MT; ++t) {
+                const size_t m = (size_t)min(t * 16 + r16, g.M - 1);
+                Frag fa[U];
+                Sc sa[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int s = min(s0 + u, s_hi - 1);
+                    fa[u] = frag(g.xq + m * (size_t)g.ldxq + (size_t)s * BA, std::integral_constant<int, FA>());
+                    sa[u] = scales(g.xs + m * (size_t)g.ldxs, s);
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (s0 + u < s_hi) acc[t] = multiply(fa[u], sa[u], fb[u], sb[u], acc[t]);
+            }
+        } else {
+            static_assert(!RAW || MT == 1, "one group of rows is quantised here");
+            const T* x = (const T*)g.raw + (size_t)min(r16, g.M - 1) * (size_t)g.ldraw;
+            auto value = [&](int c) {
+                const int k = min(c, g.C - 1);
+                const T v = x[g.raw_cols ? clamp_idx(g.raw_cols[k], g.raw_extent) : k];
+                float f;
+                if constexpr (sizeof(T) == 2) f = bf16_bits_to_f32(v);
+                else f = v;
+                return c < g.C ? f : 0.f;
+            };
+            auto peak = [](const float (&v)[8], uint32_t m) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
+                return m;
+            };
+            for (int u = 0; u < U && s0 + u < s_hi; ++u) {
+                // (8 elements each: in the order of the fragment's bytes)
+                constexpr bool SPLIT = FA == E4 || WIDE;
+                float v[4][8];
+#pragma unroll
+                for (int h = 0; h < 4; ++h) {
+                    const int c = (s0 + u) * 128 + (SPLIT ? (h >> 1) * 64 + lg * 16 + (h & 1) * 8 : lg * 32 + h * 8);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[h][i] = value(c + i);
+                }
+                Frag fa;
+                fa.hi = make_uint4(0u, 0u, 0u, 0u);
+                Sc sa;
+                if constexpr (SPLIT) {
+                    // halves of blocks lg / 2 and 2 + lg / 2: the other half is 16 lanes away
+                    uint32_t m0 = peak(v[1], peak(v[0], 0u)), m1 = peak(v[3], peak(v[2], 0u));
+                    m0 = max(m0, (uint32_t)__shfl_xor((int)m0, 16, 64));
+                    m1 = max(m1, (uint32_t)__shfl_xor((int)m1, 16, 64));
+                    const int c0 = mx_code<FA>(m0), c1 = mx_code<FA>(m1);
+                    const float i0 = c0 == 255 ? 0.f : mx_inv(c0), i1 = c1 == 255 ? 0.f : mx_inv(c1);
+                    const uint2 a = mx_encode8<FA>(v[0], i0), b = mx_encode8<FA>(v[1], i0), c = mx_encode8<FA>(v[2], i1), d = mx_encode8<FA>(v[3], i1);
+                    if constexpr (FA == E4) { fa.lo = make_uint4(a.x, a.y, b.x, b.y); fa.hi = make_uint4(c.x, c.y, d.x, d.y); }
+                    else fa.lo = make_uint4(a.x, b.x, c.x, d.x);
+                    if constexpr (WIDE) { sa.a = c0; sa.b = c1; }
+                    else {
+                        // block lg's code: lane groups 2 lg and on hold blocks 0, 1 first and 2, 3 second
+                        const int from = r16 + 32 * (lg & 1);
+                        const int lo = __shfl(c0, from, 64), hi = __shfl(c1, from, 64);
+                        sa.a = lg < 2 ? lo : hi;
+                        sa.b = 0;
+                    }
+                } else {
+                    const int c0 = mx_code<FA>(peak(v[3], peak(v[2], peak(v[1], peak(v[0], 0u)))));
+                    const float i0 = c0 == 255 ? 0.f : mx_inv(c0);
+                    fa.lo = make_uint4(mx_encode8<FA>(v[0], i0).x, mx_encode8<FA>(v[1], i0).x, mx_encode8<FA>(v[2], i0).x, mx_encode8<FA>(v[3], i0).x);
+                    sa.a = c0; sa.b = 0;
+                }
+                acc[0] = u == 0 ? multiply(fa, sa, fb[0], sb[0], acc[0]) : u == 1 ? multiply(fa, sa, fb[1], sb[1], acc[0])
+                       : u == 2 ? multiply(fa, sa, fb[2], sb[2], acc[0]) : multiply(fa, sa, fb[3], sb[3], acc[0]);
+            }
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < MT; ++t) part[wave][t][lane] = acc[t];
+    if (tid < 16) sidx[tid] = g.w_rows ? clamp_idx(g.w_rows[min(j0 + tid, g.J - 1)], g.N) : j0 + tid;
+    __syncthreads();
+    // result (m, c): row 4 (lane >> 4) + i of group t, column lane & 15
+    auto result = [&](int m, int c) {
+        const int t = m >> 4, l = ((m & 15) >> 2) * 16 + c;
+        float v = 0.f;
+#pragma unroll
+        for (int w = 0; w < FEW_WAVES; ++w) v += ((const float*)&part[w][t][l])[m & 3];
+        return to_out<T>(v);
+    };
+    T* Y = (T*)g.Y;
+    const T* prev = (const T*)g.prev;
+    if (!g.w_rows) {
+        for (int u = tid; u < 16 * g.M; u += NT) {
+            const int m = u >> 4, c = u & 15;
+            if (c < cols_valid) Y[(size_t)m * (size_t)g.ldy + j0 + c] = result(m, c);
+        }
+        return;
+    }
+    const int start = j0 == 0 ? 0 : sidx[0], end = j0 + 16 >= g.J ? g.N : clamp_idx(g.w_rows[j0 + 16], g.N);
+    const int span = end - start;
+    if (span <= 0) return;
+    for (int u = tid; u < span * g.M; u += NT) {
+        const int m = u / span, p = start + u % span;
+        const int c = lower_bound_lds(sidx, cols_valid, p);
+        const size_t off = (size_t)m * (size_t)g.ldy + p;
+        Y[off] = c < cols_valid && sidx[c] == p ? result(m, c) : prev ? prev[off] : T(0);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Host side
+// ---------------------------------------------------------------------------
+PArgs pargs_of(const MxProduct& p)
+{
+    PArgs g;
+    g.xq = p.X.q; g.xs = p.X.s; g.wq = p.W.q; g.ws = p.W.s;
+    g.ldxq = p.X.ldq; g.ldxs = p.X.lds; g.ldwq = p.W.ldq; g.ldws = p.W.lds;
+    g.w_rows = p.w_rows; g.w_extent = p.w_extent; g.M = p.M; g.J = p.J; g.steps = (p.C + 127) / 128;
+    g.Y = p.Y; g.ldy = p.ldy; g.N = p.N; g.prev = p.prev;
+    const int es = p.dtype == ZR_BF16 ? 2 : 4;
+    g.vec = (uintptr_t)p.Y % 16 == 0 && (uintptr_t)p.prev % 16 == 0 && p.ldy * es % 16 == 0;
+    g.tiles_i = g.tiles_j = 0;
+    g.raw = p.raw; g.ldraw = p.ldraw; g.raw_cols = p.raw_cols; g.raw_extent = p.raw_extent; g.C = p.C;
+    return g;
+}
+
+template <int FA, int FB, int BM, int BN, int WM, int WN, bool WIDE, class T>
+int launch_tiles(PArgs g, hipStream_t stream)
+{
+    constexpr int lds = tile_lds<T, FA, FB, BM, BN, WM, WN>();
+    static AttrFlags flags;
+    if (!ensure_max_dynamic_lds((const void*)mx_kernel<FA, FB, BM, BN, WM, WN, WIDE, T>, lds, &flags)) return ZR_ERR_HIP;
+    g.tiles_i = (g.M + BM - 1) / BM; g.tiles_j = (g.J + BN - 1) / BN;
+    const int64_t tiles = (int64_t)g.tiles_i * g.tiles_j;
+    hipLaunchKernelGGL((mx_kernel<FA, FB, BM, BN, WM, WN, WIDE, T>), dim3((uint32_t)((tiles + 7) / 8 * 8)), dim3(64 * WM * WN), lds, stream, g);
+    return hip_status(hipGetLastError());
+}
+
+template <int FA, int FB, bool WIDE, class T>
+int launch_formats(const MxProduct& p, hipStream_t stream)
+{
+    const PArgs g = pargs_of(p);
+    if (p.raw || p.M <= 64) {
+        const dim3 grid((p.J + 15) / 16), block(64 * FEW_WAVES);
+        if (p.raw) hipLaunchKernelGGL((mx_few_kernel<FA, FB, 1, WIDE, true, T>), grid, block, 0, stream, g);
+        else if (p.M <= 16) hipLaunchKernelGGL((mx_few_kernel<FA, FB, 1, WIDE, false, T>), grid, block, 0, stream, g);
+        else if (p.M <= 32) hipLaunchKernelGGL((mx_few_kernel<FA, FB, 2, WIDE, false, T>), grid, block, 0, stream, g);
+        else hipLaunchKernelGGL((mx_few_kernel<FA, FB, 4, WIDE, false, T>), grid, block, 0, stream, g);
+        return hip_status(hipGetLastError());
+    }
+    auto tiles = [&](int b) { return (int64_t)((p.M + b - 1) / b) * ((p.J + b - 1) / b); };
+    if constexpr (!WIDE)
+        if (tiles(256) >= 160) return launch_tiles<FA, FB, 256, 256, 2, 4, WIDE, T>(g, stream);
+    if (tiles(128) >= 160) return launch_tiles<FA, FB, 128, 128, 2, 2, WIDE, T>(g, stream);
+    return launch_tiles<FA, FB, 64, 64, 2, 2, WIDE, T>(g, stream);
+}
+
+}  // namespace
+
+int launch_mx_product(const MxProduct& p, hipStream_t stream)
+{
+    const bool x4 = p.X.fmt == E2, w4 = p.W.fmt == E2;
+    if (p.dtype == ZR_BF16) {
+        if (x4) return launch_formats<E2, E2, false, uint16_t>(p, stream);
+        if (w4) return launch_formats<E4, E2, false, uint16_t>(p, stream);
+        return launch_formats<E4, E4, false, uint16_t>(p, stream);
+    }
+    if (x4) return launch_formats<E2, E2, false, float>(p, stream);
+    if (w4) return launch_formats<E4, E2, true, float>(p, stream);
+    return launch_formats<E4, E4, true, float>(p, stream);
+}
+
+}  // namespace zr

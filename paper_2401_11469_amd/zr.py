@@ -9,7 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Optional, Tuple
+from typing import NamedTuple, Optional, Tuple, Union
 
 import torch
 
@@ -18,6 +18,7 @@ W_KN, W_NK = 0, 1
 WS_FRESH, WS_HOLDS_FORWARD = 0, 1
 ZERO, AVERAGE, SAME = 0, 1, 2
 F32, BF16 = 0, 1
+MX_E4M3, MX_E2M1, MX_INT8 = 0, 1, 2
 
 _LIB_PATH = os.environ.get("ZR_LIBZR_PATH") or os.path.join(os.path.dirname(os.path.abspath(__file__)), "libzr.so")
 if not os.path.exists(_LIB_PATH):
@@ -85,6 +86,23 @@ _lib.zr_debug_mfma_rate.argtypes = [_i32, _i32, _vp, ctypes.POINTER(_f64), _vp]
 _lib.zr_debug_mfma_rate.restype = ctypes.c_int
 _lib.zr_validate_keep_idx.argtypes = [_vp, _i32, _i32, _vp, _vp]
 _lib.zr_validate_keep_idx.restype = ctypes.c_int
+_lib.zr_mx_row_bytes.argtypes = [_i32, ctypes.c_int]
+_lib.zr_mx_row_bytes.restype = ctypes.c_size_t
+_lib.zr_mx_scale_bytes.argtypes = [_i32]
+_lib.zr_mx_scale_bytes.restype = ctypes.c_size_t
+_lib.zr_mx_quantize.argtypes = [_vp, _i64, _i32, _i32, ctypes.c_int, _vp, _i32, ctypes.c_int, ctypes.c_int, _vp, _i64, _vp, _i64, _vp]
+_lib.zr_mx_quantize.restype = ctypes.c_int
+_lib.zr_mx_dequantize.argtypes = [_vp, _i64, _vp, _i64, _i32, _i32, ctypes.c_int, _vp, _i64, ctypes.c_int, _vp]
+_lib.zr_mx_dequantize.restype = ctypes.c_int
+_lib.zr_mx_linear_fwd.argtypes = [_vp, _i64, _vp, _i64, _vp, _i64, ctypes.c_int, _vp, _i64, _vp, _i64, ctypes.c_int, _vp, _i64,
+                                  _i32, _i32, _i32, _vp, _i32, ctypes.c_int, ctypes.c_int, ctypes.c_int, _vp, _vp]
+_lib.zr_mx_linear_fwd.restype = ctypes.c_int
+_lib.zr_mx_bwd_workspace_bytes.argtypes = [_i32, _i32, _i32, _i32, ctypes.c_int, ctypes.c_int]
+_lib.zr_mx_bwd_workspace_bytes.restype = ctypes.c_size_t
+_lib.zr_resized_linear_bwd_mx.argtypes = [_vp, _i64, _vp, _i64, ctypes.c_int, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64,
+                                          _i32, _i32, _i32, _vp, _i32, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int,
+                                          _vp, _vp, _vp, ctypes.c_size_t, _vp]
+_lib.zr_resized_linear_bwd_mx.restype = ctypes.c_int
 
 
 class ZrError(RuntimeError):
@@ -296,6 +314,175 @@ def extract_kept_columns(inp: torch.Tensor, keep_idx: torch.Tensor, out: Optiona
     _check(_lib.zr_extract_kept_columns(ip, ld, rows, n, keep_idx.data_ptr(), keep_idx.numel(), op, ldo,
                                         _dtype_code(inp), _stream(stream)))
     return out
+
+
+class MX(NamedTuple):
+    """A matrix [rows, n] in blocks of 32 values with a power of two each: elements uint8 [rows, >= mx_row_bytes(n, fmt)],
+    scales uint8 [rows, >= mx_scale_bytes(n)] (zr.h has the layout)."""
+    q: torch.Tensor
+    scales: torch.Tensor
+    n: int
+    fmt: int
+
+
+def mx_row_bytes(n: int, fmt: int) -> int:
+    return int(_lib.zr_mx_row_bytes(n, fmt))
+
+
+def mx_scale_bytes(n: int) -> int:
+    return int(_lib.zr_mx_scale_bytes(n))
+
+
+def mx_empty(rows: int, n: int, fmt: int, device="cuda") -> MX:
+    return MX(torch.empty((rows, mx_row_bytes(n, fmt)), dtype=torch.uint8, device=device),
+              torch.empty((rows, mx_scale_bytes(n)), dtype=torch.uint8, device=device), n, fmt)
+
+
+def _mx(m: Optional[MX], rows: int, n: int, name: str):
+    """(elements, pitch, scales, pitch, format) of a matrix in blocks of the given size."""
+    if m is None:
+        return None, 0, None, 0, 0
+    if m.n != n or m.q.shape[0] != rows or m.scales.shape[0] != rows:
+        raise ValueError(f"{name}: need {rows} rows of {n} values in blocks")
+    if m.q.dtype != torch.uint8 or m.scales.dtype != torch.uint8:
+        raise ValueError(f"{name}: elements and scales are uint8")
+    return (*_mat(m.q, name), *_mat(m.scales, name), m.fmt)
+
+
+def _placed(stream, keep_idx, *tensors) -> None:
+    """The kernels run on the current device: all tensors have to be there, and the list has to be one that they can read."""
+    here = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != here:
+            raise ValueError("all tensors must be on the current GPU")
+    if stream is not None and stream.device.index != here:
+        raise ValueError("stream: of another GPU")
+    if keep_idx is not None and (keep_idx.dtype != torch.int32 or keep_idx.dim() != 1 or not keep_idx.is_contiguous()
+                                 or keep_idx.get_device() != here):
+        raise ValueError("keep_idx: need a contiguous int32 vector on the current GPU")
+
+
+def mx_quantize(src: torch.Tensor, fmt: int, axis: int = 1, keep_idx: Optional[torch.Tensor] = None,
+                out: Optional[MX] = None, stream=None) -> MX:
+    """src [rows, cols] in blocks along `axis` (0: the transpose in blocks), of the kept indices of that axis alone."""
+    _placed(stream, keep_idx, src, *(() if out is None else (out.q, out.scales)))
+    sp, ld = _mat(src, "src")
+    rows, cols = src.shape
+    n = (cols if axis == 1 else rows) if keep_idx is None else keep_idx.numel()
+    held = rows if axis == 1 else cols
+    if out is None:
+        out = mx_empty(held, n, fmt, src.device)
+    if out.fmt != fmt:
+        raise ValueError("out is of another format")
+    qp, ldq, scp, lds, _ = _mx(out, held, n, "out")
+    _check(_lib.zr_mx_quantize(sp, ld, rows, cols, axis, None if keep_idx is None else keep_idx.data_ptr(), n,
+                               _dtype_code(src), fmt, qp, ldq, scp, lds, _stream(stream)))
+    return out
+
+
+def mx_dequantize(m: MX, dtype=torch.bfloat16, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """The values [rows, n] that m stands for, in `dtype` (or in out's)."""
+    rows = m.q.shape[0]
+    _placed(stream, None, m.q, m.scales, out)
+    if out is None:
+        out = torch.empty((rows, m.n), dtype=dtype, device=m.q.device)
+    if tuple(out.shape) != (rows, m.n):
+        raise ValueError("out must be [rows, n]")
+    op, ldo = _mat(out, "out")
+    qp, ldq, scp, lds, fmt = _mx(m, rows, m.n, "m")
+    _check(_lib.zr_mx_dequantize(qp, ldq, scp, lds, rows, m.n, fmt, op, ldo, _dtype_code(out), _stream(stream)))
+    return out
+
+
+def mx_linear_fwd(X: Union[torch.Tensor, MX], W: MX, keep_idx: Optional[torch.Tensor] = None, mode: int = DROP_K,
+                  policy: int = ZERO, prev_Y: Optional[torch.Tensor] = None, Y: Optional[torch.Tensor] = None,
+                  x_fmt: int = MX_E4M3, x_mx: Optional[MX] = None, K: Optional[int] = None, dtype=torch.bfloat16,
+                  stream=None) -> torch.Tensor:
+    """X [M, K] (put into blocks of x_fmt by the call, into x_mx where given: the checkpoint for resized_linear_bwd_mx;
+    without x_mx at most 16 rows keep none, for more one is allocated), or X in blocks already (K: the layer's, for DROP_K; dtype: of Y).
+    W in blocks: [N, n_keep] (DROP_K) or the whole shard [N, K] (DROP_N).  keep_idx None: nothing is pruned."""
+    N = W.q.shape[0]
+    given = X if isinstance(X, MX) else x_mx
+    _placed(stream, keep_idx, W.q, W.scales, Y, prev_Y, *((X,) if given is not X else ()), *(() if given is None else (given.q, given.scales)))
+    if isinstance(X, MX):
+        if x_mx is not None:
+            raise ValueError("x_mx: X is in blocks already")
+        M, held = X.q.shape[0], X.n
+        K = held if K is None else K
+        x_mx, xp, ldx = X, None, 0
+        dev = X.q.device
+        dt = Y.dtype if Y is not None else dtype
+    else:
+        M, K = X.shape
+        held = K if keep_idx is None or mode != DROP_K else keep_idx.numel()
+        if x_mx is None and M > 16:
+            x_mx = mx_empty(M, held, x_fmt, X.device)
+            if stream is not None:                      # (freed on return, perhaps before the stream gets there)
+                x_mx.q.record_stream(stream)
+                x_mx.scales.record_stream(stream)
+        xp, ldx = _mat(X, "X")
+        dev, dt = X.device, X.dtype
+    if x_mx is not None:
+        if not isinstance(X, MX) and x_mx.fmt != x_fmt:
+            raise ValueError("x_mx is of another format")
+        x_fmt = x_mx.fmt
+    if Y is None:
+        Y = torch.empty((M, N), dtype=dt, device=dev)
+    if tuple(Y.shape) != (M, N) or Y.dtype != dt or (prev_Y is not None and prev_Y.dtype != dt):
+        raise ValueError("Y and prev_Y must be [M, N] of X's dtype")
+    yp, ldy = _mat(Y, "Y")
+    pp, ldp = _mat(prev_Y, "prev_Y")
+    if prev_Y is not None and ldp != ldy:
+        raise ValueError("prev_Y must share Y's leading dimension")
+    c = keep_idx.numel() if keep_idx is not None and mode == DROP_K else K
+    xq, ldxq, xs, ldxs, _ = _mx(x_mx, M, c, "X")
+    wq, ldwq, ws, ldws, w_fmt = _mx(W, N, c, "W")
+    _check(_lib.zr_mx_linear_fwd(xp, ldx, xq, ldxq, xs, ldxs, x_fmt, wq, ldwq, ws, ldws, w_fmt, yp, ldy, M, K, N,
+                                 None if keep_idx is None else keep_idx.data_ptr(),
+                                 0 if keep_idx is None else keep_idx.numel(), mode, _dtype_code(Y), policy, pp, _stream(stream)))
+    return Y
+
+
+def mx_bwd_workspace_bytes(M: int, K: int, N: int, n_keep: int, mode: int, dtype) -> int:
+    code = dtype if isinstance(dtype, int) else (BF16 if dtype == torch.bfloat16 else F32)
+    return int(_lib.zr_mx_bwd_workspace_bytes(M, K, N, n_keep, mode, code))
+
+
+def resized_linear_bwd_mx(X: Optional[MX], W: torch.Tensor, dY: torch.Tensor, keep_idx: torch.Tensor, mode: int, policy: int = ZERO,
+                          prev_dX: Optional[torch.Tensor] = None, prev_dW: Optional[torch.Tensor] = None,
+                          dX: Optional[torch.Tensor] = None, dW: Optional[torch.Tensor] = None, need_dX: bool = True,
+                          need_dW: bool = True, workspace: Optional[torch.Tensor] = None, stream=None,
+                          w_layout: int = W_KN) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor]]:
+    """resized_linear_bwd from the checkpoint of X: [M, n_keep] in blocks (DROP_K) or [M, K] (DROP_N).  workspace: of
+    mx_bwd_workspace_bytes bytes, needed for dW (None: allocated)."""
+    M, N = dY.shape
+    _placed(stream, keep_idx, W, dY, dX, dW, prev_dX, prev_dW, workspace, *((X.q, X.scales) if need_dW else ()))
+    K = W.shape[0] if w_layout == W_KN else W.shape[1]
+    wshape = (K, N) if w_layout == W_KN else (N, K)
+    if tuple(W.shape) != wshape or W.dtype != dY.dtype:
+        raise ValueError("dY must be [M, N] and W [K, N] (W_KN) or [N, K] (W_NK) of its dtype")
+    n_keep = keep_idx.numel()
+    if need_dX and dX is None:
+        dX = torch.empty((M, K), dtype=dY.dtype, device=dY.device)
+    if need_dW and dW is None:
+        dW = torch.empty(wshape, dtype=dY.dtype, device=dY.device)
+    if need_dW and workspace is None:
+        workspace = torch.empty(mx_bwd_workspace_bytes(M, K, N, n_keep, mode, dY.dtype), dtype=torch.uint8, device=dY.device)
+        if stream is not None:
+            workspace.record_stream(stream)
+    for t, shape in ((dX if need_dX else None, (M, K)), (dW if need_dW else None, wshape), (prev_dX, (M, K)), (prev_dW, wshape)):
+        if t is not None and (tuple(t.shape) != shape or t.dtype != dY.dtype):
+            raise ValueError("dX, dW and the previous tensors have the shapes of X and W and dY's dtype")
+    (wp, ldw), (gp, ldg) = _mat(W, "W"), _mat(dY, "dY")
+    (dxp, lddx), (dwp, lddw) = _mat(dX if need_dX else None, "dX"), _mat(dW if need_dW else None, "dW")
+    (pxp, ldpx), (pwp, ldpw) = _mat(prev_dX, "prev_dX"), _mat(prev_dW, "prev_dW")
+    if (prev_dX is not None and need_dX and ldpx != lddx) or (prev_dW is not None and need_dW and ldpw != lddw):
+        raise ValueError("previous tensors must share the outputs' leading dimensions")
+    xq, ldxq, xs, ldxs, fmt = _mx(X if need_dW else None, M, n_keep if mode == DROP_K else K, "X")
+    _check(_lib.zr_resized_linear_bwd_mx(xq, ldxq, xs, ldxs, fmt, wp, ldw, gp, ldg, dxp, lddx, dwp, lddw, M, K, N,
+                                         keep_idx.data_ptr(), n_keep, mode, w_layout, _dtype_code(dY), policy, pxp, pwp,
+                                         *_ws(workspace), _stream(stream)))
+    return (dX if need_dX else None), (dW if need_dW else None)
 
 
 def priority_scores(W_t: torch.Tensor, W_prev: torch.Tensor, mode: int,

@@ -1,0 +1,576 @@
+"""Block-scaled operators against the 64-bit definition (mx_util): bytes of the stored form exactly, products and gradients
+within bounds that follow from the formats.
+
+Bounds.  The stored form is a pure function of the input: every byte is compared.  A product's factors are what the blocks
+stand for, so only its sums round: fp32 sums of C exact terms p are off by at most (C + 8) 2^-23 sum |p| whatever their
+order, an 8-bit operand of a bf16 result adds 2^-13 of the largest of each group of eight products for each of them, and the
+result is rounded once (half a step).  The whole tensor: one rounding to bf16 gives 1.7e-3, failed above 5e-3; fp32
+results have to stay within the random walk of their sums, 8 sqrt(C) 2^-24."""
+import numpy as np
+import pytest
+
+from mx_util import E2M1, E4M3, INT8, NAMES, quantize, stored
+from parity_util import acc_term, check_kept_np
+
+pytestmark = pytest.mark.gpu
+
+DROP_N, DROP_K = 0, 1
+W_KN, W_NK = 0, 1
+ZERO, AVERAGE, SAME = 0, 1, 2
+FORMATS = [E4M3, E2M1, INT8]
+U = {"bf16": 2.0 ** -8, "f32": 2.0 ** -24}
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch as t
+    if not t.cuda.is_available():
+        pytest.skip("needs a GPU")
+    return t
+
+
+@pytest.fixture(scope="module")
+def zr(torch):
+    from paper_2401_11469_amd import zr as z
+    return z
+
+
+def tdt(torch, dtype):
+    return torch.bfloat16 if dtype == "bf16" else torch.float32
+
+
+def values(seed, *shape, spread=1.0):
+    """Normal values with rows and columns of unlike size."""
+    rng = np.random.Generator(np.random.PCG64(seed))
+    x = rng.standard_normal(shape) * np.exp(spread * rng.standard_normal(shape[-1:]))
+    return x * np.exp(spread * rng.standard_normal(shape[:-1] + (1,)))
+
+
+def put(torch, x, dtype, ld=None, offset=0):
+    """x on the GPU in `dtype`, rows `ld` apart, `offset` elements into its buffer; and its exact values in float64."""
+    t = torch.from_numpy(np.ascontiguousarray(x)).to(tdt(torch, dtype))
+    rows, cols = x.shape
+    ld = ld or cols
+    buf = torch.full((offset + rows * ld,), 77.0, dtype=t.dtype)
+    view = buf[offset:].view(rows, ld)
+    view[:, :cols] = t
+    dev = buf.cuda()
+    return dev[offset:].view(rows, ld)[:, :cols], t.double().numpy()
+
+
+def subset(seed, n, k):
+    return np.sort(np.random.Generator(np.random.PCG64(seed)).permutation(n)[:k]).astype(np.int32)
+
+
+def idx(torch, s):
+    return torch.from_numpy(s).cuda()
+
+
+def to_np(t):
+    return t.double().cpu().numpy()
+
+
+def mx_put(torch, zr, x, fmt):
+    """x (float64, exact) in blocks by the reference, on the GPU; and what it stands for."""
+    codes, scales, vals = quantize(x, fmt)
+    el, sc = stored(codes, scales, fmt)
+    return zr.MX(torch.from_numpy(el).cuda(), torch.from_numpy(sc).cuda(), x.shape[1], fmt), vals
+
+
+def same_bytes(m, codes, scales, fmt):
+    el, sc = stored(codes, scales, fmt)
+    got_e, got_s = m.q.cpu().numpy(), m.scales.cpu().numpy()
+    assert np.array_equal(got_s[:, :sc.shape[1]], sc), NAMES[fmt]
+    bad = got_e[:, :el.shape[1]] != el
+    if fmt == E2M1 and bad.any():
+        raise AssertionError((np.argwhere(bad)[:4], got_e[bad][:4], el[bad][:4]))
+    assert not bad.any(), (NAMES[fmt], np.argwhere(bad)[:4], got_e[:, :el.shape[1]][bad][:4], el[bad][:4])
+
+
+# ---------------------------------------------------------------------------
+# Into blocks and back
+# ---------------------------------------------------------------------------
+SIZES = [(1, 1), (1, 32), (3, 31), (5, 33), (4, 127), (2, 129), (7, 512), (6, 513), (9, 1000), (33, 2064), (130, 96)]
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,n", SIZES)
+def test_rows_into_blocks(torch, zr, rows, n, dtype, fmt):
+    for ld, offset in ((n, 0), ((n + 15) // 8 * 8, 0), (n + 3, 1)):
+        src, x = put(torch, values(rows * 1000 + n, rows, n), dtype, ld, offset)
+        same_bytes(zr.mx_quantize(src, fmt), *quantize(x, fmt)[:2], fmt)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,n,kind", [(1, 1, "one"), (5, 40, "one"), (6, 513, "half"), (9, 1000, "random"), (33, 2064, "random"),
+                                         (3, 700, "head"), (3, 700, "tail"), (2, 640, "all")])
+def test_kept_columns_into_blocks(torch, zr, rows, n, kind, dtype, fmt):
+    s = {"one": np.array([n // 2], np.int32), "half": np.arange(0, n, 2, dtype=np.int32), "random": subset(n, n, (3 * n) // 4),
+         "head": np.arange(n // 3, dtype=np.int32), "tail": np.arange(n - n // 3, n, dtype=np.int32), "all": np.arange(n, dtype=np.int32)}[kind]
+    for ld, offset in ((n, 0), (n + 3, 1)):
+        src, x = put(torch, values(rows + n, rows, n), dtype, ld, offset)
+        same_bytes(zr.mx_quantize(src, fmt, keep_idx=idx(torch, s)), *quantize(x[:, s], fmt)[:2], fmt)
+
+
+@pytest.mark.parametrize("dtype,n", [("bf16", 40000), ("f32", 20000)])
+def test_rows_longer_than_the_staging(torch, zr, dtype, n):
+    src, x = put(torch, values(n, 2, n), dtype)
+    s = subset(n, n, n // 2 + 5)
+    same_bytes(zr.mx_quantize(src, INT8, keep_idx=idx(torch, s)), *quantize(x[:, s], INT8)[:2], INT8)
+    src, x = put(torch, values(n, 2, n), dtype, n + 1, 1)
+    same_bytes(zr.mx_quantize(src, E4M3), *quantize(x, E4M3)[:2], E4M3)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,cols,keep", [(1, 1, 0), (31, 5, 0), (33, 64, 20), (129, 72, 0), (512, 65, 0), (640, 130, 517), (1000, 24, 750), (700, 9, 1)])
+def test_columns_into_blocks(torch, zr, rows, cols, keep, dtype, fmt):
+    s = subset(rows, rows, keep) if keep else None
+    for ld, offset in ((cols, 0), ((cols + 15) // 8 * 8, 0), (cols + 3, 1)):
+        src, x = put(torch, values(rows + cols, rows, cols), dtype, ld, offset)
+        got = zr.mx_quantize(src, fmt, axis=0, keep_idx=None if s is None else idx(torch, s))
+        same_bytes(got, *quantize((x if s is None else x[s]).T, fmt)[:2], fmt)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_special_values(torch, zr, fmt):
+    rng = np.random.Generator(np.random.PCG64(fmt))
+    x = rng.standard_normal((14, 96)).astype(np.float32)
+    x[0, 3], x[1, 40], x[2, 95] = np.nan, np.inf, -np.inf           # a block of NaN each
+    x[3] = 0.0
+    x[4] = -0.0
+    x[5, :32] = 0.0
+    x[6] *= np.float32(2.0 ** -126)                                 # subnormal in part
+    x[7] = np.float32(2.0 ** -149) * rng.integers(0, 9, 96)
+    x[8] = np.float32(3.4028234e38) * rng.choice([-1, 1], 96)
+    x[9] *= np.float32(2.0 ** 126)
+    x[10, 0] = 1e30                                                 # everything else of the block far below its steps
+    g = {E4M3: 448.0, E2M1: 6.0, INT8: 127 / 64}[fmt]
+    x[11, :32] = g                                                  # exactly the largest value, and just above it
+    x[11, 32:64] = np.nextafter(np.float32(g), np.float32(1e9))
+    x[12] = (rng.integers(0, 128, 96) + 0.5) / 64                   # ties of the integers
+    x[12, ::32] = 127 / 64
+    x[13] = rng.choice([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0], 96)
+    x[13, ::32] = 6.0                                               # ties of the 4-bit grid
+    src, xv = put(torch, x, "f32")
+    with np.errstate(over="ignore"):
+        codes, scales, vals = quantize(xv, fmt)
+    m = zr.mx_quantize(src, fmt)
+    el, sc = stored(codes, scales, fmt)
+    assert np.array_equal(m.scales.cpu().numpy(), sc)
+    got = to_np(zr.mx_dequantize(m, torch.float32))
+    assert np.array_equal(np.isnan(got), np.isnan(vals)) and np.isnan(vals).sum() == 3 * 32
+    # rounded to the type of the result: 3.4e38 is held as 2^128 in 8 bits, which fp32 has as an infinity
+    with np.errstate(over="ignore"):
+        assert np.array_equal(got.astype(np.float32), vals.astype(np.float32), equal_nan=True)
+    src, xv = put(torch, x.T.copy(), "f32")
+    m0 = zr.mx_quantize(src, fmt, axis=0)
+    assert torch.equal(m0.q, m.q) and torch.equal(m0.scales, m.scales)
+    # the same block wherever it lies
+    both = torch.equal(zr.mx_quantize(put(torch, x, "f32", 99, 1)[0], fmt).q, m.q)
+    assert both
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,n", SIZES)
+def test_blocks_back_into_values(torch, zr, rows, n, dtype, fmt):
+    m, vals = mx_put(torch, zr, values(n, rows, n), fmt)
+    for ld, offset in ((n, 0), ((n + 15) // 8 * 8, 0), (n + 3, 1)):
+        buf = torch.full((offset + (rows + 1) * ld,), 77.0, dtype=tdt(torch, dtype), device="cuda")
+        out = buf[offset:].view(rows + 1, ld)
+        zr.mx_dequantize(m, out=out[:rows, :n])
+        assert np.array_equal(to_np(out[:rows, :n]), vals), NAMES[fmt]      # held exactly in bf16, too
+        assert torch.all(out[:rows, n:] == 77.0) and torch.all(out[rows] == 77.0) and torch.all(buf[:offset] == 77.0)
+
+
+@pytest.mark.parametrize("axis", [0, 1])
+def test_pitched_storage_stays_clean(torch, zr, axis):
+    """Rows of elements and scales further apart than they are long: what lies between and behind stays as it was."""
+    x = values(3, 70, 150) if axis == 1 else values(3, 150, 70)
+    src, xv = put(torch, x, "bf16")
+    q = torch.full((72, 256 + 48), 99, dtype=torch.uint8, device="cuda")
+    s = torch.full((72, 32), 98, dtype=torch.uint8, device="cuda")
+    m = zr.MX(q[:70], s[:70], 150, E4M3)
+    zr.mx_quantize(src, E4M3, axis=axis, out=m)
+    same_bytes(m, *quantize(xv if axis == 1 else xv.T, E4M3)[:2], E4M3)
+    assert torch.all(q[:70, 256:] == 99) and torch.all(q[70:] == 99) and torch.all(s[:70, 16:] == 98) and torch.all(s[70:] == 98)
+    assert np.array_equal(to_np(zr.mx_dequantize(m, torch.float32)), quantize(xv if axis == 1 else xv.T, E4M3)[2])
+
+
+# ---------------------------------------------------------------------------
+# The product
+# ---------------------------------------------------------------------------
+def check_product(got, xv, wv, dtype, cut, name):
+    """got [M, J] against xv [M, C] wv [J, C]^T; cut: an operand has 8 bits and the result is bf16."""
+    C = xv.shape[1]
+    want = xv @ wv.T
+    bound = (C + 8) * 2.0 ** -23 * (np.abs(xv) @ np.abs(wv).T)
+    if cut:
+        pad = -C % 8
+        top = lambda v: np.pad(np.abs(v), ((0, 0), (0, pad))).reshape(v.shape[0], -1, 8).max(axis=2)  # noqa: E731
+        bound += 8 * 2.0 ** -13 * (top(xv) @ top(wv).T)
+    bound = bound * (1 + U[dtype]) + U[dtype] * np.abs(want)
+    g = to_np(got)
+    assert np.all(np.isfinite(g)), name
+    over = np.abs(g - want) - bound
+    assert np.all(over <= 0), (name, int((over > 0).sum()), float(over.max()))
+    rel = np.linalg.norm(g - want) / max(np.linalg.norm(want), 1e-300)
+    assert rel <= (5e-3 if dtype == "bf16" else acc_term(C)), (name, rel)
+
+
+PAIRS = [(E4M3, E2M1), (E2M1, E2M1), (E4M3, E4M3)]
+
+
+@pytest.mark.parametrize("xf,wf", PAIRS)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M,K,N", [(1, 1, 1), (1, 128, 16), (2, 33, 17), (16, 700, 40), (17, 512, 33), (32, 129, 64), (48, 1100, 50), (64, 260, 100),
+                                   (65, 64, 65), (100, 1000, 70), (200, 640, 300), (129, 2100, 129)])
+def test_product(torch, zr, M, K, N, dtype, xf, wf):
+    src, x = put(torch, values(M + K, M, K, spread=0.5), dtype, K + 5, 1)
+    w, wv = mx_put(torch, zr, 0.05 * values(N + K, N, K, spread=0.5), wf)
+    xm, xv = mx_put(torch, zr, x, xf)
+    cut = dtype == "bf16" and xf == E4M3
+    Y = zr.mx_linear_fwd(xm, w, dtype=tdt(torch, dtype))
+    check_product(Y, xv, wv, dtype, cut, "from blocks")
+    # from X itself: the checkpoint is the quantiser's, the result is the same to the bit
+    ck = zr.mx_empty(M, K, xf)
+    assert torch.equal(zr.mx_linear_fwd(src, w, x_fmt=xf, x_mx=ck), Y)
+    assert torch.equal(ck.q, xm.q) and torch.equal(ck.scales, xm.scales)
+    assert torch.equal(zr.mx_linear_fwd(src, w, x_fmt=xf), Y)              # nothing kept (up to 16 rows: one launch)
+    # rows further apart, at an odd element, and what lies around them
+    buf = torch.full((1 + (M + 1) * (N + 7),), 77.0, dtype=tdt(torch, dtype), device="cuda")
+    out = buf[1:].view(M + 1, N + 7)
+    zr.mx_linear_fwd(xm, w, Y=out[:M, :N])
+    assert torch.equal(out[:M, :N], Y) and torch.all(out[:M, N:] == 77.0) and torch.all(out[M] == 77.0) and buf[0] == 77.0
+
+
+@pytest.mark.parametrize("xf,wf", PAIRS)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M,K,N", [(2600, 300, 4000), (1500, 1024, 2100)])
+def test_product_on_larger_tiles(torch, zr, M, K, N, dtype, xf, wf):
+    src, x = put(torch, values(M, M, K, spread=0.3), dtype)
+    w, wv = mx_put(torch, zr, 0.05 * values(N, N, K, spread=0.3), wf)
+    ck = zr.mx_empty(M, K, xf)
+    Y = zr.mx_linear_fwd(src, w, x_fmt=xf, x_mx=ck)
+    xv = to_np(zr.mx_dequantize(ck, torch.float32))
+    check_product(Y, xv, wv, dtype, dtype == "bf16" and xf == E4M3, "large")
+    assert torch.equal(zr.mx_linear_fwd(src, w, x_fmt=xf, x_mx=ck), Y)
+    s = subset(N, N, N * 3 // 4)
+    prev = torch.randn(M, N, device="cuda").to(Y.dtype)
+    Z = zr.mx_linear_fwd(ck, w, idx(torch, s), DROP_N, SAME, prev_Y=prev, dtype=Y.dtype)
+    kept = torch.zeros(N, dtype=torch.bool)
+    kept[s.astype(np.int64)] = True
+    assert torch.equal(Z[:, kept], Y[:, kept]) and torch.equal(Z[:, ~kept], prev[:, ~kept])
+
+
+@pytest.mark.parametrize("policy", [ZERO, AVERAGE, SAME])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M,K,N,kind", [(1, 300, 100, "random"), (16, 64, 7, "one"), (40, 200, 333, "random"), (70, 130, 600, "sparse"), (150, 500, 257, "half"),
+                                        (150, 128, 200, "head"), (20, 128, 200, "tail"), (90, 96, 64, "all"), (300, 96, 2500, "gap"), (8, 96, 2500, "gap")])
+def test_product_of_kept_features(torch, zr, M, K, N, kind, dtype, policy):
+    s = {"one": np.array([N // 2], np.int32), "half": np.arange(0, N, 2, dtype=np.int32), "random": subset(N, N, (3 * N) // 4),
+         "sparse": subset(N, N, 3), "head": np.arange(N // 3, dtype=np.int32), "tail": np.arange(N - N // 3, N, dtype=np.int32),
+         "all": np.arange(N, dtype=np.int32), "gap": np.r_[0:40, N - 30:N].astype(np.int32)}[kind]
+    xm, xv = mx_put(torch, zr, values(M, M, K, spread=0.3), E4M3)
+    w, wv = mx_put(torch, zr, 0.05 * values(N, N, K, spread=0.3), E2M1)
+    drop = np.setdiff1d(np.arange(N), s)
+    for ld, offset in (((N + 7) // 8 * 8, 0), (N + 5, 1)):
+        prev, pv = put(torch, values(9, M, N), dtype, ld, offset)
+        buf = torch.full((offset + (M + 1) * ld,), 77.0, dtype=tdt(torch, dtype), device="cuda")
+        Y = buf[offset:].view(M + 1, ld)
+        zr.mx_linear_fwd(xm, w, idx(torch, s), DROP_N, policy, prev_Y=prev if policy == SAME else None, Y=Y[:M, :N])
+        y = to_np(Y[:M, :N])
+        check_product(Y[:M, :N][:, torch.from_numpy(s).long().cuda()], xv, wv[s], dtype, dtype == "bf16", kind)
+        if policy == ZERO:
+            assert np.all(y[:, drop] == 0) and not np.signbit(y[:, drop]).any()
+        elif policy == SAME:
+            assert np.array_equal(y[:, drop], pv[:, drop])
+            # in place: dropped positions stay
+            alias = prev.clone() if offset == 0 else prev
+            kept_before = to_np(alias)[:, drop]
+            zr.mx_linear_fwd(xm, w, idx(torch, s), DROP_N, SAME, prev_Y=alias, Y=alias)
+            assert np.array_equal(to_np(alias)[:, drop], kept_before) and np.array_equal(to_np(alias)[:, s], y[:, s])
+        elif drop.size:
+            mean = y[:, s].mean(axis=1, keepdims=True)
+            assert np.all(np.abs(y[:, drop] - mean) <= U[dtype] * np.abs(mean) + 2.0 ** -18 * np.abs(y[:, s]).max())
+        assert torch.all(Y[:M, N:] == 77.0) and torch.all(Y[M] == 77.0)
+
+
+@pytest.mark.parametrize("xf,wf", PAIRS)
+@pytest.mark.parametrize("M,K,N,keep", [(1, 300, 40, 200), (5, 1001, 77, 1), (16, 640, 30, 513), (33, 300, 40, 225), (150, 1001, 77, 751)])
+def test_product_of_part_of_the_contraction(torch, zr, M, K, N, keep, xf, wf):
+    s = subset(K, K, keep)
+    src, x = put(torch, values(M, M, K, spread=0.3), "bf16", K + 1, 1)
+    W, wsrc = put(torch, 0.05 * values(N, K, N, spread=0.3), "bf16")
+    k = idx(torch, s)
+    wm = zr.mx_quantize(W, wf, axis=0, keep_idx=k)
+    wv = quantize(wsrc[s].T, wf)[2]
+    xv = quantize(x[:, s], xf)[2]
+    ck = zr.mx_empty(M, keep, xf)
+    Y = zr.mx_linear_fwd(src, wm, k, DROP_K, x_fmt=xf, x_mx=ck)
+    check_product(Y, xv, wv, "bf16", xf == E4M3, "kept part")
+    same_bytes(ck, *quantize(x[:, s], xf)[:2], xf)
+    assert torch.equal(zr.mx_linear_fwd(src, wm, k, DROP_K, x_fmt=xf), Y)
+    assert torch.equal(zr.mx_linear_fwd(ck, wm, k, DROP_K, K=K), Y)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("xf,wf", PAIRS)
+@pytest.mark.parametrize("M", [4, 40, 100])
+def test_product_of_blocks_that_are_not_finite(torch, zr, M, xf, wf, dtype):
+    """A NaN or an infinity reaches its row (of X) or its column (of W) and no other result."""
+    x, w = values(1, M, 200, spread=0.2), 0.1 * values(2, 70, 200, spread=0.2)
+    x[2, 150], w[5, 3], w[66, 199] = np.inf, np.nan, -np.inf
+    src, xs = put(torch, x, dtype)
+    wsrc, ws = put(torch, w, dtype)
+    wm = zr.mx_quantize(wsrc, wf)
+    y = to_np(zr.mx_linear_fwd(src, wm, x_fmt=xf, x_mx=zr.mx_empty(M, 200, xf)))
+    bad = np.zeros(y.shape, bool)
+    bad[2], bad[:, [5, 66]] = True, True
+    assert np.array_equal(np.isnan(y), bad)
+    if M <= 16:
+        assert np.array_equal(np.isnan(to_np(zr.mx_linear_fwd(src, wm, x_fmt=xf))), bad)
+
+
+# ---------------------------------------------------------------------------
+# Gradients from the checkpoint
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("mode,layout", [(DROP_K, W_KN), (DROP_N, W_NK), (DROP_K, W_NK), (DROP_N, W_KN)])
+@pytest.mark.parametrize("M,K,N,ratio,policy", [(1, 40, 24, 0.25, ZERO), (130, 100, 77, 0.3, SAME), (200, 264, 328, 0.25, AVERAGE), (600, 520, 256, 0.0, ZERO)])
+def test_gradients_from_a_checkpoint(torch, zr, M, K, N, ratio, policy, mode, layout, dtype, fmt):
+    n = K if mode == DROP_K else N
+    s = subset(n, n, max(1, int((1 - ratio) * n + 0.5)))
+    keep = idx(torch, s)
+    held = values(M, M, K, spread=0.4)[:, s] if mode == DROP_K else values(M, M, K, spread=0.4)
+    xm, xv = mx_put(torch, zr, held, fmt)
+    W, wv = put(torch, 0.05 * values(1, *((K, N) if layout == W_KN else (N, K))), dtype)
+    dY, gv = put(torch, values(2, M, N, spread=0.2), dtype)
+    pX, pxv = put(torch, values(3, M, K), dtype)
+    pW, pwv = put(torch, values(4, *W.shape), dtype)
+    prev = dict(prev_dX=pX, prev_dW=pW) if policy == SAME else {}
+    ws = torch.full((zr.mx_bwd_workspace_bytes(M, K, N, s.size, mode, W.dtype),), 0x7f, dtype=torch.uint8, device="cuda")
+    dX, dW = zr.resized_linear_bwd_mx(xm, W, dY, keep, mode, policy, workspace=ws, w_layout=layout, **prev)
+    w = wv if layout == W_KN else wv.T                                      # [K, N]
+    dw = to_np(dW) if layout == W_KN else to_np(dW).T
+    pw = pwv if layout == W_KN else pwv.T
+    if mode == DROP_K:
+        parts = [("dX", to_np(dX)[:, s], gv @ w[s].T, N), ("dW", dw[s], xv.T @ gv, M)]
+    else:
+        parts = [("dX", to_np(dX), gv[:, s] @ w[:, s].T, s.size), ("dW", dw[:, s], xv.T @ gv[:, s], M)]
+    for name, got, want, C in parts:
+        check_kept_np(name, got, want, dtype, C)
+    drop = np.setdiff1d(np.arange(n), s)
+    if drop.size:
+        for name, got, pv, axis in (("dX", to_np(dX), pxv, 1), ("dW", dw, pw, 0 if mode == DROP_K else 1)):
+            if name == "dX" and mode == DROP_N:
+                continue
+            lost, kept = np.take(got, drop, axis), np.take(got, s, axis)
+            if policy == ZERO:
+                assert np.all(lost == 0), name
+            elif policy == SAME:
+                assert np.array_equal(lost, np.take(pv, drop, axis)), name
+            else:
+                mean = kept.mean(axis=axis, keepdims=True)
+                assert np.all(np.abs(lost - mean) <= U[dtype] * np.abs(mean) + 2.0 ** -18 * np.abs(kept).max()), name
+    # one at a time; the scratch for dW only; the smallest scratch that it accepts
+    oX, none = zr.resized_linear_bwd_mx(None, W, dY, keep, mode, policy, need_dW=False, w_layout=layout, **prev)
+    assert none is None
+    check_kept_np("dX alone", to_np(oX)[:, s] if mode == DROP_K else to_np(oX), parts[0][2], dtype, parts[0][3])
+    least = M * ((held.shape[1] + 63) // 64 * 64) * (2 if dtype == "bf16" else 4)
+    tight = torch.full((least + 64,), 0x7f, dtype=torch.uint8, device="cuda")
+    none, oW = zr.resized_linear_bwd_mx(xm, W, dY, keep, mode, policy, need_dX=False, workspace=tight[:least], w_layout=layout, **prev)
+    assert none is None and torch.all(tight[least:] == 0x7f)
+    ow = to_np(oW) if layout == W_KN else to_np(oW).T
+    check_kept_np("dW alone", ow[s] if mode == DROP_K else ow[:, s], parts[1][2], dtype, M)
+
+
+@pytest.mark.parametrize("mode", [DROP_N, DROP_K])
+def test_gradients_against_differences(torch, zr, mode):
+    """The product is linear in each operand: with X in blocks, W the values that its own blocks stand for, and L = <G, Y>, a step D of W
+    (or of X) changes L by <dW, D> exactly, up to fp32 sums.  Y comes from the block-scaled product itself where the step keeps
+    the operand representable: D doubles or removes whole blocks, which changes scales alone or zeros them."""
+    M, K, N = 40, 256, 96
+    n = K if mode == DROP_K else N
+    s = subset(5, n, n // 2)                                                # n / 2 = 128 or 48
+    keep = idx(torch, s)
+    held = values(1, M, K, spread=0.3)[:, s] if mode == DROP_K else values(1, M, K, spread=0.3)
+    xm, xv = mx_put(torch, zr, held, E4M3)
+    wm, wv = mx_put(torch, zr, 0.1 * values(2, N, held.shape[1], spread=0.3), E4M3)
+    G, gv = put(torch, values(3, M, N, spread=0.1), "f32")
+    # the layer's weight [K, N] or [N, K], with the values that the blocks stand for in the kept rows
+    W = torch.zeros((K, N) if mode == DROP_K else (N, K), device="cuda")
+    wd = zr.mx_dequantize(wm, torch.float32)
+    if mode == DROP_K:
+        W[keep.long()] = wd.t()
+    else:
+        W.copy_(wd)
+    dX, dW = zr.resized_linear_bwd_mx(xm, W, G, keep, mode, w_layout=W_KN if mode == DROP_K else W_NK)
+
+    def loss(x, w):
+        y = zr.mx_linear_fwd(x, w, keep, mode, K=K, dtype=torch.float32)
+        return float((to_np(y) * gv).sum()), float(np.abs(to_np(y) * gv).sum())
+
+    base, size = loss(xm, wm)
+    rng = np.random.Generator(np.random.PCG64(8))
+    for which in ("X", "W"):
+        for _ in range(4):
+            m, v = (xm, xv) if which == "X" else (wm, wv)
+            blocks = rng.random((v.shape[0], (v.shape[1] + 31) // 32)) < 0.3
+            d = v * np.repeat(blocks, 32, axis=1)[:, :v.shape[1]]           # doubling: D = the block's own values
+            sc = m.scales.clone()
+            for b in range(blocks.shape[1]):
+                at = b // 16 * 16 + 4 * (b % 4) + b % 16 // 4
+                sc[:, at] += torch.from_numpy(blocks[:, b].astype(np.uint8)).cuda()
+            moved = zr.MX(m.q, sc, m.n, m.fmt)
+            diff = (loss(moved, wm) if which == "X" else loss(xm, moved))[0] - base
+            if which == "X":
+                want = (to_np(dX)[:, s] * d).sum() if mode == DROP_K else (to_np(dX) * d).sum()
+            else:
+                want = (to_np(dW)[s] * d.T).sum() if mode == DROP_K else (to_np(dW)[s] * d[s]).sum()
+            assert abs(diff - want) <= 4 * acc_term(K) * size, (which, diff, want, size)
+
+
+# ---------------------------------------------------------------------------
+# Together, as they are used
+# ---------------------------------------------------------------------------
+def layer_step(zr, X, W, dY, keep, mode, bufs, policy=ZERO, stream=None):
+    """One training step of one projection: weight and input into blocks, the product, both gradients from the checkpoint."""
+    k = dict(stream=stream)
+    if mode == DROP_K:
+        zr.mx_quantize(W, bufs["w"].fmt, axis=0, keep_idx=keep, out=bufs["w"], **k)
+    else:
+        zr.mx_quantize(W, bufs["w"].fmt, out=bufs["w"], **k)
+    zr.mx_linear_fwd(X, bufs["w"], keep, mode, policy, Y=bufs["Y"], x_fmt=bufs["x"].fmt, x_mx=bufs["x"], **k)
+    zr.resized_linear_bwd_mx(bufs["x"], W, dY, keep, mode, policy, dX=bufs["dX"], dW=bufs["dW"], workspace=bufs["ws"],
+                             w_layout=0 if mode == DROP_K else 1, **k)
+
+
+def step_buffers(torch, zr, M, K, N, n_keep, mode, dt, xf, wf):
+    held = n_keep if mode == DROP_K else K
+    wshape = (K, N) if mode == DROP_K else (N, K)
+    e = lambda *s: torch.empty(s, dtype=dt, device="cuda")  # noqa: E731
+    return dict(x=zr.mx_empty(M, held, xf), w=zr.mx_empty(N, held, wf), Y=e(M, N), dX=e(M, K), dW=e(*wshape),
+                ws=torch.empty(zr.mx_bwd_workspace_bytes(M, K, N, n_keep, mode, dt), dtype=torch.uint8, device="cuda"))
+
+
+@pytest.mark.parametrize("mode", [DROP_N, DROP_K])
+@pytest.mark.parametrize("dtype,xf,wf", [("bf16", E4M3, E4M3), ("bf16", E4M3, E2M1), ("f32", E4M3, E4M3)])
+def test_training_step(torch, zr, mode, dtype, xf, wf):
+    M, K, N = 300, 520, 264
+    n = K if mode == DROP_K else N
+    scores = torch.rand(n, device="cuda")
+    keep, _ = zr.resize_select(scores, 0.25)
+    s = keep.cpu().numpy()
+    X, x = put(torch, values(1, M, K, spread=0.3), dtype)
+    W, w = put(torch, 0.05 * values(2, *((K, N) if mode == DROP_K else (N, K)), spread=0.3), dtype)
+    dY, g = put(torch, values(3, M, N, spread=0.1), dtype)
+    b = step_buffers(torch, zr, M, K, N, s.size, mode, W.dtype, xf, wf)
+    layer_step(zr, X, W, dY, keep, mode, b)
+    xv = quantize(x[:, s] if mode == DROP_K else x, xf)[2]
+    wv = quantize(w[s].T if mode == DROP_K else w, wf)[2]
+    cut = dtype == "bf16"
+    if mode == DROP_K:
+        check_product(b["Y"], xv, wv, dtype, cut, "Y")
+        check_kept_np("dX", to_np(b["dX"])[:, s], g @ w[s].T, dtype, N)
+        check_kept_np("dW", to_np(b["dW"])[s], xv.T @ g, dtype, M)
+    else:
+        check_product(b["Y"][:, keep.long()], xv, wv[s], dtype, cut, "Y")
+        check_kept_np("dX", to_np(b["dX"]), g[:, s] @ w[s], dtype, s.size)
+        check_kept_np("dW", to_np(b["dW"])[s], g[:, s].T @ xv, dtype, M)
+    # what the checkpoint costs in accuracy: dW against the uncompressed layer's, within half a step of the format on every value of X
+    full = (x[:, s] if mode == DROP_K else x)
+    err = np.linalg.norm(xv - full) / np.linalg.norm(full)
+    assert err <= 2.0 ** -4
+
+
+@pytest.mark.parametrize("mode", [DROP_N, DROP_K])
+def test_captured_steps_share_a_workspace(torch, zr, mode):
+    """Two captured steps that share scratch, replayed in turn on one stream with other inputs and eager work between."""
+    M, K, N = 130, 392, 264
+    n = K if mode == DROP_K else N
+    wshape = (K, N) if mode == DROP_K else (N, K)
+    keep = idx(torch, subset(3, n, n * 3 // 4))
+    X = torch.empty(M, K, dtype=torch.bfloat16, device="cuda")
+    W = torch.empty(wshape, dtype=torch.bfloat16, device="cuda")
+    dY = torch.empty(M, N, dtype=torch.bfloat16, device="cuda")
+
+    def fill(seed):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        for t in (X, W, dY):
+            t.copy_(torch.randn(t.shape, generator=g, device="cuda"))
+
+    fill(0)
+    sets = [step_buffers(torch, zr, M, K, N, keep.numel(), mode, torch.bfloat16, E4M3, f) for f in (E4M3, E2M1)]
+    sets[1]["ws"] = sets[0]["ws"]
+    eager = [step_buffers(torch, zr, M, K, N, keep.numel(), mode, torch.bfloat16, E4M3, f) for f in (E4M3, E2M1)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for b in sets:
+            layer_step(zr, X, W, dY, keep, mode, b)
+    torch.cuda.synchronize()
+    graphs = []
+    for b in sets:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            layer_step(zr, X, W, dY, keep, mode, b)
+        graphs.append(graph)
+    for seed in range(1, 4):
+        fill(seed)
+        for b in sets:
+            for k in ("Y", "dX", "dW"):
+                b[k].fill_(7.0)
+        for g in graphs:
+            g.replay()
+        for b in eager:
+            layer_step(zr, X, W, dY, keep, mode, b)
+        torch.cuda.synchronize()
+        for b, e in zip(sets, eager):
+            for k in ("Y", "dX", "dW"):
+                assert torch.equal(b[k], e[k]), (seed, k)
+
+
+def test_other_stream(torch, zr):
+    M, K, N = 200, 300, 140
+    X, _ = put(torch, values(1, M, K), "bf16")
+    W, _ = put(torch, 0.05 * values(2, K, N), "bf16")
+    dY, _ = put(torch, values(3, M, N), "bf16")
+    keep = idx(torch, subset(1, K, 222))
+    a, b = (step_buffers(torch, zr, M, K, N, 222, DROP_K, torch.bfloat16, E4M3, E2M1) for _ in range(2))
+    layer_step(zr, X, W, dY, keep, DROP_K, a)
+    st = torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    layer_step(zr, X, W, dY, keep, DROP_K, b, stream=st)
+    # temporaries of the call's own on that stream, while the current one allocates and writes
+    y = zr.mx_linear_fwd(X, b["w"], keep, DROP_K, stream=st)
+    dx, dw = zr.resized_linear_bwd_mx(b["x"], W, dY, keep, DROP_K, stream=st)
+    for _ in range(20):
+        torch.full((1 << 20,), 3, dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    for k in ("Y", "dX", "dW"):
+        assert torch.equal(a[k], b[k])
+    assert torch.equal(y, a["Y"]) and torch.equal(dx, a["dX"]) and torch.equal(dw, a["dW"])
+
+
+def test_binding_refusals(torch, zr):
+    x = torch.zeros(20, 64, dtype=torch.bfloat16, device="cuda")
+    w = zr.mx_empty(8, 64, E2M1)
+    keep = torch.arange(60, dtype=torch.int32, device="cuda")
+    bad = [lambda: zr.mx_quantize(x, 5), lambda: zr.mx_quantize(x.half(), E4M3), lambda: zr.mx_quantize(x.cpu(), E4M3),
+           lambda: zr.mx_quantize(x, E4M3, out=zr.mx_empty(20, 64, E2M1)), lambda: zr.mx_quantize(x, E4M3, out=zr.mx_empty(19, 64, E4M3)),
+           lambda: zr.mx_quantize(x, E4M3, keep_idx=keep.long()), lambda: zr.mx_quantize(x, E4M3, keep_idx=keep[::2]),
+           lambda: zr.mx_quantize(x[:, ::2], E4M3), lambda: zr.mx_dequantize(w, torch.float16), lambda: zr.mx_dequantize(w, out=x),
+           lambda: zr.mx_linear_fwd(x, zr.mx_empty(8, 65, E2M1)), lambda: zr.mx_linear_fwd(x, zr.mx_empty(8, 64, INT8)),
+           lambda: zr.mx_linear_fwd(x, w, x_mx=zr.mx_empty(20, 64, E2M1)), lambda: zr.mx_linear_fwd(x, w, keep, DROP_K),
+           lambda: zr.mx_linear_fwd(x, w, Y=torch.empty(20, 8, device="cuda")), lambda: zr.mx_linear_fwd(zr.mx_empty(20, 64, INT8), w),
+           lambda: zr.resized_linear_bwd_mx(zr.mx_empty(20, 60, E4M3), x[:8], x, keep, DROP_K),
+           lambda: zr.resized_linear_bwd_mx(zr.mx_empty(20, 60, E4M3), torch.zeros(64, 64, dtype=torch.bfloat16, device="cuda"), x, keep, DROP_K,
+                                            workspace=torch.empty(64, dtype=torch.uint8, device="cuda"))]
+    for f in bad:
+        with pytest.raises((ValueError, TypeError, zr.ZrError)):
+            f()
