@@ -12,6 +12,7 @@ namespace {
 
 typedef int v8i __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
@@ -28,6 +29,7 @@ struct PArgs {
     int N;
     const void* prev;
     int vec;                            // 16-byte accesses fit Y and prev
+    int i_base, j_base, i_end, j_end;   // the part of Y (of the multiplied columns) that this launch covers
     int tiles_i, tiles_j;
     const void* raw;                    // X as it arrives
     int64_t ldraw;
@@ -42,10 +44,39 @@ __device__ __forceinline__ void to_lds16(const void* gptr, uint32_t lds_uniform)
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" :: "v"(gptr), "s"(lds_uniform) : "memory");
 }
 // (and for the LDS reads, so that no read of a stage is under way when the barrier behind lets others write there)
+// the same from a uniform address plus a lane's 32-bit offset
+__device__ __forceinline__ void to_lds16(const uint8_t* base, uint32_t off, uint32_t lds_uniform)
+{
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" :: "v"(off), "s"(base), "s"(lds_uniform) : "memory");
+}
 template <int N> __device__ __forceinline__ void wait_vm()
 {
     static_assert(N >= 0 && N < 64, "vmcnt is a 6-bit field");
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(N) : "memory");
+}
+
+template <int N> __device__ __forceinline__ void wait_vm_only()
+{
+    static_assert(N >= 0 && N < 64, "vmcnt is a 6-bit field");
+    asm volatile("s_waitcnt vmcnt(%0)" :: "n"(N) : "memory");
+}
+
+// f(0), f(1), .. f(N - 1) with constants
+template <int N, int I = 0, class F> __device__ __forceinline__ void each(F&& f)
+{
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>());
+        each<N, I + 1>(f);
+    }
+}
+
+// All products before here, in the compiler's eyes too: it would sink them past the next branch.
+template <int TM, int TN, class ACC> __device__ __forceinline__ void pin(ACC (&acc)[TM][TN])
+{
+#pragma unroll
+    for (int a = 0; a < TM; ++a)
+#pragma unroll
+        for (int b = 0; b < TN; ++b) asm volatile("" : "+v"(acc[a][b]));
 }
 
 template <class T> __device__ __forceinline__ T to_out(float f);
@@ -71,6 +102,12 @@ template <int FA, int FB, int OP>
 __device__ __forceinline__ f32x4 mma(const Frag& a, uint32_t sa, const Frag& b, uint32_t sb, f32x4 c)
 {
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(as_v8(a), as_v8(b), c, FA == E2 ? 4 : 0, FB == E2 ? 4 : 0, OP, (int)sa, OP, (int)sb);
+}
+
+template <int FA, int FB, int OP>
+__device__ __forceinline__ f32x16 mma32(const Frag& a, uint32_t sa, const Frag& b, uint32_t sb, f32x16 c)
+{
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(as_v8(a), as_v8(b), c, FA == E2 ? 4 : 0, FB == E2 ? 4 : 0, OP, (int)sa, OP, (int)sb);
 }
 
 // Wide products.  The 8-bit form of the instruction adds up groups of eight products after cutting each at 2^-13 of the
@@ -186,6 +223,54 @@ __device__ void store_strip(const PArgs& g, const T* Cs, int cp, uint16_t* tab, 
     }
 }
 
+// Workgroups go round-robin to the 8 XCDs (each with its own L2): each gets a contiguous range of tiles, in groups of 4
+// tile rows.  False: beyond the last tile (the grid is padded to a multiple of 8).
+__device__ __forceinline__ bool tile_of(const PArgs& g, int& ti, int& tj)
+{
+    const int lin = (int)((blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8);
+    if (lin >= g.tiles_i * g.tiles_j) return false;
+    constexpr int GI = 4;
+    const int grp = lin / (GI * g.tiles_j), in_rows = min(GI, g.tiles_i - grp * GI), within = lin - grp * GI * g.tiles_j;
+    ti = grp * GI + within % in_rows;
+    tj = within / in_rows;
+    return true;
+}
+
+// All results of a tile to Y, strip by strip through LDS: SG 16-row (or 32-row) groups of every wavefront row at a time.
+// acc[a][b][i] of MS x MS results: row 4 (lane / MS) + i % 4 + 8 (i / 4), column lane % MS.
+template <class T, int BM, int BN, int WM, int WN, int MS, int SG, int TM, int TN, class ACC>
+__device__ void store_tile(const PArgs& g, uint8_t* smem, ACC (&acc)[TM][TN], int i0, int j0, int tid, int wave, int lane)
+{
+    constexpr int NT = 64 * WM * WN, ROWS = MS * WM * SG, CP = BN + 16 / (int)sizeof(T);
+    T* Cs = (T*)smem;
+    uint16_t* tab = (uint16_t*)(smem + ROWS * CP * sizeof(T));
+    int* sidx = (int*)(tab + WIN);
+    const int cols_valid = min(BN, g.j_end - j0);
+    int start = 0, end = 0;
+    if (g.w_rows) {
+        for (int u = tid; u < cols_valid; u += NT) sidx[u] = clamp_idx(g.w_rows[j0 + u], g.N);
+        start = j0 == 0 ? 0 : clamp_idx(g.w_rows[j0], g.N);
+        end = j0 + cols_valid >= g.J ? g.N : clamp_idx(g.w_rows[j0 + cols_valid], g.N);
+    }
+#pragma unroll
+    for (int a0 = 0; a0 < TM; a0 += SG) {
+        if (a0) __syncthreads();
+#pragma unroll
+        for (int a = a0; a < a0 + SG; ++a)
+#pragma unroll
+            for (int b = 0; b < TN; ++b) {
+                T* c = Cs + (wave / WN * (MS * SG) + (a - a0) * MS + 4 * (lane / MS)) * CP + wave % WN * (TN * MS) + b * MS + lane % MS;
+#pragma unroll
+                for (int i = 0; i < MS * MS / 64; ++i) c[(i % 4 + 8 * (i / 4)) * CP] = to_out<T>(acc[a][b][i]);
+            }
+        __syncthreads();
+        store_strip<T, BN, ROWS, NT>(g, Cs, CP, tab, sidx, j0, cols_valid, start, end, tid, [&](int r) {
+            const int row = i0 + r / (MS * SG) * (TM * MS) + a0 * MS + r % (MS * SG);
+            return row < g.i_end ? row : g.M;
+        });
+    }
+}
+
 // ---------------------------------------------------------------------------
 // Tiles of BM x BN on WM x WN wavefronts.  The contraction travels in steps of 128 through a ring of LDS stages, straight
 // from memory; the scales of four steps at a time, into two places of their own.
@@ -225,17 +310,9 @@ __global__ __launch_bounds__(64 * WM * WN) void mx_kernel(const PArgs g)
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
-    // workgroups go round-robin to the 8 XCDs: each gets a contiguous range of tiles, in groups of 4 tile rows
     int ti, tj;
-    {
-        const int lin = (int)((blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8);
-        if (lin >= g.tiles_i * g.tiles_j) return;
-        constexpr int GI = 4;
-        const int grp = lin / (GI * g.tiles_j), in_rows = min(GI, g.tiles_i - grp * GI), within = lin - grp * GI * g.tiles_j;
-        ti = grp * GI + within % in_rows;
-        tj = within / in_rows;
-    }
-    const int i0 = ti * BM, j0 = tj * BN;
+    if (!tile_of(g, ti, tj)) return;
+    const int i0 = g.i_base + ti * BM, j0 = g.j_base + tj * BN;
     const int KT = g.steps;
 
     // what this lane fetches: rows past the ends are the last one again (their results are not stored)
@@ -247,20 +324,20 @@ __global__ __launch_bounds__(64 * WM * WN) void mx_kernel(const PArgs g)
         for (int q = 0; q < S::NA; ++q) {
             const int r = RA * (wave + NW * q) + ra;
             const int chunk = (lane % (BA / 16)) ^ ((r >> 1) & (BA / 16 - 1));
-            pa[q] = g.xq + (size_t)min(i0 + r, g.M - 1) * (size_t)g.ldxq + chunk * 16;
+            pa[q] = g.xq + (size_t)min(i0 + r, g.i_end - 1) * (size_t)g.ldxq + chunk * 16;
         }
 #pragma unroll
         for (int q = 0; q < S::NB; ++q) {
             const int r = RB * (wave + NW * q) + rb;
             const int chunk = (lane % (BB / 16)) ^ ((r >> 1) & (BB / 16 - 1));
-            int j = min(j0 + r, g.J - 1);
+            int j = min(j0 + r, g.j_end - 1);
             if (g.w_rows) j = clamp_idx(g.w_rows[j], g.w_extent);
             pb[q] = g.wq + (size_t)j * (size_t)g.ldwq + chunk * 16;
         }
         const int r = 64 * (wave % S::SINST) + lane;        // tile rows of A, then of B
-        if (r < BM) psc = g.xs + (size_t)min(i0 + r, g.M - 1) * (size_t)g.ldxs;
+        if (r < BM) psc = g.xs + (size_t)min(i0 + r, g.i_end - 1) * (size_t)g.ldxs;
         else {
-            int j = min(j0 + r - BM, g.J - 1);
+            int j = min(j0 + r - BM, g.j_end - 1);
             if (g.w_rows) j = clamp_idx(g.w_rows[j], g.w_extent);
             psc = g.ws + (size_t)j * (size_t)g.ldws;
         }
@@ -378,34 +455,217 @@ __global__ __launch_bounds__(64 * WM * WN) void mx_kernel(const PArgs g)
     }
     __syncthreads();
 
-    // results: strips of 16 SG rows of every wavefront row through LDS
-    constexpr int SG = strip_groups<T, BM, BN, WM>(), ROWS = 16 * WM * SG, CP = BN + 16 / (int)sizeof(T);
-    T* Cs = (T*)smem;
-    uint16_t* tab = (uint16_t*)(smem + ROWS * CP * sizeof(T));
-    int* sidx = (int*)(tab + WIN);
-    const int cols_valid = min(BN, g.J - j0);
-    int start = 0, end = 0;
-    if (g.w_rows) {
-        for (int u = tid; u < cols_valid; u += NT) sidx[u] = clamp_idx(g.w_rows[j0 + u], g.N);
-        start = j0 == 0 ? 0 : clamp_idx(g.w_rows[j0], g.N);
-        end = j0 + BN >= g.J ? g.N : clamp_idx(g.w_rows[j0 + BN], g.N);
+    store_tile<T, BM, BN, WM, WN, 16, strip_groups<T, BM, BN, WM>(), TM, TN>(g, smem, acc, i0, j0, tid, wave, lane);
+}
+
+// ---------------------------------------------------------------------------
+// Tiles of 256 x 256 on 8 wavefronts (128 x 64 each), or of 128 x 128 on 4 (64 x 64 each).  The contraction travels in units of 128 bytes a row of X (256
+// 4-bit values, 128 8-bit ones), whole cache lines, each two matrix instructions deep (16 x 16 x 128, 32 x 32 x 64): two units
+// in LDS, one read while the other lands.  Fragments are read ahead, one memory instruction at a time between the matrix
+// instructions.  The one barrier of a unit stands where its last fragments have been read, two row groups before its last product:
+// behind it the first fragments of the next unit are read, and the unit after that may be requested.
+// ---------------------------------------------------------------------------
+template <int FA, int FB, int BM_, int BN_, int WM_, int WN_> struct Ring {
+    static constexpr bool BOTH4 = FA == E2;
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, NW = WM * WN, NT = 64 * NW;
+    static constexpr int MS = BOTH4 ? 16 : 32, KS = BOTH4 ? 128 : 64;        // matrix instruction: rows, depth
+    static constexpr int BA = 128, BB = FB == E2 && !BOTH4 ? 64 : 128;      // bytes of a row in a unit
+    static constexpr int TM = BM / WM / MS, TN = BN / WN / MS;
+    static constexpr int A_BYTES = BM * BA, UNIT = A_BYTES + BN * BB, SCALES = (BM + BN) * 64, BYTES = 2 * UNIT + SCALES;
+    static constexpr int NA = A_BYTES / 1024 / NW, NB = BN * BB / 1024 / NW, NL = NA + NB, NSX = BM / 16 / NW, NSW = BN / 16 / NW;
+    static constexpr int UG = 512 / (2 * KS);               // units that a group of 16 blocks of scales serves
+    static constexpr int SD = BOTH4 ? 1 : 2;                // dwords of scales a lane needs of a group
+    static_assert(TM >= 2 && TM % 2 == 0 && TN >= 2 && 8 * NW % 16 == 0 && 16 * NW % 32 == 0 && NSX * 16 * NW == BM && NSW * 16 * NW == BN && BYTES <= 160 * 1024, "shape");
+};
+template <class T, class R> constexpr int ring_strips()
+{
+    int sg = R::TM;
+    while (R::MS * R::WM * sg * (R::BN + 16 / (int)sizeof(T)) * (int)sizeof(T) > 139 * 1024) sg /= 2;
+    return sg;
+}
+template <class T, class R> constexpr int ring_lds()
+{
+    const int ep = R::MS * R::WM * ring_strips<T, R>() * (R::BN + 16 / (int)sizeof(T)) * (int)sizeof(T) + WIN * 2 + R::BN * 4;
+    return ep > R::BYTES ? ep : R::BYTES;
+}
+
+template <int FA, int FB, int BM, int BN, int WM, int WN, class T>
+__global__ __launch_bounds__(64 * WM * WN, 2) void mx_ring_kernel(const PArgs g)
+{
+    typedef Ring<FA, FB, BM, BN, WM, WN> R;
+    constexpr int MS = R::MS, TM = R::TM, TN = R::TN, UG = R::UG, SD = R::SD, NL = R::NL, NW = R::NW;
+    extern __shared__ __align__(16) uint8_t smem[];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int ti, tj;
+    if (!tile_of(g, ti, tj)) return;
+    const int i0 = g.i_base + ti * BM, j0 = g.j_base + tj * BN;
+    const int steps = g.steps * (128 / R::KS), units = (steps + 1) / 2, groups = (g.steps + 3) / 4;
+
+    // what this lane fetches: rows past the ends are the last one again (their results are not stored).  Chunk c of an LDS row of
+    // 128 bytes sits at c ^ ((row >> 1) & 7), of 64 bytes at c ^ ((row >> 1) & 3) ^ ((row >> 4) & 1): the LDS serves lanes
+    // 0-3, 12-15, 20-27 together (then 4-11, 16-19, 28-31), and no two of them, rows of one or of two chunks, share a bank.
+    // Offsets from uniform addresses: the tile's first row of X (and of W, where its rows follow each other; else W itself:
+    // launch_ring is only called if 32 bits reach all of it).
+    uint32_t oa[R::NA], ob[R::NB], os[R::NSX + R::NSW];
+    const uint8_t* xq = g.xq + (size_t)i0 * (size_t)g.ldxq;
+    const uint8_t* wq = g.wq + (g.w_rows ? 0 : (size_t)j0 * (size_t)g.ldwq);
+    const uint8_t* xs = g.xs + (size_t)i0 * (size_t)g.ldxs;
+    const uint8_t* ws = g.ws + (g.w_rows ? 0 : (size_t)j0 * (size_t)g.ldws);
+    uint32_t back = 0;                                      // (last unit of an odd number of steps: the second half is not there)
+    {
+        auto x_row = [&](int r) __attribute__((always_inline)) { return (uint32_t)min(r, g.i_end - 1 - i0); };
+        auto w_row = [&](int r) __attribute__((always_inline)) {
+            r = min(r, g.j_end - 1 - j0);
+            return (uint32_t)(g.w_rows ? clamp_idx(g.w_rows[j0 + r], g.w_extent) : r);
+        };
+        const int r8 = 8 * wave + (lane >> 3), c8 = (lane & 7) ^ ((r8 >> 1) & 7);       // 8 NW rows further on the same chunk
+        const int r16 = 16 * wave + (lane >> 2), c4 = (lane & 3) ^ ((r16 >> 1) & 3) ^ ((r16 >> 4) & 1);
+        if (c8 >= 4) back = 64;
+#pragma unroll
+        for (int q = 0; q < R::NA; ++q) oa[q] = x_row(r8 + 8 * NW * q) * (uint32_t)g.ldxq + (c8 << 4);
+#pragma unroll
+        for (int q = 0; q < R::NB; ++q)
+            ob[q] = R::BB == 128 ? w_row(r8 + 8 * NW * q) * (uint32_t)g.ldwq + (c8 << 4) : w_row(r16 + 16 * NW * q) * (uint32_t)g.ldwq + (c4 << 4);
+#pragma unroll
+        for (int q = 0; q < R::NSX + R::NSW; ++q)
+            os[q] = q < R::NSX ? x_row(r16 + 16 * NW * q) * (uint32_t)g.ldxs : w_row(r16 + 16 * NW * (q - R::NSX)) * (uint32_t)g.ldws;
     }
+    const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)smem);
+    // request j of unit u (behind the last one: that one again, into the place that is not read any more)
+    auto load = [&](int u, int place, int j) __attribute__((always_inline)) {
+        u = min(u, units - 1);
+        const uint32_t base = lds0 + place * R::UNIT;
+        const uint32_t less = R::BOTH4 && 2 * u + 1 >= steps ? back : 0u;
+        if (j < R::NA) to_lds16(xq + (size_t)u * R::BA, oa[j] - less, base + (wave + NW * j) * 1024);
+        else to_lds16(wq + (size_t)u * R::BB, ob[j - R::NA] - less, base + R::A_BYTES + (wave + NW * (j - R::NA)) * 1024);
+    };
+    // scales of four groups: 64 bytes a row, chunk c at c ^ ((row >> 2) & 3)
+    auto load_scales = [&](int quad, int q) __attribute__((always_inline)) {
+        const int grp = min(4 * quad + ((lane & 3) ^ ((lane >> 4) & 3)), groups - 1);
+        to_lds16(q < R::NSX ? xs : ws, os[q] + grp * 16, lds0 + 2 * R::UNIT + (wave + NW * q) * 1024);
+    };
+
+    const int wr = wave / WN * (TM * MS), wc = wave % WN * (TN * MS);
+    const int rl = lane % MS, lg = lane / MS;
+    // lane's chunk(s) of a fragment: lg of the step's half row, and lg + 2 of it in 8 bits
+    const uint32_t fa_at = (wr + rl) * 128 + ((lg ^ ((rl >> 1) & 7)) << 4);
+    const uint32_t fb_at = R::A_BYTES + (R::BB == 128 ? (wc + rl) * 128 + ((lg ^ ((rl >> 1) & 7)) << 4)
+                                                      : (wc + rl) * 64 + ((lg ^ ((rl >> 1) & 3) ^ ((rl >> 4) & 1)) << 4));
+    auto a_frag = [&](const uint8_t* un, int a, int h) __attribute__((always_inline)) {
+        Frag f;
+        f.hi = make_uint4(0u, 0u, 0u, 0u);
+        f.lo = *(const uint4*)(un + (fa_at ^ (h * 64)) + a * (MS * 128));
+        if constexpr (FA == E4) f.hi = *(const uint4*)(un + (fa_at ^ (h * 64 + 32)) + a * (MS * 128));
+        return f;
+    };
+    auto b_frag = [&](const uint8_t* un, int b, int h) __attribute__((always_inline)) {
+        Frag f;
+        f.hi = make_uint4(0u, 0u, 0u, 0u);
+        if constexpr (R::BB == 128) {
+            f.lo = *(const uint4*)(un + (fb_at ^ (h * 64)) + b * (MS * 128));
+            if constexpr (FB == E4) f.hi = *(const uint4*)(un + (fb_at ^ (h * 64 + 32)) + b * (MS * 128));
+        } else f.lo = *(const uint4*)(un + (fb_at ^ (h * 32)) + b * (MS * 64));
+        return f;
+    };
+    // scales of a group: dword 2 h + lg (or lg) of a row
+    uint32_t sa[TM][SD], sb[TN][SD];
+    const uint32_t sa_at = (wr + rl) * 64 + (((rl >> 2) & 3) << 4) + lg * 4, sb_at = (BM + wc + rl) * 64 + (((rl >> 2) & 3) << 4) + lg * 4;
+    auto a_scales = [&](int grp, int a) __attribute__((always_inline)) {
 #pragma unroll
-    for (int a0 = 0; a0 < TM; a0 += SG) {
-        if (a0) __syncthreads();
+        for (int h = 0; h < SD; ++h) sa[a][h] = *(const uint32_t*)(smem + 2 * R::UNIT + (sa_at ^ ((grp & 3) << 4)) + a * (MS * 64) + h * 8);
+    };
+    auto b_scales = [&](int grp, int b) __attribute__((always_inline)) {
 #pragma unroll
-        for (int a = a0; a < a0 + SG; ++a)
+        for (int h = 0; h < SD; ++h) sb[b][h] = *(const uint32_t*)(smem + 2 * R::UNIT + (sb_at ^ ((grp & 3) << 4)) + b * (MS * 64) + h * 8);
+    };
+    typedef std::conditional_t<MS == 16, f32x4, f32x16> ACC;
+    ACC acc[TM][TN];
 #pragma unroll
-            for (int b = 0; b < TN; ++b) {
-                T* c = Cs + (wave / WN * (16 * SG) + (a - a0) * 16 + 4 * lg) * CP + wc + b * 16 + r16;
+    for (int a = 0; a < TM; ++a)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) c[i * CP] = to_out<T>(acc[a][b][i]);
+        for (int b = 0; b < TN; ++b) acc[a][b] = ACC{};
+
+#pragma unroll
+    for (int q = 0; q < R::NSX + R::NSW; ++q) load_scales(0, q);
+#pragma unroll
+    for (int j = 0; j < NL; ++j) load(0, 0, j);
+    wait_vm<0>();
+    __builtin_amdgcn_s_barrier();
+
+    Frag fb[2][TN], fa[4];
+#pragma unroll
+    for (int b = 0; b < TN; ++b) fb[0][b] = b_frag(smem, b, 0);
+    fa[0] = a_frag(smem, 0, 0);
+    fa[1] = a_frag(smem, 1, 0);
+#pragma unroll
+    for (int a = 0; a < TM; ++a) a_scales(0, a);
+#pragma unroll
+    for (int b = 0; b < TN; ++b) b_scales(0, b);
+
+    // step H of unit u, the V-th of its group of scales
+    auto step = [&](int u, auto sub, auto half) __attribute__((always_inline)) {
+        constexpr int V = decltype(sub)::value, H = decltype(half)::value, P = H;
+        constexpr int OP = SD == 1 ? 2 * V + H : V, HS = SD == 1 ? 0 : H;
+        constexpr bool LAST = V == UG - 1 && H == 1;
+        // (units come in even numbers: the first of a group is in the first place)
+        const uint8_t* un = smem + (V & 1) * R::UNIT;
+        const uint8_t* nx = H == 0 ? un : smem + ((V + 1) & 1) * R::UNIT;
+        pin(acc);
+        // once in four groups the scales of the next four, into the place of these, which have been read
+        if (V == UG - 1 && H == 0 && (u / UG & 3) == 3) {
+#pragma unroll
+            for (int q = 0; q < R::NSX + R::NSW; ++q) load_scales(u / UG / 4 + 1, q);
+        }
+        each<TM * TN>([&](auto at) __attribute__((always_inline)) {
+            constexpr int SLOT = decltype(at)::value, a = SLOT / TN, b = SLOT % TN;
+            constexpr int FI = (a + TM * H) % 4;            // place of this row group's fragment
+            if constexpr (H == 1 && a == TM - 2 && b == 0) {
+                // the unit's last fragments have arrived here, and the next unit in LDS: the same for all wavefronts
+                wait_vm<0>();
+                __builtin_amdgcn_s_barrier();
             }
-        __syncthreads();
-        store_strip<T, BN, ROWS, NT>(g, Cs, CP, tab, sidx, j0, cols_valid, start, end, tid, [&](int r) {
-            return i0 + r / (16 * SG) * (TM * 16) + a0 * 16 + r % (16 * SG);
+            if constexpr (MS == 16) acc[a][b] = mma<FA, FB, OP>(fa[FI], sa[a][HS], fb[P][b], sb[b][HS], acc[a][b]);
+            else acc[a][b] = mma32<FA, FB, OP>(fa[FI], sa[a][HS], fb[P][b], sb[b][HS], acc[a][b]);
+            __builtin_amdgcn_sched_barrier(0);
+            // (after the last unit the reads ahead find old bytes that nothing uses)
+            if constexpr (b == 0) fa[(FI + 2) % 4] = a + 2 < TM ? a_frag(un, a + 2, H) : a_frag(nx, a + 2 - TM, H ^ 1);
+            // B fragments of the next step: behind the barrier if they are another unit's
+            constexpr int BF = H == 1 ? TM - 2 : TM >= 8 ? 2 : 0, PER = H == 1 ? (TN + 1) / 2 : 1, JB = (a - BF) * PER + b - (TN - PER);
+            if constexpr (a >= BF && b >= TN - PER && JB < TN) fb[P ^ 1][JB] = b_frag(nx, JB, H ^ 1);
+            // requests of the next unit
+            constexpr int HALF = TM * TN / 2, J0 = SLOT < HALF ? SLOT * NL / HALF : NL, J1 = SLOT < HALF ? (SLOT + 1) * NL / HALF : NL;
+            if constexpr (H == 0 && J0 < J1) {
+#pragma unroll
+                for (int j = J0; j < J1; ++j) load(u + 1, (V + 1) & 1, j);
+            }
+            // the next group's scales
+            if constexpr (LAST && a == TM - 2 && b == TN - 1) {
+#pragma unroll
+                for (int x = 0; x < TM - 1; ++x) a_scales(u / UG + 1, x);
+            }
+            if constexpr (LAST && a == TM - 1 && b == TN - 1) a_scales(u / UG + 1, a);
+            if constexpr (LAST && a == TM - 1) b_scales(u / UG + 1, b);
+            __builtin_amdgcn_sched_barrier(0);
         });
-    }
+        pin(acc);
+    };
+    constexpr std::integral_constant<int, 0> h0;
+    constexpr std::integral_constant<int, 1> h1;
+    int u = 0;
+    for (; 2 * (u + UG) <= steps; u += UG)
+        each<UG>([&](auto v) __attribute__((always_inline)) {
+            step(u + decltype(v)::value, v, h0);
+            step(u + decltype(v)::value, v, h1);
+        });
+    each<UG>([&](auto v) __attribute__((always_inline)) {
+        constexpr int V = decltype(v)::value;
+        if (2 * (u + V) < steps) step(u + V, v, h0);
+        if (2 * (u + V) + 1 < steps) step(u + V, v, h1);
+    });
+    wait_vm<0>();
+    __syncthreads();
+    store_tile<T, BM, BN, WM, WN, MS, ring_strips<T, R>(), TM, TN>(g, smem, acc, i0, j0, tid, wave, lane);
 }
 
 // ---------------------------------------------------------------------------
@@ -604,6 +864,7 @@ PArgs pargs_of(const MxProduct& p)
     g.Y = p.Y; g.ldy = p.ldy; g.N = p.N; g.prev = p.prev;
     const int es = p.dtype == ZR_BF16 ? 2 : 4;
     g.vec = (uintptr_t)p.Y % 16 == 0 && (uintptr_t)p.prev % 16 == 0 && p.ldy * es % 16 == 0;
+    g.i_base = g.j_base = 0; g.i_end = p.M; g.j_end = p.J;
     g.tiles_i = g.tiles_j = 0;
     g.raw = p.raw; g.ldraw = p.ldraw; g.raw_cols = p.raw_cols; g.raw_extent = p.raw_extent; g.C = p.C;
     return g;
@@ -615,9 +876,22 @@ int launch_tiles(PArgs g, hipStream_t stream)
     constexpr int lds = tile_lds<T, FA, FB, BM, BN, WM, WN>();
     static AttrFlags flags;
     if (!ensure_max_dynamic_lds((const void*)mx_kernel<FA, FB, BM, BN, WM, WN, WIDE, T>, lds, &flags)) return ZR_ERR_HIP;
-    g.tiles_i = (g.M + BM - 1) / BM; g.tiles_j = (g.J + BN - 1) / BN;
+    g.tiles_i = (g.i_end - g.i_base + BM - 1) / BM; g.tiles_j = (g.j_end - g.j_base + BN - 1) / BN;
     const int64_t tiles = (int64_t)g.tiles_i * g.tiles_j;
     hipLaunchKernelGGL((mx_kernel<FA, FB, BM, BN, WM, WN, WIDE, T>), dim3((uint32_t)((tiles + 7) / 8 * 8)), dim3(64 * WM * WN), lds, stream, g);
+    return hip_status(hipGetLastError());
+}
+
+template <int FA, int FB, int BM, int BN, int WM, int WN, class T>
+int launch_ring(PArgs g, hipStream_t stream)
+{
+    typedef Ring<FA, FB, BM, BN, WM, WN> R;
+    constexpr int lds = ring_lds<T, R>();
+    static AttrFlags flags;
+    if (!ensure_max_dynamic_lds((const void*)mx_ring_kernel<FA, FB, BM, BN, WM, WN, T>, lds, &flags)) return ZR_ERR_HIP;
+    g.tiles_i = (g.i_end - g.i_base + BM - 1) / BM; g.tiles_j = (g.j_end - g.j_base + BN - 1) / BN;
+    const int64_t tiles = (int64_t)g.tiles_i * g.tiles_j;
+    hipLaunchKernelGGL((mx_ring_kernel<FA, FB, BM, BN, WM, WN, T>), dim3((uint32_t)((tiles + 7) / 8 * 8)), dim3(R::NT), lds, stream, g);
     return hip_status(hipGetLastError());
 }
 
@@ -633,9 +907,15 @@ int launch_formats(const MxProduct& p, hipStream_t stream)
         else hipLaunchKernelGGL((mx_few_kernel<FA, FB, 4, WIDE, false, T>), grid, block, 0, stream, g);
         return hip_status(hipGetLastError());
     }
+    // the ring kernel's offsets within W, where its rows are picked, and within a tile
+    const uint64_t rows = p.w_rows ? (uint64_t)p.w_extent : 256;
+    const bool reach32 = rows * (uint64_t)p.W.ldq < (1ull << 32) && rows * (uint64_t)p.W.lds < (1ull << 32) &&
+                         256 * (uint64_t)p.X.ldq < (1ull << 32) && 256 * (uint64_t)p.X.lds < (1ull << 32);
     auto tiles = [&](int b) { return (int64_t)((p.M + b - 1) / b) * ((p.J + b - 1) / b); };
-    if constexpr (!WIDE)
-        if (tiles(256) >= 160) return launch_tiles<FA, FB, 256, 256, 2, 4, WIDE, T>(g, stream);
+    if constexpr (!WIDE) {
+        if (tiles(256) >= 160 && reach32) return launch_ring<FA, FB, 256, 256, 2, 4, T>(g, stream);
+        if (tiles(128) >= 160 && reach32) return launch_ring<FA, FB, 128, 128, 2, 2, T>(g, stream);
+    }
     if (tiles(128) >= 160) return launch_tiles<FA, FB, 128, 128, 2, 2, WIDE, T>(g, stream);
     return launch_tiles<FA, FB, 64, 64, 2, 2, WIDE, T>(g, stream);
 }
