@@ -465,16 +465,18 @@ __global__ __launch_bounds__(64 * WM * WN) void mx_kernel(const PArgs g)
 // instructions.  The one barrier of a unit stands where its last fragments have been read, two row groups before its last product:
 // behind it the first fragments of the next unit are read, and the unit after that may be requested.
 // ---------------------------------------------------------------------------
-template <int FA, int FB, int BM_, int BN_, int WM_, int WN_> struct Ring {
+template <int FA, int FB, int BM_, int BN_, int WM_, int WN_, int NBUF_> struct Ring {
     static constexpr bool BOTH4 = FA == E2;
     static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, NW = WM * WN, NT = 64 * NW;
     static constexpr int MS = BOTH4 ? 16 : 32, KS = BOTH4 ? 128 : 64;        // matrix instruction: rows, depth
     static constexpr int BA = 128, BB = FB == E2 && !BOTH4 ? 64 : 128;      // bytes of a row in a unit
     static constexpr int TM = BM / WM / MS, TN = BN / WN / MS;
-    static constexpr int A_BYTES = BM * BA, UNIT = A_BYTES + BN * BB, SCALES = (BM + BN) * 64, BYTES = 2 * UNIT + SCALES;
+    static constexpr int A_BYTES = BM * BA, UNIT = A_BYTES + BN * BB, SCALES = (BM + BN) * 64, NBUF = NBUF_, BYTES = NBUF * UNIT + SCALES;
     static constexpr int NA = A_BYTES / 1024 / NW, NB = BN * BB / 1024 / NW, NL = NA + NB, NSX = BM / 16 / NW, NSW = BN / 16 / NW;
     static constexpr int UG = 512 / (2 * KS);               // units that a group of 16 blocks of scales serves
+    static constexpr int UL = UG > NBUF ? UG : NBUF;        // units of one pass of the loop: whole groups, whole rounds of the places
     static constexpr int SD = BOTH4 ? 1 : 2;                // dwords of scales a lane needs of a group
+    static_assert(UL % UG == 0 && UL % NBUF == 0 && NBUF >= 2, "places");
     static_assert(TM >= 2 && TM % 2 == 0 && TN >= 2 && 8 * NW % 16 == 0 && 16 * NW % 32 == 0 && NSX * 16 * NW == BM && NSW * 16 * NW == BN && BYTES <= 160 * 1024, "shape");
 };
 template <class T, class R> constexpr int ring_strips()
@@ -489,11 +491,11 @@ template <class T, class R> constexpr int ring_lds()
     return ep > R::BYTES ? ep : R::BYTES;
 }
 
-template <int FA, int FB, int BM, int BN, int WM, int WN, class T>
+template <int FA, int FB, int BM, int BN, int WM, int WN, int NBUF, class T>
 __global__ __launch_bounds__(64 * WM * WN, 2) void mx_ring_kernel(const PArgs g)
 {
-    typedef Ring<FA, FB, BM, BN, WM, WN> R;
-    constexpr int MS = R::MS, TM = R::TM, TN = R::TN, UG = R::UG, SD = R::SD, NL = R::NL, NW = R::NW;
+    typedef Ring<FA, FB, BM, BN, WM, WN, NBUF> R;
+    constexpr int MS = R::MS, TM = R::TM, TN = R::TN, UG = R::UG, UL = R::UL, SD = R::SD, NL = R::NL, NW = R::NW;
     extern __shared__ __align__(16) uint8_t smem[];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -543,7 +545,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void mx_ring_kernel(const PArgs g)
     // scales of four groups: 64 bytes a row, chunk c at c ^ ((row >> 2) & 3)
     auto load_scales = [&](int quad, int q) __attribute__((always_inline)) {
         const int grp = min(4 * quad + ((lane & 3) ^ ((lane >> 4) & 3)), groups - 1);
-        to_lds16(q < R::NSX ? xs : ws, os[q] + grp * 16, lds0 + 2 * R::UNIT + (wave + NW * q) * 1024);
+        to_lds16(q < R::NSX ? xs : ws, os[q] + grp * 16, lds0 + NBUF * R::UNIT + (wave + NW * q) * 1024);
     };
 
     const int wr = wave / WN * (TM * MS), wc = wave % WN * (TN * MS);
@@ -573,11 +575,11 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void mx_ring_kernel(const PArgs g)
     const uint32_t sa_at = (wr + rl) * 64 + (((rl >> 2) & 3) << 4) + lg * 4, sb_at = (BM + wc + rl) * 64 + (((rl >> 2) & 3) << 4) + lg * 4;
     auto a_scales = [&](int grp, int a) __attribute__((always_inline)) {
 #pragma unroll
-        for (int h = 0; h < SD; ++h) sa[a][h] = *(const uint32_t*)(smem + 2 * R::UNIT + (sa_at ^ ((grp & 3) << 4)) + a * (MS * 64) + h * 8);
+        for (int h = 0; h < SD; ++h) sa[a][h] = *(const uint32_t*)(smem + NBUF * R::UNIT + (sa_at ^ ((grp & 3) << 4)) + a * (MS * 64) + h * 8);
     };
     auto b_scales = [&](int grp, int b) __attribute__((always_inline)) {
 #pragma unroll
-        for (int h = 0; h < SD; ++h) sb[b][h] = *(const uint32_t*)(smem + 2 * R::UNIT + (sb_at ^ ((grp & 3) << 4)) + b * (MS * 64) + h * 8);
+        for (int h = 0; h < SD; ++h) sb[b][h] = *(const uint32_t*)(smem + NBUF * R::UNIT + (sb_at ^ ((grp & 3) << 4)) + b * (MS * 64) + h * 8);
     };
     typedef std::conditional_t<MS == 16, f32x4, f32x16> ACC;
     ACC acc[TM][TN];
@@ -589,8 +591,11 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void mx_ring_kernel(const PArgs g)
 #pragma unroll
     for (int q = 0; q < R::NSX + R::NSW; ++q) load_scales(0, q);
 #pragma unroll
-    for (int j = 0; j < NL; ++j) load(0, 0, j);
-    wait_vm<0>();
+    for (int b = 0; b < NBUF - 1; ++b) {
+#pragma unroll
+        for (int j = 0; j < NL; ++j) load(b, b, j);
+    }
+    wait_vm<(NBUF - 2) * NL>();
     __builtin_amdgcn_s_barrier();
 
     Frag fb[2][TN], fa[4];
@@ -603,14 +608,13 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void mx_ring_kernel(const PArgs g)
 #pragma unroll
     for (int b = 0; b < TN; ++b) b_scales(0, b);
 
-    // step H of unit u, the V-th of its group of scales
+    // step H of unit u, the I-th of a pass and V-th of its group of scales
     auto step = [&](int u, auto sub, auto half) __attribute__((always_inline)) {
-        constexpr int V = decltype(sub)::value, H = decltype(half)::value, P = H;
+        constexpr int I = decltype(sub)::value, V = I % UG, H = decltype(half)::value, P = H;
         constexpr int OP = SD == 1 ? 2 * V + H : V, HS = SD == 1 ? 0 : H;
         constexpr bool LAST = V == UG - 1 && H == 1;
-        // (units come in even numbers: the first of a group is in the first place)
-        const uint8_t* un = smem + (V & 1) * R::UNIT;
-        const uint8_t* nx = H == 0 ? un : smem + ((V + 1) & 1) * R::UNIT;
+        const uint8_t* un = smem + I % NBUF * R::UNIT;
+        const uint8_t* nx = H == 0 ? un : smem + (I + 1) % NBUF * R::UNIT;
         pin(acc);
         // once in four groups the scales of the next four, into the place of these, which have been read
         if (V == UG - 1 && H == 0 && (u / UG & 3) == 3) {
@@ -621,8 +625,9 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void mx_ring_kernel(const PArgs g)
             constexpr int SLOT = decltype(at)::value, a = SLOT / TN, b = SLOT % TN;
             constexpr int FI = (a + TM * H) % 4;            // place of this row group's fragment
             if constexpr (H == 1 && a == TM - 2 && b == 0) {
-                // the unit's last fragments have arrived here, and the next unit in LDS: the same for all wavefronts
-                wait_vm<0>();
+                // the unit's last fragments have arrived here, and the next unit in LDS: the same for all wavefronts.  (The
+                // scales are requested before the data of their unit.)
+                wait_vm<(V == UG - 1 && NBUF > 2 ? 1 : NBUF - 2) * NL>();
                 __builtin_amdgcn_s_barrier();
             }
             if constexpr (MS == 16) acc[a][b] = mma<FA, FB, OP>(fa[FI], sa[a][HS], fb[P][b], sb[b][HS], acc[a][b]);
@@ -633,11 +638,11 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void mx_ring_kernel(const PArgs g)
             // B fragments of the next step: behind the barrier if they are another unit's
             constexpr int BF = H == 1 ? TM - 2 : TM >= 8 ? 2 : 0, PER = H == 1 ? (TN + 1) / 2 : 1, JB = (a - BF) * PER + b - (TN - PER);
             if constexpr (a >= BF && b >= TN - PER && JB < TN) fb[P ^ 1][JB] = b_frag(nx, JB, H ^ 1);
-            // requests of the next unit
+            // requests of the unit NBUF - 1 further on
             constexpr int HALF = TM * TN / 2, J0 = SLOT < HALF ? SLOT * NL / HALF : NL, J1 = SLOT < HALF ? (SLOT + 1) * NL / HALF : NL;
             if constexpr (H == 0 && J0 < J1) {
 #pragma unroll
-                for (int j = J0; j < J1; ++j) load(u + 1, (V + 1) & 1, j);
+                for (int j = J0; j < J1; ++j) load(u + NBUF - 1, (I + NBUF - 1) % NBUF, j);
             }
             // the next group's scales
             if constexpr (LAST && a == TM - 2 && b == TN - 1) {
@@ -653,12 +658,12 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void mx_ring_kernel(const PArgs g)
     constexpr std::integral_constant<int, 0> h0;
     constexpr std::integral_constant<int, 1> h1;
     int u = 0;
-    for (; 2 * (u + UG) <= steps; u += UG)
-        each<UG>([&](auto v) __attribute__((always_inline)) {
+    for (; 2 * (u + UL) <= steps; u += UL)
+        each<UL>([&](auto v) __attribute__((always_inline)) {
             step(u + decltype(v)::value, v, h0);
             step(u + decltype(v)::value, v, h1);
         });
-    each<UG>([&](auto v) __attribute__((always_inline)) {
+    each<UL>([&](auto v) __attribute__((always_inline)) {
         constexpr int V = decltype(v)::value;
         if (2 * (u + V) < steps) step(u + V, v, h0);
         if (2 * (u + V) + 1 < steps) step(u + V, v, h1);
@@ -882,16 +887,16 @@ int launch_tiles(PArgs g, hipStream_t stream)
     return hip_status(hipGetLastError());
 }
 
-template <int FA, int FB, int BM, int BN, int WM, int WN, class T>
+template <int FA, int FB, int BM, int BN, int WM, int WN, int NBUF, class T>
 int launch_ring(PArgs g, hipStream_t stream)
 {
-    typedef Ring<FA, FB, BM, BN, WM, WN> R;
+    typedef Ring<FA, FB, BM, BN, WM, WN, NBUF> R;
     constexpr int lds = ring_lds<T, R>();
     static AttrFlags flags;
-    if (!ensure_max_dynamic_lds((const void*)mx_ring_kernel<FA, FB, BM, BN, WM, WN, T>, lds, &flags)) return ZR_ERR_HIP;
+    if (!ensure_max_dynamic_lds((const void*)mx_ring_kernel<FA, FB, BM, BN, WM, WN, NBUF, T>, lds, &flags)) return ZR_ERR_HIP;
     g.tiles_i = (g.i_end - g.i_base + BM - 1) / BM; g.tiles_j = (g.j_end - g.j_base + BN - 1) / BN;
     const int64_t tiles = (int64_t)g.tiles_i * g.tiles_j;
-    hipLaunchKernelGGL((mx_ring_kernel<FA, FB, BM, BN, WM, WN, T>), dim3((uint32_t)((tiles + 7) / 8 * 8)), dim3(R::NT), lds, stream, g);
+    hipLaunchKernelGGL((mx_ring_kernel<FA, FB, BM, BN, WM, WN, NBUF, T>), dim3((uint32_t)((tiles + 7) / 8 * 8)), dim3(R::NT), lds, stream, g);
     return hip_status(hipGetLastError());
 }
 
@@ -913,8 +918,8 @@ int launch_formats(const MxProduct& p, hipStream_t stream)
                          256 * (uint64_t)p.X.ldq < (1ull << 32) && 256 * (uint64_t)p.X.lds < (1ull << 32);
     auto tiles = [&](int b) { return (int64_t)((p.M + b - 1) / b) * ((p.J + b - 1) / b); };
     if constexpr (!WIDE) {
-        if (tiles(256) >= 160 && reach32) return launch_ring<FA, FB, 256, 256, 2, 4, T>(g, stream);
-        if (tiles(128) >= 160 && reach32) return launch_ring<FA, FB, 128, 128, 2, 2, T>(g, stream);
+        if (tiles(256) >= 160 && reach32) return launch_ring<FA, FB, 256, 256, 2, 4, 2, T>(g, stream);
+        if (tiles(128) >= 160 && reach32) return (tiles(128) > 256 ? launch_ring<FA, FB, 128, 128, 2, 2, 2, T>(g, stream) : launch_ring<FA, FB, 128, 128, 2, 2, 4, T>(g, stream));
     }
     if (tiles(128) >= 160) return launch_tiles<FA, FB, 128, 128, 2, 2, WIDE, T>(g, stream);
     return launch_tiles<FA, FB, 64, 64, 2, 2, WIDE, T>(g, stream);
