@@ -900,6 +900,61 @@ int launch_ring(PArgs g, hipStream_t stream)
     return hip_status(hipGetLastError());
 }
 
+// Which tiles: 256 x 256, one to a CU; 128 x 128, two to a CU with two units of LDS each or one with four (which hide the way
+// from memory: 2048 x 8192 x 2048 in 8 bits 54 and 35 us); 64 x 64.  Each kind's time in us by the number of its tiles and the contraction in
+// 1024s, fitted to 41 sizes (128 to 12288 rows, 2048 to 4096 columns, contractions of 512, 2048 and 8192) of which each gives most within
+// 10 %; and a panel of whole rounds of the largest tiles with a second launch for the rest, where that is shorter (8192 x 4096 x 2064 in
+// 8 bits: 95 us on 256 x 256 tiles alone, 288 of them, 69 with a panel of 256).
+enum Kind { T256, T128_2, T128_4, T64 };
+struct Plan { Kind kind, rest; int i_end, j_end; double us; };      // [0, i_end) x [0, j_end) on `kind`, the rest of Y on `rest`
+
+inline int64_t tiles_of(int I, int J, int b) { return (int64_t)((I + b - 1) / b) * ((J + b - 1) / b); }
+
+template <int FA, int FB> double kind_us(Kind kind, int I, int J, int C)
+{
+    constexpr int F = FA == E2 ? 0 : FB == E2 ? 1 : 2;
+    constexpr double S256[3] = {6.15, 10.4, 11.3}, S2[3] = {4.8, 7.7, 8.45}, S4[3] = {2.3, 3.1, 3.7}, S64[3] = {1.35, 1.6, 1.9};
+    const double K = C / 1024.0;
+    // rounds of `per` tiles; the last one is the shorter the fewer tiles share the chip
+    auto rounds = [](int64_t tiles, int per, double least) {
+        const int64_t whole = tiles / per, left = tiles % per;
+        return (double)whole + (left ? least + (1.0 - least) * (double)left / per : 0.0);
+    };
+    if (kind == T256) return 4.0 + rounds(tiles_of(I, J, 256), 256, 0.62) * (9.6 + S256[F] * K);
+    const int64_t t = tiles_of(I, J, 128);
+    if (kind == T128_2) return 4.0 + rounds(t, 512, 0.55) * (2.0 + S2[F] * K);
+    if (kind == T128_4) return 1.0 + rounds(t, 256, 0.85) * (4.6 + S4[F] * K);
+    const double q = tiles_of(I, J, 64) / 256.0;
+    return 3.0 + 0.2 * q + std::max(1.0, q) * S64[F] * K;
+}
+
+template <int FA, int FB> Plan plan(int I, int J, int C)
+{
+    auto small = [&](int i, int j) {
+        Plan s{T64, T64, i, j, kind_us<FA, FB>(T64, i, j, C)};
+        for (Kind k : {T128_2, T128_4}) {
+            const double us = kind_us<FA, FB>(k, i, j, C);
+            if (us < s.us) s = Plan{k, k, i, j, us};
+        }
+        return s;
+    };
+    Plan best = small(I, J);
+    const double all = kind_us<FA, FB>(T256, I, J, C);
+    if (all < best.us) best = Plan{T256, T256, I, J, all};
+    const int ti = (I + 255) / 256, tj = (J + 255) / 256;
+    for (int64_t q = 256; q < (int64_t)ti * tj; q += 256) {
+        const int rows = (int)(q / tj), cols = (int)(q / ti);
+        for (int cut = 0; cut < 2; ++cut) {
+            if (cut ? cols < 1 || cols >= tj : rows < 1 || rows >= ti) continue;
+            const int i = cut ? I : rows * 256, j = cut ? cols * 256 : J;
+            const Plan rest = cut ? small(I, J - j) : small(I - i, J);
+            const double us = kind_us<FA, FB>(T256, i, j, C) + rest.us - 1.0;
+            if (us < best.us) best = Plan{T256, rest.kind, i, j, us};
+        }
+    }
+    return best;
+}
+
 template <int FA, int FB, bool WIDE, class T>
 int launch_formats(const MxProduct& p, hipStream_t stream)
 {
@@ -912,17 +967,30 @@ int launch_formats(const MxProduct& p, hipStream_t stream)
         else hipLaunchKernelGGL((mx_few_kernel<FA, FB, 4, WIDE, false, T>), grid, block, 0, stream, g);
         return hip_status(hipGetLastError());
     }
-    // the ring kernel's offsets within W, where its rows are picked, and within a tile
-    const uint64_t rows = p.w_rows ? (uint64_t)p.w_extent : 256;
-    const bool reach32 = rows * (uint64_t)p.W.ldq < (1ull << 32) && rows * (uint64_t)p.W.lds < (1ull << 32) &&
-                         256 * (uint64_t)p.X.ldq < (1ull << 32) && 256 * (uint64_t)p.X.lds < (1ull << 32);
-    auto tiles = [&](int b) { return (int64_t)((p.M + b - 1) / b) * ((p.J + b - 1) / b); };
-    if constexpr (!WIDE) {
-        if (tiles(256) >= 160 && reach32) return launch_ring<FA, FB, 256, 256, 2, 4, 2, T>(g, stream);
-        if (tiles(128) >= 160 && reach32) return (tiles(128) > 256 ? launch_ring<FA, FB, 128, 128, 2, 2, 2, T>(g, stream) : launch_ring<FA, FB, 128, 128, 2, 2, 4, T>(g, stream));
+    if constexpr (WIDE) {
+        // 160 tiles: 985 x 1001 x 771 7 us on 64 x 64, 12 on 128 x 128; 4096 x 2048 x 2048 57 and 44
+        if (tiles_of(p.M, p.J, 128) >= 160) return launch_tiles<FA, FB, 128, 128, 2, 2, true, T>(g, stream);
+        return launch_tiles<FA, FB, 64, 64, 2, 2, true, T>(g, stream);
+    } else {
+        const Plan best = plan<FA, FB>(p.M, p.J, p.C);
+        auto run = [&](int kind, PArgs h) {
+            // the ring kernels' offsets within W, where its rows are picked, and within a tile
+            const uint64_t rows = p.w_rows ? (uint64_t)p.w_extent : 256;
+            const bool reach = rows * (uint64_t)p.W.ldq < (1ull << 32) && rows * (uint64_t)p.W.lds < (1ull << 32) &&
+                               256 * (uint64_t)p.X.ldq < (1ull << 32) && 256 * (uint64_t)p.X.lds < (1ull << 32);
+            if (!reach || kind == T64) return launch_tiles<FA, FB, 64, 64, 2, 2, false, T>(h, stream);
+            if (kind == T256) return launch_ring<FA, FB, 256, 256, 2, 4, 2, T>(h, stream);
+            if (kind == T128_2) return launch_ring<FA, FB, 128, 128, 2, 2, 2, T>(h, stream);
+            return launch_ring<FA, FB, 128, 128, 2, 2, 4, T>(h, stream);
+        };
+        PArgs h = g;
+        h.i_end = best.i_end; h.j_end = best.j_end;
+        const int st = run(best.kind, h);
+        if (st != ZR_OK || (best.i_end == p.M && best.j_end == p.J)) return st;
+        h = g;
+        if (best.i_end < p.M) h.i_base = best.i_end; else h.j_base = best.j_end;
+        return run(best.rest, h);
     }
-    if (tiles(128) >= 160) return launch_tiles<FA, FB, 128, 128, 2, 2, WIDE, T>(g, stream);
-    return launch_tiles<FA, FB, 64, 64, 2, 2, WIDE, T>(g, stream);
 }
 
 }  // namespace
