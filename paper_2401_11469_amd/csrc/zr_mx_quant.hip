@@ -72,9 +72,10 @@ __global__ __launch_bounds__(256) void mx_rows_kernel(const T* __restrict__ src,
         if (r0 + r < rows) store_seg<FMT>(x[r], q + (size_t)(r0 + r) * (size_t)ldq, s + (size_t)(r0 + r) * (size_t)lds, n, seg, lane);
 }
 
-// Rows of any alignment, and gathered columns: RB whole rows come into LDS in aligned 16-byte chunks (the chunks at a row's
-// ends by elements), and are picked from there.
-template <class T, int FMT>
+// Rows of any alignment, and gathered columns: up to RB whole rows come into LDS in aligned 16-byte chunks, KL to a thread
+// (what lies before the first and behind the last whole chunk of a row by elements, one to a thread), the list beside them in 16
+// bits; all of it is requested at once.  The wavefronts then share out the segments of all rows.
+template <class T, int FMT, int KL, int RB>
 __global__ __launch_bounds__(256) void mx_gather_kernel(const T* __restrict__ src, int64_t ld, int rows, int cols, const int32_t* __restrict__ keep,
                                                         int n, int segs, int rb, int pitch, uint8_t* __restrict__ q, int64_t ldq,
                                                         uint8_t* __restrict__ s, int64_t lds)
@@ -83,42 +84,68 @@ __global__ __launch_bounds__(256) void mx_gather_kernel(const T* __restrict__ sr
     constexpr int ES = sizeof(T), PER = 16 / ES;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int r0 = blockIdx.x * rb, nr = min(rb, rows - r0);
-    for (int r = 0; r < nr; ++r) {
-        const T* row = src + (size_t)(r0 + r) * (size_t)ld;
-        const int off = (int)((uintptr_t)row & 15) / ES;         // elements between the aligned address and the row
-        const int chunks = (off + cols + PER - 1) / PER;
-        uint8_t* dst = stage + r * pitch;
-        for (int c0 = 0; c0 < chunks; c0 += 1024) {
-            uint4 v[4];
+    uint16_t* list = (uint16_t*)(stage + rb * pitch);
+    auto offset = [&](int r) { return (int)((uintptr_t)(src + (size_t)(r0 + r) * (size_t)ld) & 15) / ES; };    // elements behind an aligned address
+    uint4 v[RB][KL];
+    T edge[RB];
+    // threads 0 .. PER - 1: the elements before the first whole chunk; PER .. 2 PER - 1: behind the last
+    auto edge_at = [&](int off) {
+        const int head = min(off ? PER - off : 0, cols), tail = head + (cols - head) / PER * PER;
+        const int e = tid < PER ? tid : tail + tid - PER;
+        return tid < PER ? (e < head ? e : -1) : (tid < 2 * PER && e < cols ? e : -1);
+    };
+    // (rows past the last one are that one again)
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const int c = c0 + u * 256 + tid, e = c * PER - off;
-                if (e >= 0 && e + PER <= cols) v[u] = *(const uint4*)(row + e);
-            }
+    for (int r = 0; r < RB; ++r) {
+        const T* row = src + (size_t)(r0 + min(r, nr - 1)) * (size_t)ld;
+        const int off = offset(min(r, nr - 1));
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const int c = c0 + u * 256 + tid, e = c * PER - off;
-                if (e >= 0 && e + PER <= cols) *(uint4*)(dst + c * 16) = v[u];
-                else if (c < chunks) {
-                    for (int i = max(e, 0); i < min(e + PER, cols); ++i) *(T*)(dst + (off + i) * ES) = row[i];
-                }
-            }
+        for (int k = 0; k < KL; ++k) {
+            const int e = (tid + 256 * k) * PER - off;
+            v[r][k] = make_uint4(0u, 0u, 0u, 0u);
+            if (e >= 0 && e + PER <= cols) v[r][k] = *(const uint4*)(row + e);
         }
+        const int e = edge_at(off);
+        edge[r] = row[max(e, 0)];
+    }
+    if (keep)
+        for (int i0 = 0; i0 < n; i0 += 1024) {
+            int k[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) k[u] = keep[min(i0 + u * 256 + tid, n - 1)];
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (i0 + u * 256 + tid < ((n + 7) & ~7)) list[i0 + u * 256 + tid] = (uint16_t)clamp_idx(k[u], cols);
+        }
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+        uint8_t* dst = stage + r * pitch;
+        const int off = offset(min(r, nr - 1)), e1 = edge_at(off);
+#pragma unroll
+        for (int k = 0; k < KL; ++k) {
+            const int e = (tid + 256 * k) * PER - off;
+            if (r < nr && e >= 0 && e + PER <= cols) *(uint4*)(dst + (tid + 256 * k) * 16) = v[r][k];
+        }
+        if (r < nr && e1 >= 0) *(T*)(dst + (off + e1) * ES) = edge[r];
     }
     __syncthreads();
-    for (int seg = wave; seg < segs; seg += 4) {
-        const int at = seg * SEG + 8 * lane;
-        int pick[8];
+    for (int it = wave; it < nr * segs; it += 4) {
+        const int r = it / segs, seg = it - r * segs, at = seg * SEG + 8 * lane;
+        const size_t row = (size_t)(r0 + r);
+        const T* d = (const T*)(stage + r * pitch) + offset(r);
+        float x[8];
+        if (keep) {
+            const uint4 p = *(const uint4*)(list + min(at, (n - 1) & ~7));
+            const uint32_t w[4] = {p.x, p.y, p.z, p.w};
 #pragma unroll
-        for (int i = 0; i < 8; ++i) pick[i] = keep ? clamp_idx(keep[min(at + i, n - 1)], cols) : min(at + i, n - 1);
-        for (int r = 0; r < nr; ++r) {
-            const size_t row = (size_t)(r0 + r);
-            const T* d = (const T*)(stage + r * pitch) + (int)((uintptr_t)(src + row * (size_t)ld) & 15) / ES;
-            float x[8];
+            for (int i = 0; i < 8; ++i) x[i] = as_float(d[(w[i >> 1] >> (16 * (i & 1))) & 0xffffu]);
+        } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) { const float v = as_float(d[pick[i]]); x[i] = at + i < n ? v : 0.f; }
-            store_seg<FMT>(x, q + row * (size_t)ldq, s + row * (size_t)lds, n, seg, lane);
+            for (int i = 0; i < 8; ++i) x[i] = as_float(d[min(at + i, n - 1)]);
         }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = at + i < n ? x[i] : 0.f;
+        store_seg<FMT>(x, q + row * (size_t)ldq, s + row * (size_t)lds, n, seg, lane);
     }
 }
 
@@ -150,40 +177,53 @@ template <class T, int FMT, bool VEC>
 __global__ __launch_bounds__(256) void mx_cols_kernel(const T* __restrict__ src, int64_t ld, int rows, int cols, const int32_t* __restrict__ keep,
                                                       int n, uint8_t* __restrict__ q, int64_t ldq, uint8_t* __restrict__ s, int64_t lds)
 {
-    constexpr int KT = 128, CT = 64, PITCH = CT + 16 / (int)sizeof(T);
+    // (rows of any alignment: one chunk more of each, whose column c lies `shift` of its row further on)
+    constexpr int KT = 128, CT = 64, PER = 16 / (int)sizeof(T), PITCH = CT + PER * (VEC ? 1 : 2);
     constexpr int OB = FMT == ZR_MX_E2M1 ? 64 : 128, OP = OB + 16;       // bytes of a column's elements in a tile
     __shared__ __align__(16) T tile[KT * PITCH];
     __shared__ __align__(16) uint8_t outs[CT * OP];
+    __shared__ uint8_t shift[VEC ? 1 : KT];
     const int tid = threadIdx.x;
     const int c0 = blockIdx.x * CT, k0 = blockIdx.y * KT;
+    auto row_at = [&](int k) {
+        k = min(k, n - 1);
+        return src + (size_t)(keep ? clamp_idx(keep[k], rows) : k) * (size_t)ld;
+    };
     if constexpr (VEC) {
-        constexpr int PER = 16 / sizeof(T), LPR = CT / PER, RPP = 256 / LPR, PASSES = KT / RPP;
+        constexpr int LPR = CT / PER, RPP = 256 / LPR, PASSES = KT / RPP;
         uint4 v[PASSES];
 #pragma unroll
-        for (int p = 0; p < PASSES; ++p) {
-            const int k = min(k0 + p * RPP + tid / LPR, n - 1), c = c0 + tid % LPR * PER;
-            const int row = keep ? clamp_idx(keep[k], rows) : k;
-            v[p] = *(const uint4*)(src + (size_t)row * (size_t)ld + min(c, cols - PER));     // cols is a multiple of PER here
-        }
+        for (int p = 0; p < PASSES; ++p)
+            v[p] = *(const uint4*)(row_at(k0 + p * RPP + tid / LPR) + min(c0 + tid % LPR * PER, cols - PER));     // cols is a multiple of PER here
 #pragma unroll
         for (int p = 0; p < PASSES; ++p) {
             const int k = p * RPP + tid / LPR;
             *(uint4*)(tile + k * PITCH + tid % LPR * PER) = k0 + k < n ? v[p] : make_uint4(0u, 0u, 0u, 0u);
         }
     } else {
-        const int c = min(c0 + (tid & 63), cols - 1);
-        for (int i0 = 0; i0 < KT / 4; i0 += 8) {
-            T v[8];
+        constexpr int CH = CT / PER + 1, PASSES = (KT * CH + 255) / 256;
+        uint4 v[PASSES];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int k = min(k0 + (i0 + i) * 4 + (tid >> 6), n - 1);
-                v[i] = src[(size_t)(keep ? clamp_idx(keep[k], rows) : k) * (size_t)ld + c];
-            }
+        for (int p = 0; p < PASSES; ++p) {
+            const int u = p * 256 + tid, k = min(u / CH, KT - 1);
+            const T* row = row_at(k0 + k) + c0;
+            const int off = (int)((uintptr_t)row & 15) / (int)sizeof(T), e = u % CH * PER - off;       // columns c0 + e ..
+            v[p] = make_uint4(0u, 0u, 0u, 0u);
+            if (c0 + e >= 0 && c0 + e + PER <= cols) v[p] = *(const uint4*)(row + e);
+            else {                                                    // a row's first or last columns
+                union { uint4 w; T t[PER]; } x;
+                x.w = v[p];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int k = (i0 + i) * 4 + (tid >> 6);
-                tile[k * PITCH + (tid & 63)] = k0 + k < n ? v[i] : T(0);
+                for (int i = 0; i < PER; ++i)
+                    if (c0 + e + i >= 0 && c0 + e + i < cols) x.t[i] = row[e + i];
+                v[p] = x.w;
             }
+            if (u % CH == 0) shift[k] = (uint8_t)off;
+        }
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p) {
+            const int u = p * 256 + tid, k = u / CH;
+            if (k < KT) *(uint4*)(tile + k * PITCH + u % CH * PER) = k0 + k < n ? v[p] : make_uint4(0u, 0u, 0u, 0u);
         }
     }
     __syncthreads();
@@ -194,7 +234,7 @@ __global__ __launch_bounds__(256) void mx_cols_kernel(const T* __restrict__ src,
     for (int o = 0; o < 4; ++o)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            x[o][i] = as_float(tile[(blk * 32 + o * 8 + i) * PITCH + col]);
+            x[o][i] = as_float(tile[(blk * 32 + o * 8 + i) * PITCH + (VEC ? 0 : shift[VEC ? 0 : blk * 32 + o * 8 + i]) + col]);
             a = max(a, __float_as_uint(x[o][i]) & 0x7fffffffu);
         }
     const int code = mx_code<FMT>(a);
@@ -221,55 +261,73 @@ __global__ __launch_bounds__(256) void mx_cols_kernel(const T* __restrict__ src,
     }
 }
 
-__device__ __forceinline__ void put8(uint16_t* p, const float (&x)[8])
-{
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = f32_to_bf16_bits(x[2 * i]) | f32_to_bf16_bits(x[2 * i + 1]) << 16;
-    *(uint4*)p = make_uint4(w[0], w[1], w[2], w[3]);
-}
-__device__ __forceinline__ void put8(float* p, const float (&x)[8])
-{
-    *(float4*)p = make_float4(x[0], x[1], x[2], x[3]);
-    *(float4*)(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
-}
-__device__ __forceinline__ void put1(uint16_t* p, float v) { *p = (uint16_t)f32_to_bf16_bits(v); }
-__device__ __forceinline__ void put1(float* p, float v) { *p = v; }
+__device__ __forceinline__ uint32_t out_bits(float v, uint16_t) { return f32_to_bf16_bits(v); }
+__device__ __forceinline__ uint32_t out_bits(float v, float) { return __float_as_uint(v); }
 
-// Blocks back into values.  A wavefront takes a segment of four rows; VEC: 16-byte stores.
+// Blocks back into values.  A lane stores an aligned chunk of 16 bytes of a row, of four rows at a time; in a row that does not
+// begin on such an address, it is the elements that are read from odd places (a chunk may then lie in two blocks).
 template <class T, int FMT, bool VEC>
 __global__ __launch_bounds__(256) void mx_values_kernel(const uint8_t* __restrict__ q, int64_t ldq, const uint8_t* __restrict__ s, int64_t lds,
                                                         int rows, int n, int segs, T* __restrict__ out, int64_t ldo, int width)
 {
-    constexpr int RB = 4;
+    constexpr int RB = 4, PER = 16 / (int)sizeof(T);
     const int lane = threadIdx.x & 63;
     const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int r0 = (int)(item / segs) * RB, seg = (int)(item % segs);
+    const int r0 = (int)(item / segs) * RB, chunk = (int)(item % segs) * 64 + lane;
     if (r0 >= rows) return;
-    const int at = seg * SEG + 8 * lane;
-    if (at >= width) return;
-    uint2 e[RB];
-    int c[RB];
+    uint2 raw[RB];
+    int c0[RB], c1[RB], at[RB];
 #pragma unroll
     for (int r = 0; r < RB; ++r) {
         const size_t row = (size_t)min(r0 + r, rows - 1);
-        if constexpr (FMT == ZR_MX_E2M1) e[r] = make_uint2(*(const uint32_t*)(q + row * (size_t)ldq + at / 2), 0u);
-        else e[r] = *(const uint2*)(q + row * (size_t)ldq + at);
-        c[r] = s[row * (size_t)lds + mx_scale_at(seg * 16 + (lane >> 2))];
+        const int off = VEC ? 0 : (int)((uintptr_t)(out + row * (size_t)ldo) & 15) / (int)sizeof(T);
+        at[r] = chunk * PER - off;
+        // (from the row's first value where the chunk begins before it; never past the storage, whole groups of 128)
+        const int e = min(max(at[r], 0), width - 1), held = (n + 127) / 128 * 128;
+        if constexpr (FMT == ZR_MX_E2M1) {
+            const int b = VEC ? e >> 1 : min(e >> 1, (held - PER) / 2);
+            const uint8_t* p = q + row * (size_t)ldq + b;
+            uint32_t w;
+            if constexpr (PER == 8) __builtin_memcpy(&w, p, 4);
+            else { uint16_t h; __builtin_memcpy(&h, p, 2); w = h; }
+            if constexpr (!VEC)             // an odd place: half a byte more
+                w = (uint32_t)((w | (uint64_t)p[min(PER / 2, held / 2 - 1 - b)] << (4 * PER)) >> (4 * (e - 2 * b)));
+            raw[r].x = w;
+        } else {
+            const int b = VEC ? e : min(e, held - PER);
+            const uint8_t* p = q + row * (size_t)ldq + b;
+            uint64_t w = 0;
+            __builtin_memcpy(&w, p, PER);
+            if constexpr (!VEC) w >>= 8 * (e - b);
+            raw[r] = make_uint2((uint32_t)w, (uint32_t)(w >> 32));
+        }
+        const uint8_t* sr = s + row * (size_t)lds;
+        c0[r] = sr[mx_scale_at(e >> 5)];
+        c1[r] = VEC ? c0[r] : sr[mx_scale_at(min(e + PER - 1, width - 1) >> 5)];
     }
 #pragma unroll
     for (int r = 0; r < RB; ++r) {
         if (r0 + r >= rows) break;
+        const int e = min(max(at[r], 0), width - 1);
         float x[8];
-        mx_decode8<FMT>(e[r], mx_scale(c[r]), x);
+        mx_decode8<FMT>(raw[r], 1.f, x);        // (PER of them)
+        T* o = out + (size_t)(r0 + r) * (size_t)ldo;
+        uint32_t w[PER];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = at + i < n ? x[i] : 0.f;
-        T* o = out + (size_t)(r0 + r) * (size_t)ldo + at;
-        if (VEC && at + 8 <= width) put8(o, x);
-        else {
+        for (int i = 0; i < PER; ++i) {
+            const float v = x[i] * mx_scale(VEC || (e & 31) + i < 32 ? c0[r] : c1[r]);
+            w[i] = out_bits(e + i < n ? v : 0.f, T());
+        }
+        if (at[r] >= 0 && at[r] + PER <= width) {
+            if constexpr (PER == 8) *(uint4*)(o + at[r]) = make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
+            else *(uint4*)(o + at[r]) = make_uint4(w[0], w[1], w[2], w[3]);
+        } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (at + i < width) put1(o + i, x[i]);
+            for (int i = 0; i < PER; ++i)
+                if (e + i >= at[r] && e + i < min(at[r] + PER, width)) {
+                    if constexpr (PER == 8) o[e + i] = (uint16_t)w[i];
+                    else o[e + i] = __uint_as_float(w[i]);
+                }
         }
     }
 }
@@ -284,11 +342,16 @@ int quantize_rows(const T* src, int64_t ld, int rows, int cols, const int32_t* k
         hipLaunchKernelGGL((mx_rows_kernel<T, FMT>), dim3((uint32_t)((waves + 3) / 4)), dim3(256), 0, stream, src, ld, rows, n, segs, q, ldq, s, lds);
         return hip_status(hipGetLastError());
     }
-    const int pitch = (cols * es + 15 + 15) / 16 * 16;
-    if (pitch <= 64 * 1024) {
-        const int rb = std::max(1, std::min(4, 32 * 1024 / pitch));
-        hipLaunchKernelGGL((mx_gather_kernel<T, FMT>), dim3((rows + rb - 1) / rb), dim3(256), (size_t)rb * pitch, stream, src, ld, rows, cols, keep, n, segs, rb,
-                           pitch, q, ldq, s, lds);
+    const int pitch = (cols * es + 15 + 15) / 16 * 16, chunks = pitch / 16, list = keep ? (n + 7) / 8 * 16 : 0;
+    if (pitch + list <= 64 * 1024) {
+        // rows to a workgroup: four where thousands of workgroups remain, as many as 64 KB of LDS hold
+        const int rb = std::max(1, std::min({chunks <= 1024 ? 4 : chunks <= 2048 ? 2 : 1, (64 * 1024 - list) / pitch, rows / 1024}));
+#define ZR_GATHER(KL, RB)                                                                                                                      \
+        hipLaunchKernelGGL((mx_gather_kernel<T, FMT, KL, RB>), dim3((rows + rb - 1) / rb), dim3(256), (size_t)rb * pitch + list, stream, src, ld, rows, cols, \
+                           keep, n, segs, rb, pitch, q, ldq, s, lds)
+        if (chunks <= 256) ZR_GATHER(1, 4); else if (chunks <= 512) ZR_GATHER(2, 4); else if (chunks <= 1024) ZR_GATHER(4, 4);
+        else if (chunks <= 2048) ZR_GATHER(8, 2); else ZR_GATHER(16, 1);
+#undef ZR_GATHER
         return hip_status(hipGetLastError());
     }
     const int64_t waves = (int64_t)rows * segs;
@@ -311,13 +374,13 @@ int quantize_cols(const T* src, int64_t ld, int rows, int cols, const int32_t* k
 template <class T, int FMT>
 int dequantize(const MxArg& x, int rows, int n, T* out, int64_t ldo, int width, hipStream_t stream)
 {
-    const int segs = (width + SEG - 1) / SEG;
+    constexpr int PER = 16 / (int)sizeof(T);
+    const bool vec = (uintptr_t)out % 16 == 0 && ldo % PER == 0;
+    const int segs = ((width + PER - 1) / PER + (vec ? 0 : 1) + 63) / 64;
     const int64_t waves = (int64_t)((rows + 3) / 4) * segs;
     const dim3 grid((uint32_t)((waves + 3) / 4));
-    if ((uintptr_t)out % 16 == 0 && ldo * (int64_t)sizeof(T) % 16 == 0)
-        hipLaunchKernelGGL((mx_values_kernel<T, FMT, true>), grid, dim3(256), 0, stream, x.q, x.ldq, x.s, x.lds, rows, n, segs, out, ldo, width);
-    else
-        hipLaunchKernelGGL((mx_values_kernel<T, FMT, false>), grid, dim3(256), 0, stream, x.q, x.ldq, x.s, x.lds, rows, n, segs, out, ldo, width);
+    if (vec) hipLaunchKernelGGL((mx_values_kernel<T, FMT, true>), grid, dim3(256), 0, stream, x.q, x.ldq, x.s, x.lds, rows, n, segs, out, ldo, width);
+    else hipLaunchKernelGGL((mx_values_kernel<T, FMT, false>), grid, dim3(256), 0, stream, x.q, x.ldq, x.s, x.lds, rows, n, segs, out, ldo, width);
     return hip_status(hipGetLastError());
 }
 
