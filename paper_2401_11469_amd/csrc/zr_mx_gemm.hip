@@ -34,7 +34,8 @@ struct PArgs {
     const void* raw;                    // X as it arrives
     int64_t ldraw;
     const int32_t* raw_cols;
-    int raw_extent, C;
+    int raw_extent, C, raw_vec;         // raw_vec: rows of 16-byte loads, nothing gathered
+    int span;                           // values of a row of X in LDS at a time
 };
 
 // global memory -> LDS, 16 bytes a lane to 64 x 16 bytes from a wavefront-uniform address; from inline assembly, so
@@ -459,7 +460,7 @@ __global__ __launch_bounds__(64 * WM * WN) void mx_kernel(const PArgs g)
 }
 
 // ---------------------------------------------------------------------------
-// Tiles of 256 x 256 on 8 wavefronts (128 x 64 each), or of 128 x 128 on 4 (64 x 64 each).  The contraction travels in units of 128 bytes a row of X (256
+// Tiles of 256 x 256 on 8 wavefronts (128 x 64 each), 128 x 128 on 4 (64 x 64 each) or 64 x 64 on 2 (64 x 32 each).  The contraction travels in units of 128 bytes a row of X (256
 // 4-bit values, 128 8-bit ones), whole cache lines, each two matrix instructions deep (16 x 16 x 128, 32 x 32 x 64): two units
 // in LDS, one read while the other lands.  Fragments are read ahead, one memory instruction at a time between the matrix
 // instructions.  The one barrier of a unit stands where its last fragments have been read, two row groups before its last product:
@@ -477,7 +478,7 @@ template <int FA, int FB, int BM_, int BN_, int WM_, int WN_, int NBUF_> struct 
     static constexpr int UL = UG > NBUF ? UG : NBUF;        // units of one pass of the loop: whole groups, whole rounds of the places
     static constexpr int SD = BOTH4 ? 1 : 2;                // dwords of scales a lane needs of a group
     static_assert(UL % UG == 0 && UL % NBUF == 0 && NBUF >= 2, "places");
-    static_assert(TM >= 2 && TM % 2 == 0 && TN >= 2 && 8 * NW % 16 == 0 && 16 * NW % 32 == 0 && NSX * 16 * NW == BM && NSW * 16 * NW == BN && BYTES <= 160 * 1024, "shape");
+    static_assert(TM >= 2 && TM % 2 == 0 && TN >= 1 && 8 * NW % 16 == 0 && 16 * NW % 32 == 0 && NSX * 16 * NW == BM && NSW * 16 * NW == BN && BYTES <= 160 * 1024, "shape");
 };
 template <class T, class R> constexpr int ring_strips()
 {
@@ -674,17 +675,26 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void mx_ring_kernel(const PArgs g)
 }
 
 // ---------------------------------------------------------------------------
-// Few rows of X (up to 16 MT): the weight is read once, straight into registers, and that is the time.  A workgroup has 16 rows
-// of W; its wavefronts split the contraction and add up in LDS, in their order.  RAW: X arrives in its own type and
-// each wavefront puts the part that it needs into blocks itself.
+// Up to 16 rows of X: the weight is read once, straight into registers, and that is the time.  A workgroup has 16 rows of W; its
+// NWV wavefronts split the contraction and add up in LDS, in their order.  RAW: X arrives in its own type, and the workgroup
+// puts it into blocks in LDS (a lane 8 values, as the quantiser does: each wavefront for itself, in the layout of
+// the matrix instruction, 15 of 16 lanes would do one row's work again: 1 x 8192 x 8192 in 4 bits 23 us), while its
+// first part of the weight is on the way.
 // ---------------------------------------------------------------------------
-constexpr int FEW_WAVES = 8;
-
-template <int FA, int FB, int MT, bool WIDE, bool RAW, class T>
-__global__ __launch_bounds__(64 * FEW_WAVES) void mx_few_kernel(const PArgs g)
+constexpr int FEW_LDS = 64 * 1024;      // bytes of X in LDS at a time
+// values of a row that are put into blocks at a time
+inline int few_span(int M, int C, int fmt)
 {
-    constexpr int NT = 64 * FEW_WAVES, BA = step_bytes(FA), BB = step_bytes(FB);
-    __shared__ f32x4 part[FEW_WAVES][MT][64];
+    const int most = FEW_LDS / M * (fmt == E2 ? 2 : 1) / 512 * 512;
+    return std::min(most, (C + 511) / 512 * 512);
+}
+
+template <int FA, int FB, bool WIDE, bool RAW, int NWV, class T>
+__global__ __launch_bounds__(64 * NWV) void mx_few_kernel(const PArgs g)
+{
+    constexpr int NT = 64 * NWV, BA = step_bytes(FA), BB = step_bytes(FB);
+    extern __shared__ __align__(16) uint8_t xbuf[];         // RAW: [M][span in blocks + 16], then [M][span / 32] scales
+    __shared__ f32x4 part[NWV][64];
     __shared__ int sidx[16];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r16 = lane & 15, lg = lane >> 4;
     const int j0 = blockIdx.x * 16, cols_valid = min(16, g.J - j0);
@@ -709,18 +719,12 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void mx_few_kernel(const PArgs g)
         }
         return f;
     };
-    // the scale bytes of step s that this lane needs: of block lg, or (wide) of blocks lg / 2 and 2 + lg / 2
+    // the scales of step s that this lane needs: of block lg, or (wide) of blocks lg / 2 and 2 + lg / 2
     struct Sc { uint32_t a, b; };
     auto scales = [&](const uint8_t* p, int s) {
-        Sc c;
         const uint8_t* q = p + (s >> 2) * 16 + (s & 3);
-        c.a = q[(WIDE ? lg >> 1 : lg) * 4];
-        c.b = WIDE ? q[((lg >> 1) + 2) * 4] : 0;
-        return c;
+        return Sc{q[(WIDE ? lg >> 1 : lg) * 4], WIDE ? (uint32_t)q[((lg >> 1) + 2) * 4] : 0u};
     };
-    f32x4 acc[MT];
-#pragma unroll
-    for (int t = 0; t < MT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
     auto multiply = [&](const Frag& fa, Sc sa, const Frag& fb, Sc sb, f32x4 c) {
         if constexpr (!WIDE) return mma<FA, FB, 0>(fa, sa.a, fb, sb.a, c);
         else {
@@ -740,101 +744,97 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void mx_few_kernel(const PArgs g)
         }
     };
 
-    const int s_lo = g.steps * wave / FEW_WAVES, s_hi = g.steps * (wave + 1) / FEW_WAVES;
     constexpr int U = 4;
-    for (int s0 = s_lo; s0 < s_hi; s0 += U) {
+    const int m = min(r16, g.M - 1);
+    // steps at a time, for input in blocks too: the order of the sums does not tell whether X arrived in blocks
+    const int span = g.span / 128;
+    const int pitch = g.span / 128 * BA + 16;               // (16 rows of 16 bytes in 16 different places)
+    uint8_t* xsc = xbuf + g.M * pitch;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    for (int first = 0; first < g.steps; first += span) {
+        const int n = min(span, g.steps - first);
+        const int s_lo = first + n * wave / NWV, s_hi = first + n * (wave + 1) / NWV;
         Frag fb[U];
         Sc sb[U];
+        auto weights = [&](int s0) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int s = min(s0 + u, s_hi - 1);
-            fb[u] = frag(wq + (size_t)s * BB, std::integral_constant<int, FB>());
-            sb[u] = scales(ws, s);
-        }
-        if constexpr (!RAW) {
-#pragma unroll
-            for (int t = 0; t < MT; ++t) {
-                const size_t m = (size_t)min(t * 16 + r16, g.M - 1);
-                Frag fa[U];
-                Sc sa[U];
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    const int s = min(s0 + u, s_hi - 1);
-                    fa[u] = frag(g.xq + m * (size_t)g.ldxq + (size_t)s * BA, std::integral_constant<int, FA>());
-                    sa[u] = scales(g.xs + m * (size_t)g.ldxs, s);
-                }
-#pragma unroll
-                for (int u = 0; u < U; ++u)
-                    if (s0 + u < s_hi) acc[t] = multiply(fa[u], sa[u], fb[u], sb[u], acc[t]);
+            for (int u = 0; u < U; ++u) {
+                const int s = min(min(s0 + u, s_hi - 1), g.steps - 1);
+                fb[u] = frag(wq + (size_t)max(s, 0) * BB, std::integral_constant<int, FB>());
+                sb[u] = scales(ws, max(s, 0));
             }
-        } else {
-            static_assert(!RAW || MT == 1, "one group of rows is quantised here");
-            const T* x = (const T*)g.raw + (size_t)min(r16, g.M - 1) * (size_t)g.ldraw;
-            auto value = [&](int c) {
-                const int k = min(c, g.C - 1);
-                const T v = x[g.raw_cols ? clamp_idx(g.raw_cols[k], g.raw_extent) : k];
-                float f;
-                if constexpr (sizeof(T) == 2) f = bf16_bits_to_f32(v);
-                else f = v;
-                return c < g.C ? f : 0.f;
-            };
-            auto peak = [](const float (&v)[8], uint32_t m) {
+        };
+        weights(s_lo);
+        if constexpr (RAW) {
+            if (first) __syncthreads();                     // (the blocks before have been read)
+            const int octs = n * 16;                        // 8 values each, 4 of them a block: neighbouring lanes
+            for (int u = tid; u < g.M * octs; u += NT) {
+                const int r = u / octs, o = u - r * octs, c = first * 128 + o * 8;
+                const T* x = (const T*)g.raw + (size_t)r * (size_t)g.ldraw;
+                float f[8];
+                if (g.raw_vec && c + 8 <= g.C) {
+                    constexpr int PER = 16 / (int)sizeof(T);
+                    union { uint4 w[8 / PER]; T t[8]; } v;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
-                return m;
-            };
-            for (int u = 0; u < U && s0 + u < s_hi; ++u) {
-                // (8 elements each: in the order of the fragment's bytes)
-                constexpr bool SPLIT = FA == E4 || WIDE;
-                float v[4][8];
+                    for (int i = 0; i < 8 / PER; ++i) v.w[i] = *(const uint4*)(x + c + i * PER);
 #pragma unroll
-                for (int h = 0; h < 4; ++h) {
-                    const int c = (s0 + u) * 128 + (SPLIT ? (h >> 1) * 64 + lg * 16 + (h & 1) * 8 : lg * 32 + h * 8);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) v[h][i] = value(c + i);
-                }
-                Frag fa;
-                fa.hi = make_uint4(0u, 0u, 0u, 0u);
-                Sc sa;
-                if constexpr (SPLIT) {
-                    // halves of blocks lg / 2 and 2 + lg / 2: the other half is 16 lanes away
-                    uint32_t m0 = peak(v[1], peak(v[0], 0u)), m1 = peak(v[3], peak(v[2], 0u));
-                    m0 = max(m0, (uint32_t)__shfl_xor((int)m0, 16, 64));
-                    m1 = max(m1, (uint32_t)__shfl_xor((int)m1, 16, 64));
-                    const int c0 = mx_code<FA>(m0), c1 = mx_code<FA>(m1);
-                    const float i0 = c0 == 255 ? 0.f : mx_inv(c0), i1 = c1 == 255 ? 0.f : mx_inv(c1);
-                    const uint2 a = mx_encode8<FA>(v[0], i0), b = mx_encode8<FA>(v[1], i0), c = mx_encode8<FA>(v[2], i1), d = mx_encode8<FA>(v[3], i1);
-                    if constexpr (FA == E4) { fa.lo = make_uint4(a.x, a.y, b.x, b.y); fa.hi = make_uint4(c.x, c.y, d.x, d.y); }
-                    else fa.lo = make_uint4(a.x, b.x, c.x, d.x);
-                    if constexpr (WIDE) { sa.a = c0; sa.b = c1; }
-                    else {
-                        // block lg's code: lane groups 2 lg and on hold blocks 0, 1 first and 2, 3 second
-                        const int from = r16 + 32 * (lg & 1);
-                        const int lo = __shfl(c0, from, 64), hi = __shfl(c1, from, 64);
-                        sa.a = lg < 2 ? lo : hi;
-                        sa.b = 0;
+                    for (int i = 0; i < 8; ++i) {
+                        if constexpr (sizeof(T) == 2) f[i] = bf16_bits_to_f32(v.t[i]);
+                        else f[i] = v.t[i];
                     }
                 } else {
-                    const int c0 = mx_code<FA>(peak(v[3], peak(v[2], peak(v[1], peak(v[0], 0u)))));
-                    const float i0 = c0 == 255 ? 0.f : mx_inv(c0);
-                    fa.lo = make_uint4(mx_encode8<FA>(v[0], i0).x, mx_encode8<FA>(v[1], i0).x, mx_encode8<FA>(v[2], i0).x, mx_encode8<FA>(v[3], i0).x);
-                    sa.a = c0; sa.b = 0;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int k = min(c + i, g.C - 1);
+                        const T e = x[g.raw_cols ? clamp_idx(g.raw_cols[k], g.raw_extent) : k];
+                        if constexpr (sizeof(T) == 2) f[i] = bf16_bits_to_f32(e);
+                        else f[i] = e;
+                        f[i] = c + i < g.C ? f[i] : 0.f;
+                    }
                 }
-                acc[0] = u == 0 ? multiply(fa, sa, fb[0], sb[0], acc[0]) : u == 1 ? multiply(fa, sa, fb[1], sb[1], acc[0])
-                       : u == 2 ? multiply(fa, sa, fb[2], sb[2], acc[0]) : multiply(fa, sa, fb[3], sb[3], acc[0]);
+                uint32_t a = 0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) a = max(a, __float_as_uint(f[i]) & 0x7fffffffu);
+                a = max(a, (uint32_t)__shfl_xor((int)a, 1, 64));        // (16 octets a step: the four of a block are in or out together)
+                a = max(a, (uint32_t)__shfl_xor((int)a, 2, 64));
+                const int code = mx_code<FA>(a);
+                const uint2 e = mx_encode8<FA>(f, code == 255 ? 0.f : mx_inv(code));
+                if constexpr (FA == E2) *(uint32_t*)(xbuf + r * pitch + o * 4) = e.x;
+                else *(uint2*)(xbuf + r * pitch + o * 8) = e;
+                if ((o & 3) == 0) xsc[r * (g.span / 32) + o / 4] = (uint8_t)code;
             }
+            __syncthreads();
+        }
+        for (int s0 = s_lo; s0 < s_hi; s0 += U) {
+            if (s0 > s_lo) weights(s0);
+            Frag fa[U];
+            Sc sa[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int s = min(s0 + u, s_hi - 1);
+                if constexpr (RAW) {
+                    fa[u] = frag(xbuf + m * pitch + (s - first) * BA, std::integral_constant<int, FA>());
+                    const uint8_t* q = xsc + m * (g.span / 32) + (s - first) * 4;
+                    sa[u] = Sc{q[WIDE ? lg >> 1 : lg], WIDE ? (uint32_t)q[(lg >> 1) + 2] : 0u};
+                } else {
+                    fa[u] = frag(g.xq + (size_t)m * (size_t)g.ldxq + (size_t)s * BA, std::integral_constant<int, FA>());
+                    sa[u] = scales(g.xs + (size_t)m * (size_t)g.ldxs, s);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (s0 + u < s_hi) acc = multiply(fa[u], sa[u], fb[u], sb[u], acc);
         }
     }
-#pragma unroll
-    for (int t = 0; t < MT; ++t) part[wave][t][lane] = acc[t];
+    part[wave][lane] = acc;
     if (tid < 16) sidx[tid] = g.w_rows ? clamp_idx(g.w_rows[min(j0 + tid, g.J - 1)], g.N) : j0 + tid;
     __syncthreads();
-    // result (m, c): row 4 (lane >> 4) + i of group t, column lane & 15
+    // result (m, c): row 4 (lane >> 4) + i, column lane & 15
     auto result = [&](int m, int c) {
-        const int t = m >> 4, l = ((m & 15) >> 2) * 16 + c;
+        const int l = (m >> 2) * 16 + c;
         float v = 0.f;
 #pragma unroll
-        for (int w = 0; w < FEW_WAVES; ++w) v += ((const float*)&part[w][t][l])[m & 3];
+        for (int w = 0; w < NWV; ++w) v += ((const float*)&part[w][l])[m & 3];
         return to_out<T>(v);
     };
     T* Y = (T*)g.Y;
@@ -847,10 +847,10 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void mx_few_kernel(const PArgs g)
         return;
     }
     const int start = j0 == 0 ? 0 : sidx[0], end = j0 + 16 >= g.J ? g.N : clamp_idx(g.w_rows[j0 + 16], g.N);
-    const int span = end - start;
-    if (span <= 0) return;
-    for (int u = tid; u < span * g.M; u += NT) {
-        const int m = u / span, p = start + u % span;
+    const int width = end - start;
+    if (width <= 0) return;
+    for (int u = tid; u < width * g.M; u += NT) {
+        const int m = u / width, p = start + u % width;
         const int c = lower_bound_lds(sidx, cols_valid, p);
         const size_t off = (size_t)m * (size_t)g.ldy + p;
         Y[off] = c < cols_valid && sidx[c] == p ? result(m, c) : prev ? prev[off] : T(0);
@@ -872,6 +872,8 @@ PArgs pargs_of(const MxProduct& p)
     g.i_base = g.j_base = 0; g.i_end = p.M; g.j_end = p.J;
     g.tiles_i = g.tiles_j = 0;
     g.raw = p.raw; g.ldraw = p.ldraw; g.raw_cols = p.raw_cols; g.raw_extent = p.raw_extent; g.C = p.C;
+    g.span = p.M <= MX_FEW ? few_span(p.M, p.C, p.X.fmt) : 0;
+    g.raw_vec = !p.raw_cols && (uintptr_t)p.raw % 16 == 0 && p.ldraw * es % 16 == 0;
     return g;
 }
 
@@ -901,11 +903,11 @@ int launch_ring(PArgs g, hipStream_t stream)
 }
 
 // Which tiles: 256 x 256, one to a CU; 128 x 128, two to a CU with two units of LDS each or one with four (which hide the way
-// from memory: 2048 x 8192 x 2048 in 8 bits 54 and 35 us); 64 x 64.  Each kind's time in us by the number of its tiles and the contraction in
+// from memory: 2048 x 8192 x 2048 in 8 bits 54 and 35 us); 64 x 64 with four units on two wavefronts, or in steps on four.  Each kind's time in us by the number of its tiles and the contraction in
 // 1024s, fitted to 41 sizes (128 to 12288 rows, 2048 to 4096 columns, contractions of 512, 2048 and 8192) of which each gives most within
 // 10 %; and a panel of whole rounds of the largest tiles with a second launch for the rest, where that is shorter (8192 x 4096 x 2064 in
 // 8 bits: 95 us on 256 x 256 tiles alone, 288 of them, 69 with a panel of 256).
-enum Kind { T256, T128_2, T128_4, T64 };
+enum Kind { T256, T128_2, T128_4, T64_4, T64 };
 struct Plan { Kind kind, rest; int i_end, j_end; double us; };      // [0, i_end) x [0, j_end) on `kind`, the rest of Y on `rest`
 
 inline int64_t tiles_of(int I, int J, int b) { return (int64_t)((I + b - 1) / b) * ((J + b - 1) / b); }
@@ -913,7 +915,7 @@ inline int64_t tiles_of(int I, int J, int b) { return (int64_t)((I + b - 1) / b)
 template <int FA, int FB> double kind_us(Kind kind, int I, int J, int C)
 {
     constexpr int F = FA == E2 ? 0 : FB == E2 ? 1 : 2;
-    constexpr double S256[3] = {6.15, 10.4, 11.3}, S2[3] = {4.8, 7.7, 8.45}, S4[3] = {2.3, 3.1, 3.7}, S64[3] = {1.35, 1.6, 1.9};
+    constexpr double S256[3] = {6.15, 10.4, 11.3}, S2[3] = {4.8, 7.7, 8.45}, S4[3] = {2.3, 3.1, 3.7}, S64[3] = {1.35, 1.6, 1.9}, S64_4[3] = {1.04, 1.3, 1.42};
     const double K = C / 1024.0;
     // rounds of `per` tiles; the last one is the shorter the fewer tiles share the chip
     auto rounds = [](int64_t tiles, int per, double least) {
@@ -925,6 +927,8 @@ template <int FA, int FB> double kind_us(Kind kind, int I, int J, int C)
     if (kind == T128_2) return 4.0 + rounds(t, 512, 0.55) * (2.0 + S2[F] * K);
     if (kind == T128_4) return 1.0 + rounds(t, 256, 0.85) * (4.6 + S4[F] * K);
     const double q = tiles_of(I, J, 64) / 256.0;
+    // (64 x 5120 x 1728 in 4 bits 8.6 us with four units, 9.6 in steps; 1536 x 2048 x 2048 12.2 and 10.5)
+    if (kind == T64_4) return q > 2.0 ? 1e9 : 3.6 + std::max(1.0, q) * S64_4[F] * K;
     return 3.0 + 0.2 * q + std::max(1.0, q) * S64[F] * K;
 }
 
@@ -932,7 +936,7 @@ template <int FA, int FB> Plan plan(int I, int J, int C)
 {
     auto small = [&](int i, int j) {
         Plan s{T64, T64, i, j, kind_us<FA, FB>(T64, i, j, C)};
-        for (Kind k : {T128_2, T128_4}) {
+        for (Kind k : {T128_2, T128_4, T64_4}) {
             const double us = kind_us<FA, FB>(k, i, j, C);
             if (us < s.us) s = Plan{k, k, i, j, us};
         }
@@ -955,17 +959,27 @@ template <int FA, int FB> Plan plan(int I, int J, int C)
     return best;
 }
 
+template <int FA, int FB, bool WIDE, bool RAW, int NWV, class T>
+int launch_few(const PArgs& g, dim3 grid, hipStream_t stream)
+{
+    const int lds = RAW ? g.M * (g.span / 128 * step_bytes(FA) + 16 + g.span / 32) : 0;
+    static AttrFlags flags;
+    if (RAW && !ensure_max_dynamic_lds((const void*)mx_few_kernel<FA, FB, WIDE, RAW, NWV, T>, FEW_LDS + FEW_LDS / 16 + 16 * MX_FEW, &flags)) return ZR_ERR_HIP;
+    hipLaunchKernelGGL((mx_few_kernel<FA, FB, WIDE, RAW, NWV, T>), grid, dim3(64 * NWV), lds, stream, g);
+    return hip_status(hipGetLastError());
+}
+
 template <int FA, int FB, bool WIDE, class T>
 int launch_formats(const MxProduct& p, hipStream_t stream)
 {
     const PArgs g = pargs_of(p);
-    if (p.raw || p.M <= 64) {
-        const dim3 grid((p.J + 15) / 16), block(64 * FEW_WAVES);
-        if (p.raw) hipLaunchKernelGGL((mx_few_kernel<FA, FB, 1, WIDE, true, T>), grid, block, 0, stream, g);
-        else if (p.M <= 16) hipLaunchKernelGGL((mx_few_kernel<FA, FB, 1, WIDE, false, T>), grid, block, 0, stream, g);
-        else if (p.M <= 32) hipLaunchKernelGGL((mx_few_kernel<FA, FB, 2, WIDE, false, T>), grid, block, 0, stream, g);
-        else hipLaunchKernelGGL((mx_few_kernel<FA, FB, 4, WIDE, false, T>), grid, block, 0, stream, g);
-        return hip_status(hipGetLastError());
+    // (in blocks already 4096 x 2752 in 4 bits takes one row 6.4 us, 8 rows 8.0 and 16 rows 9.4; on 64 x 64 tiles 7.8.  All of them
+    // run here, so that a result is the same to the bit whether its input was kept in blocks or not.)
+    if (p.M <= MX_FEW) {
+        // 16 wavefronts where that leaves at most one workgroup to a CU, 8 for more
+        const dim3 grid((p.J + 15) / 16);
+        if (grid.x <= 256) return p.raw ? launch_few<FA, FB, WIDE, true, 16, T>(g, grid, stream) : launch_few<FA, FB, WIDE, false, 16, T>(g, grid, stream);
+        return p.raw ? launch_few<FA, FB, WIDE, true, 8, T>(g, grid, stream) : launch_few<FA, FB, WIDE, false, 8, T>(g, grid, stream);
     }
     if constexpr (WIDE) {
         // 160 tiles: 985 x 1001 x 771 7 us on 64 x 64, 12 on 128 x 128; 4096 x 2048 x 2048 57 and 44
@@ -980,6 +994,7 @@ int launch_formats(const MxProduct& p, hipStream_t stream)
                                256 * (uint64_t)p.X.ldq < (1ull << 32) && 256 * (uint64_t)p.X.lds < (1ull << 32);
             if (!reach || kind == T64) return launch_tiles<FA, FB, 64, 64, 2, 2, false, T>(h, stream);
             if (kind == T256) return launch_ring<FA, FB, 256, 256, 2, 4, 2, T>(h, stream);
+            if (kind == T64_4) return launch_ring<FA, FB, 64, 64, 1, 2, 4, T>(h, stream);
             if (kind == T128_2) return launch_ring<FA, FB, 128, 128, 2, 2, 2, T>(h, stream);
             return launch_ring<FA, FB, 128, 128, 2, 2, 4, T>(h, stream);
         };

@@ -338,59 +338,101 @@ def mx_empty(rows: int, n: int, fmt: int, device="cuda") -> MX:
               torch.empty((rows, mx_scale_bytes(n)), dtype=torch.uint8, device=device), n, fmt)
 
 
-def _mx(m: Optional[MX], rows: int, n: int, name: str):
+# The calls below are made once a layer and token while decoding, where the host's part of a call is longer than the GPU's:
+# attributes are looked up once, the current stream without an object for it.
+_raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else None
+_get_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else None
+_DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
+
+
+def _here() -> int:
+    """The current GPU, on which the kernels run."""
+    if not torch.cuda.is_initialized():
+        torch.cuda.init()
+    return _get_device()
+
+
+def _on(stream, here: int) -> int:
+    if stream is None:
+        return _raw_stream(here)
+    if stream.device.index != here:
+        raise ValueError("stream: of another GPU")
+    return stream.cuda_stream
+
+
+def _grid(t: Optional[torch.Tensor], here: int, name: str):
+    """(pointer, leading dimension) of a 2-D tensor on the current GPU."""
+    if t.get_device() != here:
+        raise ValueError(f"{name}: must be on the current GPU")
+    st = t.stride()
+    if len(st) != 2 or st[1] != 1:
+        raise ValueError(f"{name}: need a 2-D tensor with unit column stride")
+    return t.data_ptr(), st[0]
+
+
+def _list(keep_idx: Optional[torch.Tensor], here: int):
+    """(pointer, length) of a kept list, None: (None, 0)."""
+    if keep_idx is None:
+        return None, 0
+    if (keep_idx.dtype is not torch.int32 or keep_idx.dim() != 1 or not keep_idx.is_contiguous()
+            or keep_idx.get_device() != here):
+        raise ValueError("keep_idx: need a contiguous int32 vector on the current GPU")
+    return keep_idx.data_ptr(), keep_idx.numel()
+
+
+def _mx(m: Optional[MX], rows: int, n: int, here: int, name: str):
     """(elements, pitch, scales, pitch, format) of a matrix in blocks of the given size."""
     if m is None:
         return None, 0, None, 0, 0
-    if m.n != n or m.q.shape[0] != rows or m.scales.shape[0] != rows:
+    q, s, held, fmt = m
+    if held != n or q.shape[0] != rows or s.shape[0] != rows:
         raise ValueError(f"{name}: need {rows} rows of {n} values in blocks")
-    if m.q.dtype != torch.uint8 or m.scales.dtype != torch.uint8:
+    if q.dtype is not torch.uint8 or s.dtype is not torch.uint8:
         raise ValueError(f"{name}: elements and scales are uint8")
-    return (*_mat(m.q, name), *_mat(m.scales, name), m.fmt)
+    return (*_grid(q, here, name), *_grid(s, here, name), fmt)
 
 
-def _placed(stream, keep_idx, *tensors) -> None:
-    """The kernels run on the current device: all tensors have to be there, and the list has to be one that they can read."""
-    here = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t.get_device() != here:
-            raise ValueError("all tensors must be on the current GPU")
-    if stream is not None and stream.device.index != here:
-        raise ValueError("stream: of another GPU")
-    if keep_idx is not None and (keep_idx.dtype != torch.int32 or keep_idx.dim() != 1 or not keep_idx.is_contiguous()
-                                 or keep_idx.get_device() != here):
-        raise ValueError("keep_idx: need a contiguous int32 vector on the current GPU")
+def _code(dtype) -> int:
+    code = _DTYPES.get(dtype)
+    if code is None:
+        raise TypeError(f"unsupported dtype {dtype}")
+    return code
 
 
 def mx_quantize(src: torch.Tensor, fmt: int, axis: int = 1, keep_idx: Optional[torch.Tensor] = None,
                 out: Optional[MX] = None, stream=None) -> MX:
     """src [rows, cols] in blocks along `axis` (0: the transpose in blocks), of the kept indices of that axis alone."""
-    _placed(stream, keep_idx, src, *(() if out is None else (out.q, out.scales)))
-    sp, ld = _mat(src, "src")
+    here = _here()
+    sp, ld = _grid(src, here, "src")
     rows, cols = src.shape
-    n = (cols if axis == 1 else rows) if keep_idx is None else keep_idx.numel()
-    held = rows if axis == 1 else cols
+    held, n = (rows, cols) if axis == 1 else (cols, rows)
+    kp, nk = _list(keep_idx, here)
+    if kp is not None:
+        n = nk
     if out is None:
         out = mx_empty(held, n, fmt, src.device)
     if out.fmt != fmt:
         raise ValueError("out is of another format")
-    qp, ldq, scp, lds, _ = _mx(out, held, n, "out")
-    _check(_lib.zr_mx_quantize(sp, ld, rows, cols, axis, None if keep_idx is None else keep_idx.data_ptr(), n,
-                               _dtype_code(src), fmt, qp, ldq, scp, lds, _stream(stream)))
+    qp, ldq, scp, lds, _ = _mx(out, held, n, here, "out")
+    st = _lib.zr_mx_quantize(sp, ld, rows, cols, axis, kp, n, _code(src.dtype), fmt, qp, ldq, scp, lds, _on(stream, here))
+    if st:
+        raise ZrError(st)
     return out
 
 
 def mx_dequantize(m: MX, dtype=torch.bfloat16, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """The values [rows, n] that m stands for, in `dtype` (or in out's)."""
+    here = _here()
     rows = m.q.shape[0]
-    _placed(stream, None, m.q, m.scales, out)
     if out is None:
         out = torch.empty((rows, m.n), dtype=dtype, device=m.q.device)
-    if tuple(out.shape) != (rows, m.n):
+    if out.shape != (rows, m.n):
         raise ValueError("out must be [rows, n]")
-    op, ldo = _mat(out, "out")
-    qp, ldq, scp, lds, fmt = _mx(m, rows, m.n, "m")
-    _check(_lib.zr_mx_dequantize(qp, ldq, scp, lds, rows, m.n, fmt, op, ldo, _dtype_code(out), _stream(stream)))
+    op, ldo = _grid(out, here, "out")
+    qp, ldq, scp, lds, fmt = _mx(m, rows, m.n, here, "m")
+    st = _lib.zr_mx_dequantize(qp, ldq, scp, lds, rows, m.n, fmt, op, ldo, _code(out.dtype), _on(stream, here))
+    if st:
+        raise ZrError(st)
     return out
 
 
@@ -401,51 +443,50 @@ def mx_linear_fwd(X: Union[torch.Tensor, MX], W: MX, keep_idx: Optional[torch.Te
     """X [M, K] (put into blocks of x_fmt by the call, into x_mx where given: the checkpoint for resized_linear_bwd_mx;
     without x_mx at most 16 rows keep none, for more one is allocated), or X in blocks already (K: the layer's, for DROP_K; dtype: of Y).
     W in blocks: [N, n_keep] (DROP_K) or the whole shard [N, K] (DROP_N).  keep_idx None: nothing is pruned."""
+    here = _here()
     N = W.q.shape[0]
-    given = X if isinstance(X, MX) else x_mx
-    _placed(stream, keep_idx, W.q, W.scales, Y, prev_Y, *((X,) if given is not X else ()), *(() if given is None else (given.q, given.scales)))
-    if isinstance(X, MX):
+    kp, nk = _list(keep_idx, here)
+    if type(X) is MX:
         if x_mx is not None:
             raise ValueError("x_mx: X is in blocks already")
-        M, held = X.q.shape[0], X.n
-        K = held if K is None else K
-        x_mx, xp, ldx = X, None, 0
-        dev = X.q.device
-        dt = Y.dtype if Y is not None else dtype
+        x_mx, x_fmt, M = X, X.fmt, X.q.shape[0]
+        K = X.n if K is None else K
+        xp, ldx, dt = None, 0, dtype if Y is None else Y.dtype
+        c = nk if kp is not None and mode == DROP_K else K
     else:
+        xp, ldx = _grid(X, here, "X")
         M, K = X.shape
-        held = K if keep_idx is None or mode != DROP_K else keep_idx.numel()
-        if x_mx is None and M > 16:
-            x_mx = mx_empty(M, held, x_fmt, X.device)
-            if stream is not None:                      # (freed on return, perhaps before the stream gets there)
-                x_mx.q.record_stream(stream)
-                x_mx.scales.record_stream(stream)
-        xp, ldx = _mat(X, "X")
-        dev, dt = X.device, X.dtype
-    if x_mx is not None:
-        if not isinstance(X, MX) and x_mx.fmt != x_fmt:
+        dt = X.dtype
+        c = nk if kp is not None and mode == DROP_K else K
+        if x_mx is None:
+            if M > 16:
+                x_mx = mx_empty(M, c, x_fmt, X.device)
+                if stream is not None:                      # (freed on return, perhaps before the stream gets there)
+                    x_mx.q.record_stream(stream)
+                    x_mx.scales.record_stream(stream)
+        elif x_mx.fmt != x_fmt:
             raise ValueError("x_mx is of another format")
-        x_fmt = x_mx.fmt
     if Y is None:
-        Y = torch.empty((M, N), dtype=dt, device=dev)
-    if tuple(Y.shape) != (M, N) or Y.dtype != dt or (prev_Y is not None and prev_Y.dtype != dt):
-        raise ValueError("Y and prev_Y must be [M, N] of X's dtype")
-    yp, ldy = _mat(Y, "Y")
-    pp, ldp = _mat(prev_Y, "prev_Y")
-    if prev_Y is not None and ldp != ldy:
-        raise ValueError("prev_Y must share Y's leading dimension")
-    c = keep_idx.numel() if keep_idx is not None and mode == DROP_K else K
-    xq, ldxq, xs, ldxs, _ = _mx(x_mx, M, c, "X")
-    wq, ldwq, ws, ldws, w_fmt = _mx(W, N, c, "W")
-    _check(_lib.zr_mx_linear_fwd(xp, ldx, xq, ldxq, xs, ldxs, x_fmt, wq, ldwq, ws, ldws, w_fmt, yp, ldy, M, K, N,
-                                 None if keep_idx is None else keep_idx.data_ptr(),
-                                 0 if keep_idx is None else keep_idx.numel(), mode, _dtype_code(Y), policy, pp, _stream(stream)))
+        Y = torch.empty((M, N), dtype=dt, device=W.q.device)
+    elif Y.dtype is not dt or Y.shape != (M, N):
+        raise ValueError("Y must be [M, N] of X's dtype")
+    yp, ldy = _grid(Y, here, "Y")
+    pp = None
+    if prev_Y is not None:
+        pp, ldp = _grid(prev_Y, here, "prev_Y")
+        if ldp != ldy or prev_Y.dtype is not dt or prev_Y.shape != (M, N):
+            raise ValueError("prev_Y must be like Y, its leading dimension too")
+    xq, ldxq, xs, ldxs, _ = _mx(x_mx, M, c, here, "X")
+    wq, ldwq, ws, ldws, w_fmt = _mx(W, N, c, here, "W")
+    st = _lib.zr_mx_linear_fwd(xp, ldx, xq, ldxq, xs, ldxs, x_fmt, wq, ldwq, ws, ldws, w_fmt, yp, ldy, M, K, N, kp, nk,
+                               mode, _code(dt), policy, pp, _on(stream, here))
+    if st:
+        raise ZrError(st)
     return Y
 
 
 def mx_bwd_workspace_bytes(M: int, K: int, N: int, n_keep: int, mode: int, dtype) -> int:
-    code = dtype if isinstance(dtype, int) else (BF16 if dtype == torch.bfloat16 else F32)
-    return int(_lib.zr_mx_bwd_workspace_bytes(M, K, N, n_keep, mode, code))
+    return int(_lib.zr_mx_bwd_workspace_bytes(M, K, N, n_keep, mode, dtype if isinstance(dtype, int) else _code(dtype)))
 
 
 def resized_linear_bwd_mx(X: Optional[MX], W: torch.Tensor, dY: torch.Tensor, keep_idx: torch.Tensor, mode: int, policy: int = ZERO,
@@ -455,34 +496,48 @@ def resized_linear_bwd_mx(X: Optional[MX], W: torch.Tensor, dY: torch.Tensor, ke
                           w_layout: int = W_KN) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor]]:
     """resized_linear_bwd from the checkpoint of X: [M, n_keep] in blocks (DROP_K) or [M, K] (DROP_N).  workspace: of
     mx_bwd_workspace_bytes bytes, needed for dW (None: allocated)."""
+    here = _here()
     M, N = dY.shape
-    _placed(stream, keep_idx, W, dY, dX, dW, prev_dX, prev_dW, workspace, *((X.q, X.scales) if need_dW else ()))
-    K = W.shape[0] if w_layout == W_KN else W.shape[1]
-    wshape = (K, N) if w_layout == W_KN else (N, K)
-    if tuple(W.shape) != wshape or W.dtype != dY.dtype:
+    wshape = W.shape
+    K = wshape[0] if w_layout == W_KN else wshape[1]
+    dt = dY.dtype
+    if wshape != ((K, N) if w_layout == W_KN else (N, K)) or W.dtype is not dt:
         raise ValueError("dY must be [M, N] and W [K, N] (W_KN) or [N, K] (W_NK) of its dtype")
-    n_keep = keep_idx.numel()
-    if need_dX and dX is None:
-        dX = torch.empty((M, K), dtype=dY.dtype, device=dY.device)
-    if need_dW and dW is None:
-        dW = torch.empty(wshape, dtype=dY.dtype, device=dY.device)
-    if need_dW and workspace is None:
-        workspace = torch.empty(mx_bwd_workspace_bytes(M, K, N, n_keep, mode, dY.dtype), dtype=torch.uint8, device=dY.device)
+    kp, n_keep = _list(keep_idx, here)
+    wp, ldw = _grid(W, here, "W")
+    gp, ldg = _grid(dY, here, "dY")
+
+    def result(need, t, prev, shape, name):
+        """(tensor, pointer, leading dimension, previous one's pointer) of an output."""
+        if not need:
+            return None, None, 0, None
+        if t is None:
+            t = torch.empty(shape, dtype=dt, device=dY.device)
+        elif t.shape != shape or t.dtype is not dt:
+            raise ValueError(f"{name}: wrong shape or dtype")
+        p, ld = _grid(t, here, name)
+        pp = None
+        if prev is not None:
+            pp, ldp = _grid(prev, here, "prev_" + name)
+            if ldp != ld or prev.shape != shape or prev.dtype is not dt:
+                raise ValueError(f"prev_{name} must be like {name}, its leading dimension too")
+        return t, p, ld, pp
+
+    dX, dxp, lddx, pxp = result(need_dX, dX, prev_dX, (M, K), "dX")
+    dW, dwp, lddw, pwp = result(need_dW, dW, prev_dW, wshape, "dW")
+    xq, ldxq, xs, ldxs, fmt = _mx(X if need_dW else None, M, n_keep if mode == DROP_K else K, here, "X")
+    if workspace is None and need_dW:
+        workspace = torch.empty(mx_bwd_workspace_bytes(M, K, N, n_keep, mode, dt), dtype=torch.uint8, device=dY.device)
         if stream is not None:
             workspace.record_stream(stream)
-    for t, shape in ((dX if need_dX else None, (M, K)), (dW if need_dW else None, wshape), (prev_dX, (M, K)), (prev_dW, wshape)):
-        if t is not None and (tuple(t.shape) != shape or t.dtype != dY.dtype):
-            raise ValueError("dX, dW and the previous tensors have the shapes of X and W and dY's dtype")
-    (wp, ldw), (gp, ldg) = _mat(W, "W"), _mat(dY, "dY")
-    (dxp, lddx), (dwp, lddw) = _mat(dX if need_dX else None, "dX"), _mat(dW if need_dW else None, "dW")
-    (pxp, ldpx), (pwp, ldpw) = _mat(prev_dX, "prev_dX"), _mat(prev_dW, "prev_dW")
-    if (prev_dX is not None and need_dX and ldpx != lddx) or (prev_dW is not None and need_dW and ldpw != lddw):
-        raise ValueError("previous tensors must share the outputs' leading dimensions")
-    xq, ldxq, xs, ldxs, fmt = _mx(X if need_dW else None, M, n_keep if mode == DROP_K else K, "X")
-    _check(_lib.zr_resized_linear_bwd_mx(xq, ldxq, xs, ldxs, fmt, wp, ldw, gp, ldg, dxp, lddx, dwp, lddw, M, K, N,
-                                         keep_idx.data_ptr(), n_keep, mode, w_layout, _dtype_code(dY), policy, pxp, pwp,
-                                         *_ws(workspace), _stream(stream)))
-    return (dX if need_dX else None), (dW if need_dW else None)
+    if workspace is not None and workspace.get_device() != here:
+        raise ValueError("workspace: must be on the current GPU")
+    st = _lib.zr_resized_linear_bwd_mx(xq, ldxq, xs, ldxs, fmt, wp, ldw, gp, ldg, dxp, lddx, dwp, lddw, M, K, N,
+                                       kp, n_keep, mode, w_layout, _code(dt), policy, pxp, pwp,
+                                       *_ws(workspace), _on(stream, here))
+    if st:
+        raise ZrError(st)
+    return dX, dW
 
 
 def priority_scores(W_t: torch.Tensor, W_prev: torch.Tensor, mode: int,
