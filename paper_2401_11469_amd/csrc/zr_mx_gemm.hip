@@ -71,7 +71,7 @@ template <int N, int I = 0, class F> __device__ __forceinline__ void each(F&& f)
     }
 }
 
-// All products before here, in the compiler's eyes too: it would sink them past the next branch.
+// All products before here, in the compiler's eyes too (it would sink them past the next branch).
 template <int TM, int TN, class ACC> __device__ __forceinline__ void pin(ACC (&acc)[TM][TN])
 {
 #pragma unroll
@@ -140,90 +140,6 @@ template <int F> __device__ __forceinline__ bf16x8 widen8(uint2 r, float scale)
 // own order); 4-bit: 32 g .. + 31, but in wide products, where both operands have to agree, as for 8-bit.
 // The scale of block g goes with lane group g either way; a wide product needs those of blocks g / 2 and 2 + g / 2.
 
-// ---------------------------------------------------------------------------
-// Results of one strip of a tile, laid out in LDS, to Y: plain, or the kept columns at their places and the imputed
-// value in the others.  A scattering tile owns the original columns from its first kept one (0 for the first tile) up to
-// the next tile's first (all for the last).
-// ---------------------------------------------------------------------------
-constexpr int WIN = 1024;       // original columns per pass
-
-template <class T, int BN, int ROWS, int NT, class ROWOF>
-__device__ void store_strip(const PArgs& g, const T* Cs, int cp, uint16_t* tab, const int* sidx, int j0, int cols_valid,
-                            int start, int end, int tid, ROWOF row_of)
-{
-    constexpr int PER = 16 / (int)sizeof(T);
-    T* Y = (T*)g.Y;
-    const T* prev = (const T*)g.prev;
-    if (!g.w_rows) {
-        if (g.vec) {
-            for (int u = tid; u < ROWS * (BN / PER); u += NT) {
-                const int r = u / (BN / PER), c = u % (BN / PER) * PER, row = row_of(r);
-                if (row >= g.M || c >= cols_valid) continue;
-                T* o = Y + (size_t)row * (size_t)g.ldy + j0 + c;
-                if (c + PER <= cols_valid) *(uint4*)o = *(const uint4*)(Cs + r * cp + c);
-                else
-                    for (int e = 0; c + e < cols_valid; ++e) o[e] = Cs[r * cp + c + e];
-            }
-        } else {
-            for (int u = tid; u < ROWS * BN; u += NT) {
-                const int r = u / BN, c = u % BN, row = row_of(r);
-                if (row < g.M && c < cols_valid) Y[(size_t)row * (size_t)g.ldy + j0 + c] = Cs[r * cp + c];
-            }
-        }
-        return;
-    }
-    for (int base = start / PER * PER; base < end; base += WIN) {
-        const int span = min(WIN, end - base);
-        __syncthreads();
-        for (int u = tid; u < WIN; u += NT) tab[u] = 0xffffu;
-        __syncthreads();
-        for (int u = tid; u < cols_valid; u += NT) {
-            const int p = sidx[u] - base;
-            if (p >= 0 && p < WIN) tab[p] = (uint16_t)u;
-        }
-        __syncthreads();
-        if (g.vec) {
-            const int nch = (span + PER - 1) / PER;
-            for (int u = tid; u < ROWS * nch; u += NT) {
-                const int r = u / nch, c = u - r * nch, row = row_of(r), p = base + c * PER;
-                if (row >= g.M) continue;
-                const size_t off = (size_t)row * (size_t)g.ldy + p;
-                const bool whole = p >= start && p + PER <= end;
-                union { uint4 v; T e[PER]; } x;
-                x.v = make_uint4(0u, 0u, 0u, 0u);
-                if (prev) {
-                    if (whole) x.v = *(const uint4*)(prev + off);
-                    else {
-#pragma unroll
-                        for (int e = 0; e < PER; ++e)
-                            if (p + e >= start && p + e < end) x.e[e] = prev[off + e];
-                    }
-                }
-#pragma unroll
-                for (int e = 0; e < PER; ++e) {
-                    const int k = tab[c * PER + e];
-                    const T y = Cs[r * cp + (k & (BN - 1))];
-                    x.e[e] = k == 0xffff ? x.e[e] : y;
-                }
-                if (whole) *(uint4*)(Y + off) = x.v;
-                else {
-#pragma unroll
-                    for (int e = 0; e < PER; ++e)
-                        if (p + e >= start && p + e < end) Y[off + e] = x.e[e];
-                }
-            }
-        } else {
-            for (int u = tid; u < ROWS * span; u += NT) {
-                const int r = u / span, c = u - r * span, row = row_of(r), p = base + c;
-                if (row >= g.M || p < start) continue;
-                const size_t off = (size_t)row * (size_t)g.ldy + p;
-                const int k = tab[c];
-                Y[off] = k != 0xffff ? Cs[r * cp + k] : prev ? prev[off] : T(0);
-            }
-        }
-    }
-}
-
 // Workgroups go round-robin to the 8 XCDs (each with its own L2): each gets a contiguous range of tiles, in groups of 4
 // tile rows.  False: beyond the last tile (the grid is padded to a multiple of 8).
 __device__ __forceinline__ bool tile_of(const PArgs& g, int& ti, int& tj)
@@ -237,39 +153,142 @@ __device__ __forceinline__ bool tile_of(const PArgs& g, int& ti, int& tj)
     return true;
 }
 
-// All results of a tile to Y, strip by strip through LDS: SG 16-row (or 32-row) groups of every wavefront row at a time.
+// All results of a tile to Y, strip by strip through LDS: SG groups of MS rows of every wavefront row at a time.
 // acc[a][b][i] of MS x MS results: row 4 (lane / MS) + i % 4 + 8 (i / 4), column lane % MS.
-template <class T, int BM, int BN, int WM, int WN, int MS, int SG, int TM, int TN, class ACC>
+// A scattering tile owns the original columns from its first kept one (0 for the first tile) up to the next tile's first (all for
+// the last).  It lays them out by ORIGINAL column, 2 BN of them and SC groups of rows at a time: the imputed values, the
+// results on top, then copied out like a plain tile (8192 x 4096 x 2752 of 2064 kept, 4 bits: 61 us, 50 without the scatter; 83 with a
+// table of columns looked up for every element).
+template <class T, int BM, int BN, int WM, int WN, int MS, int SG, int SC, int TM, int TN, class ACC>
 __device__ void store_tile(const PArgs& g, uint8_t* smem, ACC (&acc)[TM][TN], int i0, int j0, int tid, int wave, int lane)
 {
-    constexpr int NT = 64 * WM * WN, ROWS = MS * WM * SG, CP = BN + 16 / (int)sizeof(T);
+    constexpr int NW = WM * WN, NT = 64 * NW, PER = 16 / (int)sizeof(T);
     T* Cs = (T*)smem;
-    uint16_t* tab = (uint16_t*)(smem + ROWS * CP * sizeof(T));
-    int* sidx = (int*)(tab + WIN);
+    T* Y = (T*)g.Y;
+    const T* prev = (const T*)g.prev;
     const int cols_valid = min(BN, g.j_end - j0);
-    int start = 0, end = 0;
-    if (g.w_rows) {
-        for (int u = tid; u < cols_valid; u += NT) sidx[u] = clamp_idx(g.w_rows[j0 + u], g.N);
-        start = j0 == 0 ? 0 : clamp_idx(g.w_rows[j0], g.N);
-        end = j0 + cols_valid >= g.J ? g.N : clamp_idx(g.w_rows[j0 + cols_valid], g.N);
-    }
+    // the results as they will be stored: bf16 in pairs of rows, half of the registers
+    constexpr int PN = MS * MS / 64 / (sizeof(T) == 2 ? 2 : 1);
+    std::conditional_t<sizeof(T) == 2, uint32_t, float> res[TM][TN][PN];
 #pragma unroll
-    for (int a0 = 0; a0 < TM; a0 += SG) {
-        if (a0) __syncthreads();
+    for (int a = 0; a < TM; ++a)
 #pragma unroll
-        for (int a = a0; a < a0 + SG; ++a)
+        for (int b = 0; b < TN; ++b)
 #pragma unroll
-            for (int b = 0; b < TN; ++b) {
-                T* c = Cs + (wave / WN * (MS * SG) + (a - a0) * MS + 4 * (lane / MS)) * CP + wave % WN * (TN * MS) + b * MS + lane % MS;
-#pragma unroll
-                for (int i = 0; i < MS * MS / 64; ++i) c[(i % 4 + 8 * (i / 4)) * CP] = to_out<T>(acc[a][b][i]);
+            for (int i = 0; i < PN; ++i) {
+                if constexpr (sizeof(T) == 2) res[a][b][i] = to_out<T>(acc[a][b][2 * i]) | (uint32_t)to_out<T>(acc[a][b][2 * i + 1]) << 16;
+                else res[a][b][i] = acc[a][b][i];
             }
-        __syncthreads();
-        store_strip<T, BN, ROWS, NT>(g, Cs, CP, tab, sidx, j0, cols_valid, start, end, tid, [&](int r) {
-            const int row = i0 + r / (MS * SG) * (TM * MS) + a0 * MS + r % (MS * SG);
-            return row < g.i_end ? row : g.M;
+    // results of groups a0 .. a0 + n - 1 into LDS, the lane's columns at place(b)
+    auto lay = [&](auto a0_, auto n_, int pitch, auto&& place) __attribute__((always_inline)) {
+        constexpr int a0 = decltype(a0_)::value, n = decltype(n_)::value;
+#pragma unroll
+        for (int b = 0; b < TN; ++b) {
+            const int p = place(b);
+#pragma unroll
+            for (int a = a0; a < a0 + n; ++a) {
+                T* c = Cs + (wave / WN * (MS * n) + (a - a0) * MS + 4 * (lane / MS)) * pitch + p;
+                if (p >= 0) {
+#pragma unroll
+                    for (int i = 0; i < PN; ++i) {
+                        if constexpr (sizeof(T) == 2) {
+                            c[(2 * i % 4 + 8 * (i / 2)) * pitch] = (T)res[a][b][i];
+                            c[((2 * i + 1) % 4 + 8 * (i / 2)) * pitch] = (T)(res[a][b][i] >> 16);
+                        } else c[(i % 4 + 8 * (i / 4)) * pitch] = res[a][b][i];
+                    }
+                }
+            }
+        }
+    };
+    // whole(LDS, offset in Y) of every whole chunk of columns [lo, hi) of Y in the strip's rows, 4 rows at a time, and single(..) of
+    // every other element: at most PER - 1 at either end, or (rows that are not aligned) all.  LDS column 0 is column `base` of Y, an aligned one.
+    auto copy = [&](auto a0_, auto n_, auto pitch_, int base, int lo, int hi, auto&& whole, auto&& single) __attribute__((always_inline)) {
+        constexpr int a0 = decltype(a0_)::value, n = decltype(n_)::value, ROWS = MS * WM * n, pitch = decltype(pitch_)::value;
+        constexpr int LPR = std::min(64, pitch / PER / 8 * 8), RPW = 64 / LPR;        // lanes to a row, rows to a wavefront
+        auto row_of = [&](int r) {
+            const int row = i0 + r / (MS * n) * (TM * MS) + a0 * MS + r % (MS * n);
+            return r < ROWS && row < g.i_end ? row : -1;
+        };
+        lo -= base;
+        hi -= base;
+        if (!g.vec) {
+            for (int r = wave; r < ROWS; r += NW) {
+                const int row = row_of(r);
+                if (row >= 0)
+                    for (int p = lo + lane; p < hi; p += 64) single(Cs + r * pitch + p, (size_t)row * (size_t)g.ldy + base + p);
+            }
+            return;
+        }
+        const int c_lo = (lo + PER - 1) / PER, c_hi = hi / PER;
+        for (int c = c_lo + lane % LPR; c < c_hi; c += LPR)
+            for (int r = wave * RPW + lane / LPR; r < ROWS; r += 4 * NW * RPW) {
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    const int q = r + v * NW * RPW, row = row_of(q);
+                    if (row >= 0) whole(Cs + q * pitch + c * PER, (size_t)row * (size_t)g.ldy + base + c * PER);
+                }
+            }
+        const int head = min(c_lo * PER, hi), tail = max(c_hi * PER, head), singles = head - lo + hi - tail;
+        if (singles > 0)
+            for (int u = tid; u < ROWS * singles; u += NT) {
+                const int r = u / singles, k = u - r * singles, row = row_of(r);
+                const int p = k < head - lo ? lo + k : tail + k - (head - lo);
+                if (row >= 0) single(Cs + r * pitch + p, (size_t)row * (size_t)g.ldy + base + p);
+            }
+    };
+    auto store16 = [&](T* c, size_t o) __attribute__((always_inline)) { *(uint4*)(Y + o) = *(const uint4*)c; };
+    auto store1 = [&](T* c, size_t o) __attribute__((always_inline)) { Y[o] = *c; };
+    if (!g.w_rows) {
+        each<TM / SG>([&](auto strip) __attribute__((always_inline)) {
+            constexpr std::integral_constant<int, decltype(strip)::value * SG> a0;
+            constexpr std::integral_constant<int, SG> n;
+            if (a0 > 0) __syncthreads();
+            lay(a0, n, BN + PER, [&](int b) __attribute__((always_inline)) { return wave % WN * (TN * MS) + b * MS + lane % MS; });
+            __syncthreads();
+            copy(a0, n, std::integral_constant<int, BN + PER>(), j0, j0, j0 + cols_valid, store16, store1);
+        });
+        return;
+    }
+    constexpr int CP = 2 * BN + PER;
+    const int start = j0 == 0 ? 0 : clamp_idx(g.w_rows[j0], g.N);
+    const int end = j0 + cols_valid >= g.J ? g.N : clamp_idx(g.w_rows[j0 + cols_valid], g.N);
+    int kept[TN];                           // the lane's columns
+#pragma unroll
+    for (int b = 0; b < TN; ++b) {
+        const int c = wave % WN * (TN * MS) + b * MS + lane % MS;
+        kept[b] = c < cols_valid ? clamp_idx(g.w_rows[j0 + c], g.N) : -1;
+    }
+    for (int base = start / PER * PER; base < end; base += 2 * BN) {
+        const int lo = max(start, base), hi = min(end, base + 2 * BN);
+        each<TM / SC>([&](auto strip) __attribute__((always_inline)) {
+            constexpr std::integral_constant<int, decltype(strip)::value * SC> a0;
+            constexpr std::integral_constant<int, SC> n;
+            constexpr int ROWS = MS * WM * SC;
+            __syncthreads();
+            if (prev)
+                copy(a0, n, std::integral_constant<int, CP>(), base, lo, hi, [&](T* c, size_t o) { *(uint4*)c = *(const uint4*)(prev + o); }, [&](T* c, size_t o) { *c = prev[o]; });
+            else
+                for (int c = lane; c * PER < hi - base; c += 64)
+                    for (int r = wave; r < ROWS; r += NW) *(uint4*)(Cs + r * CP + c * PER) = make_uint4(0u, 0u, 0u, 0u);
+            __syncthreads();
+            lay(a0, n, CP, [&](int b) __attribute__((always_inline)) { return kept[b] >= lo && kept[b] < hi ? kept[b] - base : -1; });
+            __syncthreads();
+            copy(a0, n, std::integral_constant<int, CP>(), base, lo, hi, store16, store1);
         });
     }
+}
+// rows of a strip: as many groups as `bytes` of LDS hold of rows of `cols`
+template <class T> constexpr int strip_groups(int TM, int rows, int cols, int bytes)
+{
+    int sg = TM;
+    while (sg > 1 && rows * sg * (cols + 16 / (int)sizeof(T)) * (int)sizeof(T) > bytes) sg /= 2;
+    return sg;
+}
+// LDS of a tile: what its contraction needs, or the strips of a plain store
+template <class T> constexpr int tile_bytes(int TM, int rows, int BN, int loop)
+{
+    const int ep = rows * strip_groups<T>(TM, rows, BN, 139 * 1024) * (BN + 16 / (int)sizeof(T)) * (int)sizeof(T);
+    return ep > loop ? ep : loop;
 }
 
 // ---------------------------------------------------------------------------
@@ -288,20 +307,6 @@ template <int FA, int FB, int BM, int BN, int WM, int WN> struct Shape {
     static constexpr int SINST = SCALES / 1024;             // instructions for the scales of four steps, one a wavefront at most
     static_assert(SINST <= NW && NW % SINST == 0, "scales");
 };
-// rows of a strip of the epilogue: as many 16-row groups of every wavefront row as leave room
-template <class T, int BM, int BN, int WM> constexpr int strip_groups()
-{
-    int sg = BM / WM / 16;
-    while (16 * WM * sg * (BN + 16 / (int)sizeof(T)) * (int)sizeof(T) > 139 * 1024) sg /= 2;
-    return sg;
-}
-template <class T, int FA, int FB, int BM, int BN, int WM, int WN> constexpr int tile_lds()
-{
-    const int ep = 16 * WM * strip_groups<T, BM, BN, WM>() * (BN + 16 / (int)sizeof(T)) * (int)sizeof(T) + WIN * 2 + BN * 4;
-    const int ring = Shape<FA, FB, BM, BN, WM, WN>::RING;
-    return ep > ring ? ep : ring;
-}
-
 template <int FA, int FB, int BM, int BN, int WM, int WN, bool WIDE, class T>
 __global__ __launch_bounds__(64 * WM * WN) void mx_kernel(const PArgs g)
 {
@@ -456,7 +461,8 @@ __global__ __launch_bounds__(64 * WM * WN) void mx_kernel(const PArgs g)
     }
     __syncthreads();
 
-    store_tile<T, BM, BN, WM, WN, 16, strip_groups<T, BM, BN, WM>(), TM, TN>(g, smem, acc, i0, j0, tid, wave, lane);
+    constexpr int SG = strip_groups<T>(TM, 16 * WM, BN, 139 * 1024), SC = strip_groups<T>(TM, 16 * WM, 2 * BN, tile_bytes<T>(TM, 16 * WM, BN, S::RING));
+    store_tile<T, BM, BN, WM, WN, 16, SG, SC, TM, TN>(g, smem, acc, i0, j0, tid, wave, lane);
 }
 
 // ---------------------------------------------------------------------------
@@ -480,18 +486,6 @@ template <int FA, int FB, int BM_, int BN_, int WM_, int WN_, int NBUF_> struct 
     static_assert(UL % UG == 0 && UL % NBUF == 0 && NBUF >= 2, "places");
     static_assert(TM >= 2 && TM % 2 == 0 && TN >= 1 && 8 * NW % 16 == 0 && 16 * NW % 32 == 0 && NSX * 16 * NW == BM && NSW * 16 * NW == BN && BYTES <= 160 * 1024, "shape");
 };
-template <class T, class R> constexpr int ring_strips()
-{
-    int sg = R::TM;
-    while (R::MS * R::WM * sg * (R::BN + 16 / (int)sizeof(T)) * (int)sizeof(T) > 139 * 1024) sg /= 2;
-    return sg;
-}
-template <class T, class R> constexpr int ring_lds()
-{
-    const int ep = R::MS * R::WM * ring_strips<T, R>() * (R::BN + 16 / (int)sizeof(T)) * (int)sizeof(T) + WIN * 2 + R::BN * 4;
-    return ep > R::BYTES ? ep : R::BYTES;
-}
-
 template <int FA, int FB, int BM, int BN, int WM, int WN, int NBUF, class T>
 __global__ __launch_bounds__(64 * WM * WN, 2) void mx_ring_kernel(const PArgs g)
 {
@@ -671,7 +665,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void mx_ring_kernel(const PArgs g)
     });
     wait_vm<0>();
     __syncthreads();
-    store_tile<T, BM, BN, WM, WN, MS, ring_strips<T, R>(), TM, TN>(g, smem, acc, i0, j0, tid, wave, lane);
+    constexpr int SG = strip_groups<T>(TM, MS * WM, BN, 139 * 1024), SC = strip_groups<T>(TM, MS * WM, 2 * BN, tile_bytes<T>(TM, MS * WM, BN, R::BYTES));
+    store_tile<T, BM, BN, WM, WN, MS, SG, SC, TM, TN>(g, smem, acc, i0, j0, tid, wave, lane);
 }
 
 // ---------------------------------------------------------------------------
@@ -880,7 +875,8 @@ PArgs pargs_of(const MxProduct& p)
 template <int FA, int FB, int BM, int BN, int WM, int WN, bool WIDE, class T>
 int launch_tiles(PArgs g, hipStream_t stream)
 {
-    constexpr int lds = tile_lds<T, FA, FB, BM, BN, WM, WN>();
+    typedef Shape<FA, FB, BM, BN, WM, WN> S;
+    constexpr int lds = tile_bytes<T>(S::TM, 16 * WM, BN, S::RING);
     static AttrFlags flags;
     if (!ensure_max_dynamic_lds((const void*)mx_kernel<FA, FB, BM, BN, WM, WN, WIDE, T>, lds, &flags)) return ZR_ERR_HIP;
     g.tiles_i = (g.i_end - g.i_base + BM - 1) / BM; g.tiles_j = (g.j_end - g.j_base + BN - 1) / BN;
@@ -893,7 +889,7 @@ template <int FA, int FB, int BM, int BN, int WM, int WN, int NBUF, class T>
 int launch_ring(PArgs g, hipStream_t stream)
 {
     typedef Ring<FA, FB, BM, BN, WM, WN, NBUF> R;
-    constexpr int lds = ring_lds<T, R>();
+    constexpr int lds = tile_bytes<T>(R::TM, R::MS * WM, BN, R::BYTES);
     static AttrFlags flags;
     if (!ensure_max_dynamic_lds((const void*)mx_ring_kernel<FA, FB, BM, BN, WM, WN, NBUF, T>, lds, &flags)) return ZR_ERR_HIP;
     g.tiles_i = (g.i_end - g.i_base + BM - 1) / BM; g.tiles_j = (g.j_end - g.j_base + BN - 1) / BN;
