@@ -546,8 +546,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void mx_ring_kernel(const PArgs g)
     const int wr = wave / WN * (TM * MS), wc = wave % WN * (TN * MS);
     const int rl = lane % MS, lg = lane / MS;
     // lane's chunk(s) of a fragment: lg of the step's half row, and lg + 2 of it in 8 bits
-    const uint32_t fa_at = (wr + rl) * 128 + ((lg ^ ((rl >> 1) & 7)) << 4);
-    const uint32_t fb_at = R::A_BYTES + (R::BB == 128 ? (wc + rl) * 128 + ((lg ^ ((rl >> 1) & 7)) << 4)
+    uint32_t fa_at = (wr + rl) * 128 + ((lg ^ ((rl >> 1) & 7)) << 4);
+    uint32_t fb_at = R::A_BYTES + (R::BB == 128 ? (wc + rl) * 128 + ((lg ^ ((rl >> 1) & 7)) << 4)
                                                       : (wc + rl) * 64 + ((lg ^ ((rl >> 1) & 3) ^ ((rl >> 4) & 1)) << 4));
     auto a_frag = [&](const uint8_t* un, int a, int h) __attribute__((always_inline)) {
         Frag f;
@@ -567,7 +567,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void mx_ring_kernel(const PArgs g)
     };
     // scales of a group: dword 2 h + lg (or lg) of a row
     uint32_t sa[TM][SD], sb[TN][SD];
-    const uint32_t sa_at = (wr + rl) * 64 + (((rl >> 2) & 3) << 4) + lg * 4, sb_at = (BM + wc + rl) * 64 + (((rl >> 2) & 3) << 4) + lg * 4;
+    uint32_t sa_at = (wr + rl) * 64 + (((rl >> 2) & 3) << 4) + lg * 4, sb_at = (BM + wc + rl) * 64 + (((rl >> 2) & 3) << 4) + lg * 4;
     auto a_scales = [&](int grp, int a) __attribute__((always_inline)) {
 #pragma unroll
         for (int h = 0; h < SD; ++h) sa[a][h] = *(const uint32_t*)(smem + NBUF * R::UNIT + (sa_at ^ ((grp & 3) << 4)) + a * (MS * 64) + h * 8);
@@ -611,6 +611,9 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void mx_ring_kernel(const PArgs g)
         const uint8_t* un = smem + I % NBUF * R::UNIT;
         const uint8_t* nx = H == 0 ? un : smem + (I + 1) % NBUF * R::UNIT;
         pin(acc);
+        // (addresses made from these are not kept from step to step: registers are what the largest tiles are short of, and a wait for one
+        // that was put into memory is a wait for every request before it)
+        asm volatile("" : "+v"(fa_at), "+v"(fb_at), "+v"(sa_at), "+v"(sb_at));
         // once in four groups the scales of the next four, into the place of these, which have been read
         if (V == UG - 1 && H == 0 && (u / UG & 3) == 3) {
 #pragma unroll
