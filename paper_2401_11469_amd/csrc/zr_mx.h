@@ -69,10 +69,10 @@ template <int FMT> __device__ __forceinline__ int mx_code(uint32_t abits)
     return abits >= 0x7f800000u ? 255 : c;
 }
 
-// 2^-(code - 127); 2^-127 is subnormal
+// 2^-(code - 127), for codes up to 254; 2^-127 is subnormal
 __device__ __forceinline__ float mx_inv(int code)
 {
-    return __uint_as_float(code >= 254 ? (code == 254 ? 0x00400000u : 0u) : (uint32_t)(254 - code) << 23);
+    return __uint_as_float(code >= 254 ? 0x00400000u : (uint32_t)(254 - code) << 23);
 }
 
 // 2^(code - 127); NaN for 255
@@ -81,13 +81,14 @@ __device__ __forceinline__ float mx_scale(int code)
     return __uint_as_float(code == 0 ? 0x00400000u : code == 255 ? 0x7fc00000u : (uint32_t)code << 23);
 }
 
-// Eight values times inv, on the format's grid: 8 bytes, or 4 in .x
-// (the conversions round to nearest even; nothing is beyond the largest value)
-template <int FMT> __device__ __forceinline__ uint2 mx_encode8(const float (&x)[8], float inv)
+// Eight values of a block with this code, on the format's grid: 8 bytes, or 4 in .x
+// (the conversions round to nearest even; nothing is beyond the largest value; zeros if the block is not finite)
+template <int FMT> __device__ __forceinline__ uint2 mx_encode8(const float (&x)[8], int code)
 {
+    const float inv = mx_inv(code);
     float y[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = inv == 0.f ? 0.f : x[i] * inv;       // (0: a block that is not finite)
+    for (int i = 0; i < 8; ++i) y[i] = x[i] * inv;
     uint2 r = make_uint2(0u, 0u);
     if constexpr (FMT == ZR_MX_E4M3) {
         r.x = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
@@ -106,7 +107,7 @@ template <int FMT> __device__ __forceinline__ uint2 mx_encode8(const float (&x)[
         r.x = (v[0] & 255) | (v[1] & 255) << 8 | (v[2] & 255) << 16 | (uint32_t)v[3] << 24;
         r.y = (v[4] & 255) | (v[5] & 255) << 8 | (v[6] & 255) << 16 | (uint32_t)v[7] << 24;
     }
-    return r;
+    return code == 255 ? make_uint2(0u, 0u) : r;
 }
 
 // The eight values that mx_encode8's bytes stand for

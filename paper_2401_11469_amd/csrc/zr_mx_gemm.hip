@@ -796,7 +796,7 @@ __global__ __launch_bounds__(64 * NWV) void mx_few_kernel(const PArgs g)
                 a = max(a, (uint32_t)__shfl_xor((int)a, 1, 64));        // (16 octets a step: the four of a block are in or out together)
                 a = max(a, (uint32_t)__shfl_xor((int)a, 2, 64));
                 const int code = mx_code<FA>(a);
-                const uint2 e = mx_encode8<FA>(f, code == 255 ? 0.f : mx_inv(code));
+                const uint2 e = mx_encode8<FA>(f, code);
                 if constexpr (FA == E2) *(uint32_t*)(xbuf + r * pitch + o * 4) = e.x;
                 else *(uint2*)(xbuf + r * pitch + o * 8) = e;
                 if ((o & 3) == 0) xsc[r * (g.span / 32) + o / 4] = (uint8_t)code;

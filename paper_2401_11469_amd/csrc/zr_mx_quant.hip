@@ -39,7 +39,7 @@ __device__ __forceinline__ void store_seg(const float (&x)[8], uint8_t* __restri
     const int c = mx_code<FMT>(a);
     const int at = seg * SEG + 8 * lane;
     if (at < (n + 127) / 128 * 128) {
-        const uint2 e = mx_encode8<FMT>(x, c == 255 ? 0.f : mx_inv(c));
+        const uint2 e = mx_encode8<FMT>(x, c);
         if constexpr (FMT == ZR_MX_E2M1) *(uint32_t*)(q + at / 2) = e.x;
         else *(uint2*)(q + at) = e;
     }
@@ -141,10 +141,12 @@ __global__ __launch_bounds__(256) void mx_gather_kernel(const T* __restrict__ sr
             for (int i = 0; i < 8; ++i) x[i] = as_float(d[(w[i >> 1] >> (16 * (i & 1))) & 0xffffu]);
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = as_float(d[min(at + i, n - 1)]);
+            for (int i = 0; i < 8; ++i) x[i] = as_float(d[at + 8 <= n ? at + i : min(at + i, n - 1)]);
         }
+        if (at + 8 > n) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = at + i < n ? x[i] : 0.f;
+            for (int i = 0; i < 8; ++i) x[i] = at + i < n ? x[i] : 0.f;
+        }
         store_seg<FMT>(x, q + row * (size_t)ldq, s + row * (size_t)lds, n, seg, lane);
     }
 }
@@ -238,10 +240,9 @@ __global__ __launch_bounds__(256) void mx_cols_kernel(const T* __restrict__ src,
             a = max(a, __float_as_uint(x[o][i]) & 0x7fffffffu);
         }
     const int code = mx_code<FMT>(a);
-    const float inv = code == 255 ? 0.f : mx_inv(code);
 #pragma unroll
     for (int o = 0; o < 4; ++o) {
-        const uint2 e = mx_encode8<FMT>(x[o], inv);
+        const uint2 e = mx_encode8<FMT>(x[o], code);
         if constexpr (FMT == ZR_MX_E2M1) *(uint32_t*)(outs + col * OP + blk * 16 + o * 4) = e.x;
         else *(uint2*)(outs + col * OP + blk * 32 + o * 8) = e;
     }
