@@ -132,6 +132,13 @@ template <int FMT> __device__ __forceinline__ void mx_decode8(uint2 r, float sca
     for (int i = 0; i < 8; ++i) x[i] *= scale;
 }
 
+// the largest of four neighbouring lanes' values
+__device__ __forceinline__ uint32_t mx_max4(uint32_t a)
+{
+    a = max(a, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)a, 0xb1, 0xf, 0xf, true));       // lanes 1 0 3 2
+    return max(a, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)a, 0x4e, 0xf, 0xf, true));    // lanes 2 3 0 1
+}
+
 // byte of block b's scale in its row
 __device__ __forceinline__ int mx_scale_at(int b) { return (b & ~15) + 4 * (b & 3) + ((b >> 2) & 3); }
 #endif

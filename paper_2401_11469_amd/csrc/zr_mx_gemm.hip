@@ -793,9 +793,7 @@ __global__ __launch_bounds__(64 * NWV) void mx_few_kernel(const PArgs g)
                 uint32_t a = 0;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) a = max(a, __float_as_uint(f[i]) & 0x7fffffffu);
-                a = max(a, (uint32_t)__shfl_xor((int)a, 1, 64));        // (16 octets a step: the four of a block are in or out together)
-                a = max(a, (uint32_t)__shfl_xor((int)a, 2, 64));
-                const int code = mx_code<FA>(a);
+                const int code = mx_code<FA>(mx_max4(a));               // (16 octets a step: the four of a block are in or out together)
                 const uint2 e = mx_encode8<FA>(f, code);
                 if constexpr (FA == E2) *(uint32_t*)(xbuf + r * pitch + o * 4) = e.x;
                 else *(uint2*)(xbuf + r * pitch + o * 8) = e;
@@ -981,8 +979,9 @@ int launch_formats(const MxProduct& p, hipStream_t stream)
         return p.raw ? launch_few<FA, FB, WIDE, true, 8, T>(g, grid, stream) : launch_few<FA, FB, WIDE, false, 8, T>(g, grid, stream);
     }
     if constexpr (WIDE) {
-        // 160 tiles: 985 x 1001 x 771 7 us on 64 x 64, 12 on 128 x 128; 4096 x 2048 x 2048 57 and 44
-        if (tiles_of(p.M, p.J, 128) >= 160) return launch_tiles<FA, FB, 128, 128, 2, 2, true, T>(g, stream);
+        // (56 tiles of 128 x 128, 985 x 751 x 771: 14.1 us, 7.1 on 64 x 64; 160, 1280 x 2048 x 2048: 22.5 and 20.5; 256, 2048 x 1024 x
+        // 2048: 15.4 and 16.3; 512, 4096 x 2048 x 2048: 44 and 48)
+        if (tiles_of(p.M, p.J, 128) >= 192) return launch_tiles<FA, FB, 128, 128, 2, 2, true, T>(g, stream);
         return launch_tiles<FA, FB, 64, 64, 2, 2, true, T>(g, stream);
     } else {
         const Plan best = plan<FA, FB>(p.M, p.J, p.C);

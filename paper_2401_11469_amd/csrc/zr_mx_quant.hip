@@ -34,9 +34,7 @@ __device__ __forceinline__ void store_seg(const float (&x)[8], uint8_t* __restri
     uint32_t a = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) a = max(a, __float_as_uint(x[i]) & 0x7fffffffu);
-    a = max(a, (uint32_t)__shfl_xor((int)a, 1, 64));
-    a = max(a, (uint32_t)__shfl_xor((int)a, 2, 64));
-    const int c = mx_code<FMT>(a);
+    const int c = mx_code<FMT>(mx_max4(a));
     const int at = seg * SEG + 8 * lane;
     if (at < (n + 127) / 128 * 128) {
         const uint2 e = mx_encode8<FMT>(x, c);
@@ -94,7 +92,6 @@ __global__ __launch_bounds__(256) void mx_gather_kernel(const T* __restrict__ sr
         const int e = tid < PER ? tid : tail + tid - PER;
         return tid < PER ? (e < head ? e : -1) : (tid < 2 * PER && e < cols ? e : -1);
     };
-    // (rows past the last one are that one again)
 #pragma unroll
     for (int r = 0; r < RB; ++r) {
         const T* row = src + (size_t)(r0 + min(r, nr - 1)) * (size_t)ld;
@@ -103,10 +100,11 @@ __global__ __launch_bounds__(256) void mx_gather_kernel(const T* __restrict__ sr
         for (int k = 0; k < KL; ++k) {
             const int e = (tid + 256 * k) * PER - off;
             v[r][k] = make_uint4(0u, 0u, 0u, 0u);
-            if (e >= 0 && e + PER <= cols) v[r][k] = *(const uint4*)(row + e);
+            if (r < nr && e >= 0 && e + PER <= cols) v[r][k] = *(const uint4*)(row + e);
         }
         const int e = edge_at(off);
-        edge[r] = row[max(e, 0)];
+        edge[r] = T(0);
+        if (r < nr && e >= 0) edge[r] = row[e];
     }
     if (keep)
         for (int i0 = 0; i0 < n; i0 += 1024) {
@@ -129,25 +127,34 @@ __global__ __launch_bounds__(256) void mx_gather_kernel(const T* __restrict__ sr
         if (r < nr && e1 >= 0) *(T*)(dst + (off + e1) * ES) = edge[r];
     }
     __syncthreads();
-    for (int it = wave; it < nr * segs; it += 4) {
-        const int r = it / segs, seg = it - r * segs, at = seg * SEG + 8 * lane;
+    // items (segment, row) in this order, a quarter to each wavefront: where a lane finds its 8 values is looked up once a segment
+    const int items = nr * segs, lo = items * wave / 4, hi = items * (wave + 1) / 4;
+    int seg = lo / nr, r = lo - seg * nr;
+    int pick[8];
+    for (int it = lo; it < hi; ++it) {
+        const int at = seg * SEG + 8 * lane;
+        if (it == lo || r == 0) {
+            if (keep) {
+                const uint4 p = *(const uint4*)(list + min(at, (n - 1) & ~7));
+                const uint32_t w[4] = {p.x, p.y, p.z, p.w};
+#pragma unroll
+                for (int i = 0; i < 8; ++i) pick[i] = (w[i >> 1] >> (16 * (i & 1))) & 0xffffu;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) pick[i] = min(at + i, n - 1);
+            }
+        }
         const size_t row = (size_t)(r0 + r);
         const T* d = (const T*)(stage + r * pitch) + offset(r);
         float x[8];
-        if (keep) {
-            const uint4 p = *(const uint4*)(list + min(at, (n - 1) & ~7));
-            const uint32_t w[4] = {p.x, p.y, p.z, p.w};
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = as_float(d[(w[i >> 1] >> (16 * (i & 1))) & 0xffffu]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = as_float(d[at + 8 <= n ? at + i : min(at + i, n - 1)]);
-        }
+        for (int i = 0; i < 8; ++i) x[i] = as_float(d[pick[i]]);
         if (at + 8 > n) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) x[i] = at + i < n ? x[i] : 0.f;
         }
         store_seg<FMT>(x, q + row * (size_t)ldq, s + row * (size_t)lds, n, seg, lane);
+        if (++r == nr) { r = 0; ++seg; }
     }
 }
 
@@ -350,7 +357,8 @@ int quantize_rows(const T* src, int64_t ld, int rows, int cols, const int32_t* k
 #define ZR_GATHER(KL, RB)                                                                                                                      \
         hipLaunchKernelGGL((mx_gather_kernel<T, FMT, KL, RB>), dim3((rows + rb - 1) / rb), dim3(256), (size_t)rb * pitch + list, stream, src, ld, rows, cols, \
                            keep, n, segs, rb, pitch, q, ldq, s, lds)
-        if (chunks <= 256) ZR_GATHER(1, 4); else if (chunks <= 512) ZR_GATHER(2, 4); else if (chunks <= 1024) ZR_GATHER(4, 4);
+        if (rb == 1 && chunks <= 512) ZR_GATHER(2, 1); else if (rb == 1 && chunks <= 1024) ZR_GATHER(4, 1);
+        else if (chunks <= 256) ZR_GATHER(1, 4); else if (chunks <= 512) ZR_GATHER(2, 4); else if (chunks <= 1024) ZR_GATHER(4, 4);
         else if (chunks <= 2048) ZR_GATHER(8, 2); else ZR_GATHER(16, 1);
 #undef ZR_GATHER
         return hip_status(hipGetLastError());
