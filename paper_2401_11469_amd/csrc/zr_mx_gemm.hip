@@ -157,7 +157,7 @@ __device__ __forceinline__ bool tile_of(const PArgs& g, int& ti, int& tj)
 // acc[a][b][i] of MS x MS results: row 4 (lane / MS) + i % 4 + 8 (i / 4), column lane % MS.
 // A scattering tile owns the original columns from its first kept one (0 for the first tile) up to the next tile's first (all for
 // the last).  It lays them out by ORIGINAL column, 2 BN of them and SC groups of rows at a time: the imputed values, the
-// results on top, then copied out like a plain tile (8192 x 4096 x 2752 of 2064 kept, 4 bits: 61 us, 50 without the scatter; 83 with a
+// results on top, then copied out like a plain tile (8192 x 4096 x 2752 of 2064 kept, 4 bits: 57 us, 49 without the scatter; 84 with a
 // table of columns looked up for every element).
 template <class T, int BM, int BN, int WM, int WN, int MS, int SG, int SC, int TM, int TN, class ACC>
 __device__ void store_tile(const PArgs& g, uint8_t* smem, ACC (&acc)[TM][TN], int i0, int j0, int tid, int wave, int lane)
@@ -292,8 +292,10 @@ template <class T> constexpr int tile_bytes(int TM, int rows, int BN, int loop)
 }
 
 // ---------------------------------------------------------------------------
-// Tiles of BM x BN on WM x WN wavefronts.  The contraction travels in steps of 128 through a ring of LDS stages, straight
-// from memory; the scales of four steps at a time, into two places of their own.
+// Tiles of BM x BN on WM x WN wavefronts: 64 x 64 for short contractions and small products (985 x 751 x 771 5 us, most of it the
+// launch, the first loads and the store), and the wide products (4096 x 2048 x 2048 44 us, 0.77 PFLOP/s, bound by the conversions
+// beside the bf16 instruction).  The contraction travels in steps of 128 through a ring of LDS stages, straight from memory;
+// the scales of four steps at a time, into two places of their own.
 // ---------------------------------------------------------------------------
 template <int FA, int FB, int BM, int BN, int WM, int WN> struct Shape {
     static constexpr int NW = WM * WN, NT = 64 * NW, TM = BM / WM / 16, TN = BN / WN / 16;
@@ -471,6 +473,13 @@ __global__ __launch_bounds__(64 * WM * WN) void mx_kernel(const PArgs g)
 // in LDS, one read while the other lands.  Fragments are read ahead, one memory instruction at a time between the matrix
 // instructions.  The one barrier of a unit stands where its last fragments have been read, two row groups before its last product:
 // behind it the first fragments of the next unit are read, and the unit after that may be requested.
+//
+// What it measured.  8192 x 8192 x 8192: 4 x 4 bits 242 us (4.5 PFLOP/s), 8 x 4 376 (2.9), 8 x 8 406 (2.7); the instructions alone, on
+// registers, hold 7.6 and 4.3 PFLOP/s at the clock that the chip then keeps (1.8 GHz of 2.4).  8192 x 4096 x 2048, one round of 256 tiles: 42,
+// 59 and 59 us.  What bounds it is the way of the operands: the requests alone take 0.33 us for what the instructions do in 0.48, the LDS
+// reads 0.2, and they hide each other in part (0.7 together).  Rows of 64 bytes a request, half a cache line, in four stages of a ring:
+// 72 us for 8 x 8 (70 % more time for the requests); scales fetched for one group of 512 at a time, 16 bytes of a line: 15 % of all requests.
+// Offsets from uniform addresses and not pointers: with pointers the loop spilled.
 // ---------------------------------------------------------------------------
 template <int FA, int FB, int BM_, int BN_, int WM_, int WN_, int NBUF_> struct Ring {
     static constexpr bool BOTH4 = FA == E2;
@@ -676,8 +685,9 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void mx_ring_kernel(const PArgs g)
 // Up to 16 rows of X: the weight is read once, straight into registers, and that is the time.  A workgroup has 16 rows of W; its
 // NWV wavefronts split the contraction and add up in LDS, in their order.  RAW: X arrives in its own type, and the workgroup
 // puts it into blocks in LDS (a lane 8 values, as the quantiser does: each wavefront for itself, in the layout of
-// the matrix instruction, 15 of 16 lanes would do one row's work again: 1 x 8192 x 8192 in 4 bits 23 us), while its
-// first part of the weight is on the way.
+// the matrix instruction, 15 of 16 lanes would do one row's work again: 1 x 8192 x 8192 in 4 bits 23 us, now 11.7), while its
+// first part of the weight is on the way.  1 x 4096 x 2752 6.2 us (5.6 MB of weight, 1.1 us at the copy's rate: an empty launch, the first load and
+// the sum over the wavefronts are the rest), 1 x 4096 x 11008 8.5.
 // ---------------------------------------------------------------------------
 constexpr int FEW_LDS = 64 * 1024;      // bytes of X in LDS at a time
 // values of a row that are put into blocks at a time
