@@ -360,6 +360,23 @@ def _on(stream, here: int) -> int:
     return stream.cuda_stream
 
 
+def _empty(shape, dtype, device, stream, returned: bool = True) -> torch.Tensor:
+    """Memory for a call on `stream`, of that stream's own: another's may still be read by work that was queued there before it was freed.
+    What the caller gets back is also kept from reuse until the current stream has done what it has queued when it is freed."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    if returned:
+        t.record_stream(torch.cuda.current_stream())
+    return t
+
+
+def _mx_empty(rows: int, n: int, fmt: int, device, stream, returned: bool = True) -> MX:
+    return MX(_empty((rows, mx_row_bytes(n, fmt)), torch.uint8, device, stream, returned),
+              _empty((rows, mx_scale_bytes(n)), torch.uint8, device, stream, returned), n, fmt)
+
+
 def _grid(t: Optional[torch.Tensor], here: int, name: str):
     """(pointer, leading dimension) of a 2-D tensor on the current GPU."""
     if t.get_device() != here:
@@ -377,6 +394,8 @@ def _list(keep_idx: Optional[torch.Tensor], here: int):
     if (keep_idx.dtype is not torch.int32 or keep_idx.dim() != 1 or not keep_idx.is_contiguous()
             or keep_idx.get_device() != here):
         raise ValueError("keep_idx: need a contiguous int32 vector on the current GPU")
+    if keep_idx.numel() == 0:       # (an empty tensor's pointer is null, which would mean that nothing is pruned)
+        raise ZrError(3)
     return keep_idx.data_ptr(), keep_idx.numel()
 
 
@@ -389,6 +408,8 @@ def _mx(m: Optional[MX], rows: int, n: int, here: int, name: str):
         raise ValueError(f"{name}: need {rows} rows of {n} values in blocks")
     if q.dtype is not torch.uint8 or s.dtype is not torch.uint8:
         raise ValueError(f"{name}: elements and scales are uint8")
+    if q.shape[1] << (fmt == MX_E2M1) < (n + 127) // 128 * 128 or s.shape[1] < (n + 511) // 512 * 16:
+        raise ValueError(f"{name}: its rows do not hold {n} values")
     return (*_grid(q, here, name), *_grid(s, here, name), fmt)
 
 
@@ -403,6 +424,7 @@ def mx_quantize(src: torch.Tensor, fmt: int, axis: int = 1, keep_idx: Optional[t
                 out: Optional[MX] = None, stream=None) -> MX:
     """src [rows, cols] in blocks along `axis` (0: the transpose in blocks), of the kept indices of that axis alone."""
     here = _here()
+    on = _on(stream, here)
     sp, ld = _grid(src, here, "src")
     rows, cols = src.shape
     held, n = (rows, cols) if axis == 1 else (cols, rows)
@@ -410,11 +432,11 @@ def mx_quantize(src: torch.Tensor, fmt: int, axis: int = 1, keep_idx: Optional[t
     if kp is not None:
         n = nk
     if out is None:
-        out = mx_empty(held, n, fmt, src.device)
+        out = _mx_empty(held, n, fmt, src.device, stream)
     if out.fmt != fmt:
         raise ValueError("out is of another format")
     qp, ldq, scp, lds, _ = _mx(out, held, n, here, "out")
-    st = _lib.zr_mx_quantize(sp, ld, rows, cols, axis, kp, n, _code(src.dtype), fmt, qp, ldq, scp, lds, _on(stream, here))
+    st = _lib.zr_mx_quantize(sp, ld, rows, cols, axis, kp, n, _code(src.dtype), fmt, qp, ldq, scp, lds, on)
     if st:
         raise ZrError(st)
     return out
@@ -423,14 +445,15 @@ def mx_quantize(src: torch.Tensor, fmt: int, axis: int = 1, keep_idx: Optional[t
 def mx_dequantize(m: MX, dtype=torch.bfloat16, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """The values [rows, n] that m stands for, in `dtype` (or in out's)."""
     here = _here()
+    on = _on(stream, here)
     rows = m.q.shape[0]
     if out is None:
-        out = torch.empty((rows, m.n), dtype=dtype, device=m.q.device)
+        out = _empty((rows, m.n), dtype, m.q.device, stream)
     if out.shape != (rows, m.n):
         raise ValueError("out must be [rows, n]")
     op, ldo = _grid(out, here, "out")
     qp, ldq, scp, lds, fmt = _mx(m, rows, m.n, here, "m")
-    st = _lib.zr_mx_dequantize(qp, ldq, scp, lds, rows, m.n, fmt, op, ldo, _code(out.dtype), _on(stream, here))
+    st = _lib.zr_mx_dequantize(qp, ldq, scp, lds, rows, m.n, fmt, op, ldo, _code(out.dtype), on)
     if st:
         raise ZrError(st)
     return out
@@ -444,6 +467,7 @@ def mx_linear_fwd(X: Union[torch.Tensor, MX], W: MX, keep_idx: Optional[torch.Te
     without x_mx at most 16 rows keep none, for more one is allocated), or X in blocks already (K: the layer's, for DROP_K; dtype: of Y).
     W in blocks: [N, n_keep] (DROP_K) or the whole shard [N, K] (DROP_N).  keep_idx None: nothing is pruned."""
     here = _here()
+    on = _on(stream, here)
     N = W.q.shape[0]
     kp, nk = _list(keep_idx, here)
     if type(X) is MX:
@@ -460,14 +484,11 @@ def mx_linear_fwd(X: Union[torch.Tensor, MX], W: MX, keep_idx: Optional[torch.Te
         c = nk if kp is not None and mode == DROP_K else K
         if x_mx is None:
             if M > 16:
-                x_mx = mx_empty(M, c, x_fmt, X.device)
-                if stream is not None:                      # (freed on return, perhaps before the stream gets there)
-                    x_mx.q.record_stream(stream)
-                    x_mx.scales.record_stream(stream)
+                x_mx = _mx_empty(M, c, x_fmt, X.device, stream, returned=False)
         elif x_mx.fmt != x_fmt:
             raise ValueError("x_mx is of another format")
     if Y is None:
-        Y = torch.empty((M, N), dtype=dt, device=W.q.device)
+        Y = _empty((M, N), dt, W.q.device, stream)
     elif Y.dtype is not dt or Y.shape != (M, N):
         raise ValueError("Y must be [M, N] of X's dtype")
     yp, ldy = _grid(Y, here, "Y")
@@ -479,7 +500,7 @@ def mx_linear_fwd(X: Union[torch.Tensor, MX], W: MX, keep_idx: Optional[torch.Te
     xq, ldxq, xs, ldxs, _ = _mx(x_mx, M, c, here, "X")
     wq, ldwq, ws, ldws, w_fmt = _mx(W, N, c, here, "W")
     st = _lib.zr_mx_linear_fwd(xp, ldx, xq, ldxq, xs, ldxs, x_fmt, wq, ldwq, ws, ldws, w_fmt, yp, ldy, M, K, N, kp, nk,
-                               mode, _code(dt), policy, pp, _on(stream, here))
+                               mode, _code(dt), policy, pp, on)
     if st:
         raise ZrError(st)
     return Y
@@ -497,6 +518,7 @@ def resized_linear_bwd_mx(X: Optional[MX], W: torch.Tensor, dY: torch.Tensor, ke
     """resized_linear_bwd from the checkpoint of X: [M, n_keep] in blocks (DROP_K) or [M, K] (DROP_N).  workspace: of
     mx_bwd_workspace_bytes bytes, needed for dW (None: allocated)."""
     here = _here()
+    on = _on(stream, here)
     M, N = dY.shape
     wshape = W.shape
     K = wshape[0] if w_layout == W_KN else wshape[1]
@@ -512,7 +534,7 @@ def resized_linear_bwd_mx(X: Optional[MX], W: torch.Tensor, dY: torch.Tensor, ke
         if not need:
             return None, None, 0, None
         if t is None:
-            t = torch.empty(shape, dtype=dt, device=dY.device)
+            t = _empty(shape, dt, dY.device, stream)
         elif t.shape != shape or t.dtype is not dt:
             raise ValueError(f"{name}: wrong shape or dtype")
         p, ld = _grid(t, here, name)
@@ -527,14 +549,12 @@ def resized_linear_bwd_mx(X: Optional[MX], W: torch.Tensor, dY: torch.Tensor, ke
     dW, dwp, lddw, pwp = result(need_dW, dW, prev_dW, wshape, "dW")
     xq, ldxq, xs, ldxs, fmt = _mx(X if need_dW else None, M, n_keep if mode == DROP_K else K, here, "X")
     if workspace is None and need_dW:
-        workspace = torch.empty(mx_bwd_workspace_bytes(M, K, N, n_keep, mode, dt), dtype=torch.uint8, device=dY.device)
-        if stream is not None:
-            workspace.record_stream(stream)
+        workspace = _empty(mx_bwd_workspace_bytes(M, K, N, n_keep, mode, dt), torch.uint8, dY.device, stream, returned=False)
     if workspace is not None and workspace.get_device() != here:
         raise ValueError("workspace: must be on the current GPU")
     st = _lib.zr_resized_linear_bwd_mx(xq, ldxq, xs, ldxs, fmt, wp, ldw, gp, ldg, dxp, lddx, dwp, lddw, M, K, N,
                                        kp, n_keep, mode, w_layout, _code(dt), policy, pxp, pwp,
-                                       *_ws(workspace), _on(stream, here))
+                                       *_ws(workspace), on)
     if st:
         raise ZrError(st)
     return dX, dW

@@ -574,3 +574,37 @@ def test_binding_refusals(torch, zr):
     for f in bad:
         with pytest.raises((ValueError, TypeError, zr.ZrError)):
             f()
+
+
+def test_empty_list_prunes_everything_and_is_refused(torch, zr):
+    x = torch.zeros(20, 64, dtype=torch.bfloat16, device="cuda")
+    w = zr.mx_quantize(x[:8], E2M1)
+    for none in (torch.empty(0, dtype=torch.int32, device="cuda"), torch.arange(5, dtype=torch.int32, device="cuda")[:0]):
+        for f in (lambda: zr.mx_quantize(x, E4M3, keep_idx=none), lambda: zr.mx_linear_fwd(x, w, none, DROP_N),
+                  lambda: zr.mx_linear_fwd(x, w, none, DROP_K), lambda: zr.mx_linear_fwd(x[:1], w, none, DROP_N),
+                  lambda: zr.resized_linear_bwd_mx(zr.mx_quantize(x, E4M3), x.new_zeros(64, 16), x[:, :16], none, DROP_N)):
+            with pytest.raises(zr.ZrError):
+                f()
+
+
+def test_memory_of_a_call_on_another_stream_is_that_streams(torch, zr):
+    """Blocks that the current stream has given back may still be read by what it has queued: no call on another stream gets one."""
+    M, K, N = 4096, 4096, 2048                              # (every buffer above 1 MB: blocks of the allocator's own for each stream)
+    X = torch.zeros(M, K, dtype=torch.bfloat16, device="cuda")
+    W = torch.zeros(K, N, dtype=torch.bfloat16, device="cuda")
+    dY = torch.zeros(M, N, dtype=torch.bfloat16, device="cuda")
+    keep = torch.arange(2880, dtype=torch.int32, device="cuda")
+    wm = zr.mx_quantize(W, E4M3, axis=0, keep_idx=keep)
+    ck = zr.mx_quantize(X, E4M3, keep_idx=keep)
+    st = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    sizes = (M * 2944, M * N * 2, M * K * 2, K * N * 2, M * 2944 * 2)
+    freed = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in sizes]
+    ranges = [(t.data_ptr(), t.data_ptr() + t.numel()) for t in freed]
+    del freed
+    out = [zr.mx_quantize(X, E4M3, keep_idx=keep, stream=st).q, zr.mx_dequantize(ck, stream=st),
+           zr.mx_linear_fwd(X, wm, keep, DROP_K, stream=st), *zr.resized_linear_bwd_mx(ck, W, dY, keep, DROP_K, stream=st)]
+    for t in out:
+        assert not any(lo <= t.data_ptr() < hi for lo, hi in ranges)
+    torch.cuda.synchronize()

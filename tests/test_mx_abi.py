@@ -125,3 +125,20 @@ def test_binding_refuses_tensors_elsewhere():
     for f in (lambda: zr.mx_quantize(x, zr.MX_E4M3), lambda: zr.mx_dequantize(m), lambda: zr.mx_linear_fwd(x, m)):
         with pytest.raises((ValueError, RuntimeError, AssertionError)):
             f()
+
+
+def test_binding_refuses_empty_lists_and_narrow_storage():
+    """What the binding looks at before any pointer is used (a device index of -1 is the CPU's)."""
+    import torch
+    from paper_2401_11469_amd import zr
+    with pytest.raises(zr.ZrError):
+        zr._list(torch.empty(0, dtype=torch.int32), -1)
+    assert zr._list(None, -1) == (None, 0) and zr._list(torch.zeros(3, dtype=torch.int32), -1)[1] == 3
+    wide = torch.empty(4, 4096, dtype=torch.uint8)
+    for fmt, row in ((zr.MX_E4M3, 384), (zr.MX_INT8, 384), (zr.MX_E2M1, 192)):
+        good = zr.MX(wide[:, :row], wide[:, :16], 300, fmt)
+        assert zr._mx(good, 4, 300, -1, "m")[1::2] == (4096, 4096)
+        for bad in (good._replace(q=wide[:, :row - 1]), good._replace(scales=wide[:, :15]), good._replace(n=385),
+                    zr.MX(wide, wide[:, :16], 513, fmt)):
+            with pytest.raises(ValueError):
+                zr._mx(bad, 4, bad.n, -1, "m")
