@@ -468,8 +468,8 @@ __global__ __launch_bounds__(64 * WM * WN) void mx_kernel(const PArgs g)
 }
 
 // ---------------------------------------------------------------------------
-// Tiles of 256 x 256 on 8 wavefronts (128 x 64 each), 128 x 128 on 4 (64 x 64 each) or 64 x 64 on 2 (64 x 32 each).  The contraction travels in units of 128 bytes a row of X (256
-// 4-bit values, 128 8-bit ones), whole cache lines, each two matrix instructions deep (16 x 16 x 128, 32 x 32 x 64): two units
+// Tiles of 256 x 256 on 8 wavefronts (128 x 64 each), 128 x 128 on 4 (64 x 64 each) or 64 x 64 on 2 (64 x 32 each).  The
+// contraction travels in units of 128 bytes a row of X (256 4-bit values, 128 8-bit ones), whole cache lines, each two matrix instructions deep (16 x 16 x 128, 32 x 32 x 64): two units
 // in LDS, one read while the other lands.  Fragments are read ahead, one memory instruction at a time between the matrix
 // instructions.  The one barrier of a unit stands where its last fragments have been read, two row groups before its last product:
 // behind it the first fragments of the next unit are read, and the unit after that may be requested.
