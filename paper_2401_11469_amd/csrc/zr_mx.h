@@ -139,6 +139,45 @@ __device__ __forceinline__ uint32_t mx_max4(uint32_t a)
     return max(a, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)a, 0x4e, 0xf, 0xf, true));    // lanes 2 3 0 1
 }
 
+// What a lane reads that puts elements at .. at + PER - 1 of a row of `width` back into values (width: n, or up to the whole groups of
+// 128 that the row's storage holds).  Every read lies in the row's storage, whatever `at` is: chunks that begin before the row read
+// from its first element, chunks that lie behind it (the idle lanes of a row's last wavefront) from inside its last group.
+// VEC: `at` is a multiple of PER.
+struct MxRead {
+    int e;          // the first element that is in the row
+    int b;          // the byte from which PER elements' worth are read
+    int more;       // (elements from odd places, 4 bits) a byte more, from here
+};
+template <int FMT, int PER, bool VEC> __host__ __device__ __forceinline__ MxRead mx_read_at(int at, int n, int width)
+{
+    const int held = (n + 127) / 128 * 128, last = VEC ? held - PER : width - 1;
+    const int e = at < 0 ? 0 : at < last ? at : last;
+    if constexpr (FMT == ZR_MX_E2M1) {
+        const int top = (held - PER) / 2, b = e / 2 < top ? e / 2 : top, next = held / 2 - 1 - b;
+        return MxRead{e, b, b + (PER / 2 < next ? PER / 2 : next)};
+    }
+    return MxRead{e, e < held - PER ? e : held - PER, 0};
+}
+// their bits from `row`, element e's first
+template <int FMT, int PER, bool VEC> __host__ __device__ __forceinline__ uint2 mx_read(const uint8_t* row, MxRead a)
+{
+    const uint8_t* p = row + a.b;
+    if constexpr (FMT == ZR_MX_E2M1) {
+        uint32_t w;
+        if constexpr (PER == 8) __builtin_memcpy(&w, p, 4);
+        else { uint16_t h; __builtin_memcpy(&h, p, 2); w = h; }
+        if constexpr (!VEC) w = (uint32_t)((w | (uint64_t)row[a.more] << (4 * PER)) >> (4 * (a.e - 2 * a.b)));     // an odd place: half a byte more
+        return uint2{w, 0u};
+    } else {
+        uint64_t w = 0;
+        __builtin_memcpy(&w, p, PER);
+        if constexpr (!VEC) w >>= 8 * (a.e - a.b);
+        return uint2{(uint32_t)w, (uint32_t)(w >> 32)};
+    }
+}
+// wavefronts of 64 chunks to a row; rows that are not aligned may begin inside a chunk and so take one more
+__host__ __device__ inline int mx_value_segs(int width, int per, bool vec) { return ((width + per - 1) / per + (vec ? 0 : 1) + 63) / 64; }
+
 // byte of block b's scale in its row
 __device__ __forceinline__ int mx_scale_at(int b) { return (b & ~15) + 4 * (b & 3) + ((b >> 2) & 3); }
 #endif

@@ -301,25 +301,9 @@ __global__ __launch_bounds__(256) void mx_values_kernel(const uint8_t* __restric
         const size_t row = (size_t)min(r0 + r, rows - 1);
         const int off = VEC ? 0 : (int)((uintptr_t)(out + row * (size_t)ldo) & 15) / (int)sizeof(T);
         at[r] = chunk * PER - off;
-        // (from the row's first value where the chunk begins before it; never past the storage, whole groups of 128)
-        const int e = min(max(at[r], 0), width - 1), held = (n + 127) / 128 * 128;
-        if constexpr (FMT == ZR_MX_E2M1) {
-            const int b = VEC ? e >> 1 : min(e >> 1, (held - PER) / 2);
-            const uint8_t* p = q + row * (size_t)ldq + b;
-            uint32_t w;
-            if constexpr (PER == 8) __builtin_memcpy(&w, p, 4);
-            else { uint16_t h; __builtin_memcpy(&h, p, 2); w = h; }
-            if constexpr (!VEC)             // an odd place: half a byte more
-                w = (uint32_t)((w | (uint64_t)p[min(PER / 2, held / 2 - 1 - b)] << (4 * PER)) >> (4 * (e - 2 * b)));
-            raw[r].x = w;
-        } else {
-            const int b = VEC ? e : min(e, held - PER);
-            const uint8_t* p = q + row * (size_t)ldq + b;
-            uint64_t w = 0;
-            __builtin_memcpy(&w, p, PER);
-            if constexpr (!VEC) w >>= 8 * (e - b);
-            raw[r] = make_uint2((uint32_t)w, (uint32_t)(w >> 32));
-        }
+        const MxRead a = mx_read_at<FMT, PER, VEC>(at[r], n, width);
+        const int e = a.e;
+        raw[r] = mx_read<FMT, PER, VEC>(q + row * (size_t)ldq, a);
         const uint8_t* sr = s + row * (size_t)lds;
         c0[r] = sr[mx_scale_at(e >> 5)];
         c1[r] = VEC ? c0[r] : sr[mx_scale_at(min(e + PER - 1, width - 1) >> 5)];
@@ -327,7 +311,7 @@ __global__ __launch_bounds__(256) void mx_values_kernel(const uint8_t* __restric
 #pragma unroll
     for (int r = 0; r < RB; ++r) {
         if (r0 + r >= rows) break;
-        const int e = min(max(at[r], 0), width - 1);
+        const int e = mx_read_at<FMT, PER, VEC>(at[r], n, width).e;
         float x[8];
         mx_decode8<FMT>(raw[r], 1.f, x);        // (PER of them)
         T* o = out + (size_t)(r0 + r) * (size_t)ldo;
@@ -399,7 +383,7 @@ int dequantize(const MxArg& x, int rows, int n, T* out, int64_t ldo, int width, 
 {
     constexpr int PER = 16 / (int)sizeof(T);
     const bool vec = (uintptr_t)out % 16 == 0 && ldo % PER == 0;
-    const int segs = ((width + PER - 1) / PER + (vec ? 0 : 1) + 63) / 64;
+    const int segs = mx_value_segs(width, PER, vec);
     const int64_t waves = (int64_t)((rows + 3) / 4) * segs;
     const dim3 grid((uint32_t)((waves + 3) / 4));
     if (vec) hipLaunchKernelGGL((mx_values_kernel<T, FMT, true>), grid, dim3(256), 0, stream, x.q, x.ldq, x.s, x.lds, rows, n, segs, out, ldo, width);
