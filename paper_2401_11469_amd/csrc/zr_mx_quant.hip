@@ -167,25 +167,29 @@ __global__ __launch_bounds__(256) void mx_gather_kernel(const T* __restrict__ sr
     }
 }
 
-// Rows too long for LDS that are gathered or of any alignment: element by element.
+// Rows too long for LDS that are gathered or of any alignment: element by element, a segment of a row at a time.  The one kernel here
+// whose lanes can outnumber what a launch can have (32 bits of them: 34 G values, 69 GB; the others' 4 rows a wavefront would be
+// 275 GB): the wavefronts of at most LONG_BLOCKS workgroups take turns.
+constexpr int64_t LONG_BLOCKS = 1 << 22;
 template <class T, int FMT>
 __global__ __launch_bounds__(256) void mx_long_kernel(const T* __restrict__ src, int64_t ld, int rows, int cols, const int32_t* __restrict__ keep,
                                                       int n, int segs, uint8_t* __restrict__ q, int64_t ldq, uint8_t* __restrict__ s, int64_t lds)
 {
     const int lane = threadIdx.x & 63;
-    const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int r = (int)(item / segs), seg = (int)(item % segs);
-    if (r >= rows) return;
-    const int at = seg * SEG + 8 * lane;
-    const T* p = src + (size_t)r * (size_t)ld;
-    float x[8];
+    const int64_t items = (int64_t)rows * segs;
+    for (int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); item < items; item += (int64_t)gridDim.x * 4) {
+        const int r = (int)(item / segs), seg = (int)(item % segs);
+        const int at = seg * SEG + 8 * lane;
+        const T* p = src + (size_t)r * (size_t)ld;
+        float x[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int k = min(at + i, n - 1);
-        const float v = as_float(p[keep ? clamp_idx(keep[k], cols) : k]);
-        x[i] = at + i < n ? v : 0.f;
+        for (int i = 0; i < 8; ++i) {
+            const int k = min(at + i, n - 1);
+            const float v = as_float(p[keep ? clamp_idx(keep[k], cols) : k]);
+            x[i] = at + i < n ? v : 0.f;
+        }
+        store_seg<FMT>(x, q + (size_t)r * (size_t)ldq, s + (size_t)r * (size_t)lds, n, seg, lane);
     }
-    store_seg<FMT>(x, q + (size_t)r * (size_t)ldq, s + (size_t)r * (size_t)lds, n, seg, lane);
 }
 
 // Blocks along the strided axis: a tile of 128 (kept) rows x 64 columns comes into LDS; each thread then takes one block of
@@ -362,7 +366,7 @@ int quantize_rows(const T* src, int64_t ld, int rows, int cols, const int32_t* k
         return hip_status(hipGetLastError());
     }
     const int64_t waves = (int64_t)rows * segs;
-    hipLaunchKernelGGL((mx_long_kernel<T, FMT>), dim3((uint32_t)((waves + 3) / 4)), dim3(256), 0, stream, src, ld, rows, cols, keep, n, segs, q, ldq, s, lds);
+    hipLaunchKernelGGL((mx_long_kernel<T, FMT>), dim3((uint32_t)std::min((waves + 3) / 4, LONG_BLOCKS)), dim3(256), 0, stream, src, ld, rows, cols, keep, n, segs, q, ldq, s, lds);
     return hip_status(hipGetLastError());
 }
 
