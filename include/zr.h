@@ -292,7 +292,7 @@ int zr_mx_dequantize(const void* q, int64_t ldq, const void* scales, int64_t lds
  *  largest of its group of eight, 1e-5 of a result's size on the whole; fp32 results are multiplied in bf16 instead (exact factors).
  *  Products and sums below 2^-126 may be taken for zero.
  *  prev_Y as for zr_resized_linear_fwd.  Launches: 1, +1 if Xq / Xs are written, +1 where a panel of whole rounds of the largest
- *  tiles leaves a rest, +1 for AVERAGE.  Results are repeatable to the bit, and the same whether X is kept in blocks or not; the order
+ *  tiles leaves a rest, +1 for AVERAGE; more where the lanes of one would pass 2^32 (2^36 results on the smallest tiles).  Results are repeatable to the bit, and the same whether X is kept in blocks or not; the order
  *  of a sum depends on the product's extents and formats (and on pitches that 32 bits do not reach) alone.
  *  Errors: NULL, SHAPE, INDEX, DTYPE, MODE, POLICY, LIMIT, HIP. */
 int zr_mx_linear_fwd(const void* X, int64_t ldx, void* Xq, int64_t ldxq, void* Xs, int64_t ldxs, int x_format,

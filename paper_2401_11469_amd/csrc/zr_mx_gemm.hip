@@ -883,6 +883,25 @@ PArgs pargs_of(const MxProduct& p)
     return g;
 }
 
+// The tiles of a part of Y, XCD by XCD.  A launch has 32 bits of lanes (the runtime drops what lies above them without an error): more
+// tiles than that, 2^24 on 256 lanes, are several launches of whole rows of tiles.
+template <int BM, int BN, int LANES, class F> int launch_panels(PArgs g, F&& launch)
+{
+    g.tiles_j = (g.j_end - g.j_base + BN - 1) / BN;
+    const int64_t most = ((1ll << 32) / LANES - 8) / g.tiles_j * BM;           // rows of Y; tiles_j is at most 2^15
+    const int i_end = g.i_end;
+    while (g.i_base < i_end) {
+        g.i_end = (int)std::min<int64_t>(i_end, g.i_base + most);
+        g.tiles_i = (g.i_end - g.i_base + BM - 1) / BM;
+        const int64_t tiles = (int64_t)g.tiles_i * g.tiles_j;
+        launch(g, (uint32_t)((tiles + 7) / 8 * 8));
+        const int st = hip_status(hipGetLastError());
+        if (st != ZR_OK) return st;
+        g.i_base = g.i_end;
+    }
+    return ZR_OK;
+}
+
 template <int FA, int FB, int BM, int BN, int WM, int WN, bool WIDE, class T>
 int launch_tiles(PArgs g, hipStream_t stream)
 {
@@ -890,10 +909,9 @@ int launch_tiles(PArgs g, hipStream_t stream)
     constexpr int lds = tile_bytes<T>(S::TM, 16 * WM, BN, S::RING);
     static AttrFlags flags;
     if (!ensure_max_dynamic_lds((const void*)mx_kernel<FA, FB, BM, BN, WM, WN, WIDE, T>, lds, &flags)) return ZR_ERR_HIP;
-    g.tiles_i = (g.i_end - g.i_base + BM - 1) / BM; g.tiles_j = (g.j_end - g.j_base + BN - 1) / BN;
-    const int64_t tiles = (int64_t)g.tiles_i * g.tiles_j;
-    hipLaunchKernelGGL((mx_kernel<FA, FB, BM, BN, WM, WN, WIDE, T>), dim3((uint32_t)((tiles + 7) / 8 * 8)), dim3(64 * WM * WN), lds, stream, g);
-    return hip_status(hipGetLastError());
+    return launch_panels<BM, BN, 64 * WM * WN>(g, [&](const PArgs& h, uint32_t blocks) {
+        hipLaunchKernelGGL((mx_kernel<FA, FB, BM, BN, WM, WN, WIDE, T>), dim3(blocks), dim3(64 * WM * WN), lds, stream, h);
+    });
 }
 
 template <int FA, int FB, int BM, int BN, int WM, int WN, int NBUF, class T>
@@ -903,10 +921,9 @@ int launch_ring(PArgs g, hipStream_t stream)
     constexpr int lds = tile_bytes<T>(R::TM, R::MS * WM, BN, R::BYTES);
     static AttrFlags flags;
     if (!ensure_max_dynamic_lds((const void*)mx_ring_kernel<FA, FB, BM, BN, WM, WN, NBUF, T>, lds, &flags)) return ZR_ERR_HIP;
-    g.tiles_i = (g.i_end - g.i_base + BM - 1) / BM; g.tiles_j = (g.j_end - g.j_base + BN - 1) / BN;
-    const int64_t tiles = (int64_t)g.tiles_i * g.tiles_j;
-    hipLaunchKernelGGL((mx_ring_kernel<FA, FB, BM, BN, WM, WN, NBUF, T>), dim3((uint32_t)((tiles + 7) / 8 * 8)), dim3(R::NT), lds, stream, g);
-    return hip_status(hipGetLastError());
+    return launch_panels<BM, BN, R::NT>(g, [&](const PArgs& h, uint32_t blocks) {
+        hipLaunchKernelGGL((mx_ring_kernel<FA, FB, BM, BN, WM, WN, NBUF, T>), dim3(blocks), dim3(R::NT), lds, stream, h);
+    });
 }
 
 // Which tiles: 256 x 256, one to a CU; 128 x 128, two to a CU with two units of LDS each or one with four (which hide the way
