@@ -339,9 +339,9 @@ def mx_empty(rows: int, n: int, fmt: int, device="cuda") -> MX:
 
 
 # The calls below are made once a layer and token while decoding, where the host's part of a call is longer than the GPU's:
-# attributes are looked up once, the current stream without an object for it.
-_raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else None
-_get_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else None
+# attributes are looked up once, the current stream without an object for it (by torch's public calls where it has no shorter way).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+_get_device = getattr(torch._C, "_cuda_getDevice", None) or (lambda: torch.cuda.current_device())
 _DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
 
 
