@@ -303,9 +303,12 @@ int zr_mx_linear_fwd(const void* X, int64_t ldx, void* Xq, int64_t ldxq, void* X
 /* zr_resized_linear_bwd from a checkpoint of X in blocks (any format): Xq / Xs hold [M x n_keep] in DROP_K (the kept columns) and
  * [M x K] in DROP_N, as zr_mx_quantize and zr_mx_linear_fwd leave them.  W, dY, dX, dW, lists, policies and errors as
  * there; dX and dW are the gradients at the values that the checkpoint stands for.
- *  workspace: needed for dW (NULL otherwise allowed), 16-byte aligned, at least zr_mx_bwd_workspace_bytes: the checkpoint's
+ *  workspace: needed for dW (NULL otherwise allowed), 16-byte aligned, of zr_mx_bwd_workspace_bytes: the checkpoint's
  *  values go there ([M x width], width = the held columns rounded up to 64), and what is left serves as
- *  zr_resized_linear_bwd's scratch.  Errors also: NULL without it, SHAPE if it is too small or not aligned. */
+ *  zr_resized_linear_bwd's scratch.  Less will do, down to the values alone (M * width elements of dtype), with fewer ways open to the
+ *  products.  In DROP_K and bf16 2 * M * width bytes less lose no launch a thing that an uncompressed call has: it would extract the
+ *  kept columns there, which the checkpoint holds side by side.  Errors also: NULL without it, SHAPE if it is smaller than the values
+ *  or not aligned. */
 size_t zr_mx_bwd_workspace_bytes(int32_t M, int32_t K, int32_t N, int32_t n_keep, int mode, int dtype);
 int zr_resized_linear_bwd_mx(const void* Xq, int64_t ldxq, const void* Xs, int64_t ldxs, int x_format,
                              const void* W, int64_t ldw, const void* dY, int64_t lddy,

@@ -510,13 +510,21 @@ def mx_bwd_workspace_bytes(M: int, K: int, N: int, n_keep: int, mode: int, dtype
     return int(_lib.zr_mx_bwd_workspace_bytes(M, K, N, n_keep, mode, dtype if isinstance(dtype, int) else _code(dtype)))
 
 
+def _bwd_scratch(M: int, K: int, N: int, n_keep: int, mode: int, dt) -> int:
+    """Bytes for a call that is given no buffer: without the place of the columns that a call on uncompressed X extracts, which
+    are side by side in a DROP_K checkpoint.  (With them 20 of 211 large calls split their contraction into more slices, 17 of those
+    to no gain.)"""
+    size = mx_bwd_workspace_bytes(M, K, N, n_keep, mode, dt)
+    return size - 2 * M * ((n_keep + 63) // 64 * 64) if mode == DROP_K and dt is torch.bfloat16 else size
+
+
 def resized_linear_bwd_mx(X: Optional[MX], W: torch.Tensor, dY: torch.Tensor, keep_idx: torch.Tensor, mode: int, policy: int = ZERO,
                           prev_dX: Optional[torch.Tensor] = None, prev_dW: Optional[torch.Tensor] = None,
                           dX: Optional[torch.Tensor] = None, dW: Optional[torch.Tensor] = None, need_dX: bool = True,
                           need_dW: bool = True, workspace: Optional[torch.Tensor] = None, stream=None,
                           w_layout: int = W_KN) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor]]:
     """resized_linear_bwd from the checkpoint of X: [M, n_keep] in blocks (DROP_K) or [M, K] (DROP_N).  workspace: of
-    mx_bwd_workspace_bytes bytes, needed for dW (None: allocated)."""
+    mx_bwd_workspace_bytes bytes (zr.h says how far less will do), needed for dW (None: allocated)."""
     here = _here()
     on = _on(stream, here)
     M, N = dY.shape
@@ -549,7 +557,7 @@ def resized_linear_bwd_mx(X: Optional[MX], W: torch.Tensor, dY: torch.Tensor, ke
     dW, dwp, lddw, pwp = result(need_dW, dW, prev_dW, wshape, "dW")
     xq, ldxq, xs, ldxs, fmt = _mx(X if need_dW else None, M, n_keep if mode == DROP_K else K, here, "X")
     if workspace is None and need_dW:
-        workspace = _empty(mx_bwd_workspace_bytes(M, K, N, n_keep, mode, dt), torch.uint8, dY.device, stream, returned=False)
+        workspace = _empty(_bwd_scratch(M, K, N, n_keep, mode, dt), torch.uint8, dY.device, stream, returned=False)
     if workspace is not None and workspace.get_device() != here:
         raise ValueError("workspace: must be on the current GPU")
     st = _lib.zr_resized_linear_bwd_mx(xq, ldxq, xs, ldxs, fmt, wp, ldw, gp, ldg, dxp, lddx, dwp, lddw, M, K, N,
