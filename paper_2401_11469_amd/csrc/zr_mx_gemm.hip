@@ -114,7 +114,8 @@ __device__ __forceinline__ f32x16 mma32(const Frag& a, uint32_t sa, const Frag& 
 // Wide products.  The 8-bit form of the instruction adds up groups of eight products after cutting each at 2^-13 of the
 // group's largest (read off the hardware with two-term sums); rounded to bf16 that is lost in the rounding (1e-5 of a
 // result's size, against 2^-9), but an fp32 result would show it.  For fp32 results with an 8-bit operand the elements,
-// scaled, are turned into bf16 (exact: at most 4 significant bits) and multiplied by the bf16 instruction, whose sums are fp32.
+// scaled, are turned into bf16 (at most 4 significant bits: exact from 2^-126 up, below that the nearest multiple of 2^-133) and multiplied
+// by the bf16 instruction, whose sums are fp32.
 // Eight elements (8 bytes, or 4 in .x) -> bf16
 template <int F> __device__ __forceinline__ bf16x8 widen8(uint2 r, float scale)
 {
