@@ -304,7 +304,9 @@ int zr_mx_linear_fwd(const void* X, int64_t ldx, void* Xq, int64_t ldxq, void* X
 
 /* zr_resized_linear_bwd from a checkpoint of X in blocks (any format): Xq / Xs hold [M x n_keep] in DROP_K (the kept columns) and
  * [M x K] in DROP_N, as zr_mx_quantize and zr_mx_linear_fwd leave them.  W, dY, dX, dW, lists, policies and errors as
- * there; dX and dW are the gradients at the values that the checkpoint stands for.
+ * there (keep_idx is needed: all indices where nothing is pruned).  dW is the gradient at the values that the checkpoint stands for; dX
+ * is dY times W as it is given: where the forward multiplied the blocks of a W that is kept in full (a training step), that is the
+ * straight-through gradient, and with W's own values from zr_mx_dequantize it is the forward's exact one.
  *  workspace: needed for dW (NULL otherwise allowed), 16-byte aligned, of zr_mx_bwd_workspace_bytes: the checkpoint's
  *  values go there ([M x width], width = the held columns rounded up to 64), and what is left serves as
  *  zr_resized_linear_bwd's scratch.  Less will do, down to the values alone (M * width elements of dtype), with fewer ways open to the
