@@ -44,22 +44,17 @@ __device__ __forceinline__ void to_lds16(const void* gptr, uint32_t lds_uniform)
 {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" :: "v"(gptr), "s"(lds_uniform) : "memory");
 }
-// (and for the LDS reads, so that no read of a stage is under way when the barrier behind lets others write there)
 // the same from a uniform address plus a lane's 32-bit offset
 __device__ __forceinline__ void to_lds16(const uint8_t* base, uint32_t off, uint32_t lds_uniform)
 {
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" :: "v"(off), "s"(base), "s"(lds_uniform) : "memory");
 }
+// All but the last N requests have landed; and the LDS reads, so that no read of a stage is under way when the barrier behind lets
+// others write there.
 template <int N> __device__ __forceinline__ void wait_vm()
 {
     static_assert(N >= 0 && N < 64, "vmcnt is a 6-bit field");
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(N) : "memory");
-}
-
-template <int N> __device__ __forceinline__ void wait_vm_only()
-{
-    static_assert(N >= 0 && N < 64, "vmcnt is a 6-bit field");
-    asm volatile("s_waitcnt vmcnt(%0)" :: "n"(N) : "memory");
 }
 
 // f(0), f(1), .. f(N - 1) with constants
