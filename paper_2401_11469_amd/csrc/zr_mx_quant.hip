@@ -352,15 +352,19 @@ int quantize_rows(const T* src, int64_t ld, int rows, int cols, const int32_t* k
     const bool odd = (uintptr_t)src % 16 != 0 || ld * es % 16 != 0 || cols * es % 16 != 0;
     const int pitch = odd ? (cols * es + 15 + 15) / 16 * 16 : cols * es, chunks = pitch / 16, list = keep ? (n + 7) / 8 * 16 : 0;
     if (pitch + list <= 64 * 1024) {
-        // rows to a workgroup: four where thousands of workgroups remain, as many as 64 KB of LDS hold
-        const int rb = std::max(1, std::min({chunks <= 1024 ? 4 : chunks <= 2048 ? 2 : 1, (64 * 1024 - list) / pitch, rows / 1024}));
+        // Rows to a workgroup: short ones up to four, where a thousand workgroups remain; long ones alone, of which the LDS holds more
+        // workgroups.  bf16 into 8 bits, one row to a workgroup and four: 8192 x 1000, 750 kept, 9.7 and 7.0 us; 4096 x 2752 of 2064 11.5 and
+        // 9.5; 197 x 256 of 192 2.7 and 2.9; 1500 x 1000 of 750 3.7 and 3.7.  One and two: 8192 x 8000 of 6000 45 and 50, 2048 x 8000 15.1 and
+        // 16.7, 8192 x 11008 of 8256 73 and 87 (the least to gain: fp32 2048 x 4000 of 3000 10.5 and 9.5).  Chunks a thread: as few as hold the row (8192 x 2752 in two 17.6, in four 18.2; 8192 x 8000
+        // in four 45.3, in eight 46.1; 8192 x 11008 in eight 72.9, in sixteen 74.8); single short rows in two (2.5 us in one, 2.7).
+        const int rb = std::max(1, std::min({chunks <= 512 ? 4 : 1, (64 * 1024 - list) / pitch, rows / 1024}));
 #define ZR_GATHER_AS(KL, RB, ODD)                                                                                                              \
         hipLaunchKernelGGL((mx_gather_kernel<T, FMT, KL, RB, ODD>), dim3((rows + rb - 1) / rb), dim3(256), (size_t)rb * pitch + list, stream, src, ld, rows, \
                            cols, keep, n, segs, rb, pitch, q, ldq, s, lds)
 #define ZR_GATHER(KL, RB) do { if (odd) ZR_GATHER_AS(KL, RB, true); else ZR_GATHER_AS(KL, RB, false); } while (0)
-        if (rb == 1 && chunks <= 512) ZR_GATHER(2, 1); else if (rb == 1 && chunks <= 1024) ZR_GATHER(4, 1);
-        else if (chunks <= 256) ZR_GATHER(1, 4); else if (chunks <= 512) ZR_GATHER(2, 4); else if (chunks <= 1024) ZR_GATHER(4, 4);
-        else if (chunks <= 2048) ZR_GATHER(8, 2); else ZR_GATHER(16, 1);
+        if (chunks <= 512) {
+            if (rb == 1) ZR_GATHER(2, 1); else if (chunks <= 256) ZR_GATHER(1, 4); else ZR_GATHER(2, 4);
+        } else if (chunks <= 1024) ZR_GATHER(4, 1); else if (chunks <= 2048) ZR_GATHER(8, 1); else ZR_GATHER(16, 1);
 #undef ZR_GATHER_AS
 #undef ZR_GATHER
         return hip_status(hipGetLastError());

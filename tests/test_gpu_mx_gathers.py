@@ -10,19 +10,13 @@ from test_gpu_mx import torch, zr  # noqa: F401  (fixtures)
 
 pytestmark = pytest.mark.gpu
 
-# rows, bytes of a row / 2, kept (0: all, from rows off 16 bytes): chunks of 16 bytes to a thread, rows to a workgroup
-FORMS = [(4099, 1000, 751),         # one chunk, four rows
-         (3073, 1999, 1500),        # three of them
-         (2049, 520, 0),            # two
-         (8191, 2752, 2064),        # two chunks, four rows
-         (2050, 4001, 0),           # two rows
-         (4103, 8000, 100),         # four chunks, four rows
-         (4101, 8000, 5001),        # three: what the list leaves
-         (2051, 8192, 8191),        # two
-         (2053, 11008, 8256),       # eight chunks, two rows
-         (70, 11009, 0),            # one row of as many
-         (1500, 20000, 12001),      # sixteen chunks
-         (40, 32750, 0)]
+# rows, bytes of a row / 2, kept (0: all, from rows off 16 bytes).  Up to 256, 512, 1024, 2048 and 4096 chunks of 16 bytes a row; where the
+# rows are short, four, three and two of them to a workgroup; a last workgroup of fewer.
+FORMS = [(4099, 1000, 751), (3073, 1999, 1500), (2049, 520, 0),
+         (8191, 2752, 2064), (2050, 4001, 0),
+         (4103, 8000, 100), (4101, 8000, 5001), (2051, 8192, 8191),
+         (2053, 11008, 8256), (70, 11009, 0),
+         (1500, 20000, 12001), (40, 32750, 0)]
 
 
 @pytest.mark.parametrize("fmt", [E4M3, E2M1, INT8])
