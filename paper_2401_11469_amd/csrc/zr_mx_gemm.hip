@@ -288,9 +288,9 @@ template <class T> constexpr int tile_bytes(int TM, int rows, int BN, int loop)
 }
 
 // ---------------------------------------------------------------------------
-// Tiles of BM x BN on WM x WN wavefronts: 64 x 64 for short contractions and small products (985 x 751 x 771 5 us, most of it the
-// launch, the first loads and the store), and the wide products (4096 x 2048 x 2048 44 us, 0.77 PFLOP/s, bound by the conversions
-// beside the bf16 instruction).  The contraction travels in steps of 128 through a ring of LDS stages, straight from memory;
+// Tiles of BM x BN on WM x WN wavefronts: 64 x 64 for short contractions and small products, and the wide products (bf16 results from
+// 8 x 4 bits, 985 x 751 x 771: 5.1 us, most of it the launch, the first loads and the store; fp32 ones 6.8; fp32 4096 x 2048 x 2048 43 us in 8 x 4 bits, 0.80
+// PFLOP/s, bound by the conversions beside the bf16 instruction).  The contraction travels in steps of 128 through a ring of LDS stages, straight from memory;
 // the scales of four steps at a time, into two places of their own.
 // ---------------------------------------------------------------------------
 template <int FA, int FB, int BM, int BN, int WM, int WN> struct Shape {
@@ -952,6 +952,18 @@ template <int FA, int FB> double kind_us(Kind kind, int I, int J, int C)
     return 3.0 + 0.2 * q + std::max(1.0, q) * S64[F] * K;
 }
 
+// Wide products: 64 x 64 or 128 x 128, in rounds of one tile to a CU.  Fitted to 20 sizes (48 to 1100 tiles of 128 x 128) with contractions of
+// 512, 2048 and 6000, both formats of W; what it picks takes 0.1 % more than the shorter on average (128 x 128 from 192 tiles on: 5).  (2048 deep, 8 x 4 bits, 64 and 128: 160 tiles of
+// 128 x 128 20.5 and 22.0 us; 208 25.8 and 22.5; 256 26.2 and 23.4; 288 30.9 and 41.4; 512 46.6 and 43.0; 576 52.0 and 61.2; 1024 89 and 83.  6000 deep, 8 x 8
+// bits, 256 tiles: 71 and 57.)
+template <int FB> double wide_us(int b, int I, int J, int C)
+{
+    constexpr bool W4 = FB == E2;
+    const double K = C / 1024.0, rounds = (double)((tiles_of(I, J, b) + 255) / 256);
+    if (b == 64) return 3.0 + (W4 ? 0.8 : 0.5) * K + rounds * (W4 ? 0.4 + 2.45 * K : 0.7 + 2.74 * K);
+    return (W4 ? 1.5 : 2.0) + rounds * (W4 ? 4.3 + 8.0 * K : 4.0 + 8.25 * K);
+}
+
 template <int FA, int FB> Plan plan(int I, int J, int C)
 {
     auto small = [&](int i, int j) {
@@ -1002,9 +1014,7 @@ int launch_formats(const MxProduct& p, hipStream_t stream)
         return p.raw ? launch_few<FA, FB, WIDE, true, 8, T>(g, grid, stream) : launch_few<FA, FB, WIDE, false, 8, T>(g, grid, stream);
     }
     if constexpr (WIDE) {
-        // (56 tiles of 128 x 128, 985 x 751 x 771: 14.1 us, 7.1 on 64 x 64; 160, 1280 x 2048 x 2048: 22.5 and 20.5; 256, 2048 x 1024 x
-        // 2048: 15.4 and 16.3; 512, 4096 x 2048 x 2048: 44 and 48)
-        if (tiles_of(p.M, p.J, 128) >= 192) return launch_tiles<FA, FB, 128, 128, 2, 2, true, T>(g, stream);
+        if (wide_us<FB>(128, p.M, p.J, p.C) < wide_us<FB>(64, p.M, p.J, p.C)) return launch_tiles<FA, FB, 128, 128, 2, 2, true, T>(g, stream);
         return launch_tiles<FA, FB, 64, 64, 2, 2, true, T>(g, stream);
     } else {
         const Plan best = plan<FA, FB>(p.M, p.J, p.C);
