@@ -681,9 +681,9 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void mx_ring_kernel(const PArgs g)
 // Up to 16 rows of X: the weight is read once, straight into registers, and that is the time.  A workgroup has 16 rows of W; its
 // NWV wavefronts split the contraction and add up in LDS, in their order.  RAW: X arrives in its own type, and the workgroup
 // puts it into blocks in LDS (a lane 8 values, as the quantiser does: each wavefront for itself, in the layout of
-// the matrix instruction, 15 of 16 lanes would do one row's work again: 1 x 8192 x 8192 in 4 bits 23 us, now 11.7), while its
-// first part of the weight is on the way.  1 x 4096 x 2752 6.2 us (5.6 MB of weight, 1.1 us at the copy's rate: an empty launch, the first load and
-// the sum over the wavefronts are the rest), 1 x 4096 x 11008 8.5.
+// the matrix instruction, 15 of 16 lanes would do one row's work again: 1 x 8192 x 8192 in 4 bits 23 us, now 11.3), while its
+// first part of the weight is on the way.  1 x 4096 x 2752 4.6 us (5.6 MB of weight, 1.1 us at the copy's rate: an empty launch, the first load and
+// the sum over the wavefronts are the rest), 1 x 4096 x 11008 8.2 (graphs of 20 calls).
 // ---------------------------------------------------------------------------
 constexpr int FEW_LDS = 64 * 1024;      // bytes of X in LDS at a time
 // values of a row that are put into blocks at a time
@@ -1005,12 +1005,16 @@ template <int FA, int FB, bool WIDE, class T>
 int launch_formats(const MxProduct& p, hipStream_t stream)
 {
     const PArgs g = pargs_of(p);
-    // (in blocks already 4096 x 2752 in 4 bits takes one row 6.4 us, 8 rows 8.0 and 16 rows 9.4; on 64 x 64 tiles 7.8.  All of them
+    // (in blocks already 4096 x 2752 in 4 bits takes one row 4.2 us, 8 rows 5.2 and 16 rows 5.8; on 64 x 64 tiles 7.4.  All of them
     // run here, so that a result is the same to the bit whether its input was kept in blocks or not.)
     if (p.M <= MX_FEW) {
-        // 16 wavefronts where that leaves at most one workgroup to a CU, 8 for more
+        // 8 wavefronts; 16 for contractions of more than 16384 where there is at most one workgroup to a CU and X is in 4 bits or at most 4
+        // rows.  16 and 8, 4096 columns, graphs of 20 calls: 1 x 4096 in 8 x 4 bits from X itself 6.0 and 4.6 us, from blocks 6.8 and
+        // 4.5; 1 x 11008 10.2 and 9.4; 1 x 22016 (from blocks) 14.6 and 15.2; 16 x 22016 in 4 x 4 bits 42 and 60 (fp32, from X itself), 19.0 and 19.0
+        // (from blocks); 16 x 22016 in 8 x 4 bits from blocks 43 and 24.  More columns: 1 x 4096 into 11008 14.8 and 8.2.
         const dim3 grid((p.J + 15) / 16);
-        if (grid.x <= 256) return p.raw ? launch_few<FA, FB, WIDE, true, 16, T>(g, grid, stream) : launch_few<FA, FB, WIDE, false, 16, T>(g, grid, stream);
+        if (grid.x <= 256 && p.C > 16384 && (FA == E2 || p.M <= 4))
+            return p.raw ? launch_few<FA, FB, WIDE, true, 16, T>(g, grid, stream) : launch_few<FA, FB, WIDE, false, 16, T>(g, grid, stream);
         return p.raw ? launch_few<FA, FB, WIDE, true, 8, T>(g, grid, stream) : launch_few<FA, FB, WIDE, false, 8, T>(g, grid, stream);
     }
     if constexpr (WIDE) {

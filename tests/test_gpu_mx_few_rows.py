@@ -1,5 +1,5 @@
-"""Up to 16 rows of X: contractions that pass through LDS in more than one part (64 K of X in 8 bits, 128 K in 4, are one), and enough
-columns for workgroups of eight wavefronts (more than 256 workgroups of 16).  Against float64, within the bounds of test_gpu_mx.py; an input
+"""Up to 16 rows of X: contractions that pass through LDS in more than one part (64 K of X in 8 bits, 128 K in 4, are one), with 8 and with
+16 wavefronts to a workgroup, and more columns than the chip takes at once (256 workgroups of 16).  Against float64, within the bounds of test_gpu_mx.py; an input
 that arrives in its own type and one in blocks give the same to the bit."""
 import pytest
 
@@ -43,7 +43,7 @@ def test_contractions_of_several_parts(torch, zr, M, C, dtype, xf, wf):  # noqa:
 @pytest.mark.parametrize("xf,wf", PAIRS)
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("M,N,C", [(1, 4096, 300), (1, 4112, 1000), (9, 4112, 7300), (16, 4099, 4200), (1, 11008, 4096), (16, 11008, 512), (3, 40000, 129)])
-def test_columns_for_workgroups_of_eight_wavefronts(torch, zr, M, N, C, dtype, xf, wf):  # noqa: F811
+def test_more_columns_than_the_chip_takes_at_once(torch, zr, M, N, C, dtype, xf, wf):  # noqa: F811
     dt = tdt(torch, dtype)
     cut = dtype == "bf16" and xf == E4M3
     X, W = normal(torch, M + C, M, C, dtype=dt), normal(torch, N, N, C, dtype=dt, scale=0.05)
@@ -55,7 +55,7 @@ def test_columns_for_workgroups_of_eight_wavefronts(torch, zr, M, N, C, dtype, x
     check(torch, Y, xv, wv, dtype, cut)
     assert torch.equal(zr.mx_linear_fwd(xm, wm, dtype=dt), Y)
     assert torch.all(buf[M] == 77.0) and torch.all(buf[:, N:] == 77.0)
-    # kept features, more and fewer than take eight wavefronts; the others as they were
+    # kept features, the others as they were
     for n in {max(1, N - 7), N * 3 // 4}:
         s = subset(n, N, n)
         keep, k = idx(torch, s), torch.from_numpy(s).long().cuda()
