@@ -153,7 +153,7 @@ __device__ __forceinline__ bool tile_of(const PArgs& g, int& ti, int& tj)
 // acc[a][b][i] of MS x MS results: row 4 (lane / MS) + i % 4 + 8 (i / 4), column lane % MS.
 // A scattering tile owns the original columns from its first kept one (0 for the first tile) up to the next tile's first (all for
 // the last).  It lays them out by ORIGINAL column, 2 BN of them and SC groups of rows at a time: the imputed values, the
-// results on top, then copied out like a plain tile (8192 x 4096 x 2752 of 2064 kept, 4 bits: 57 us, 49 without the scatter; 84 with a
+// results on top, then copied out like a plain tile (8192 x 4096 x 2752 of 2064 kept, 4 bits: 55 us, 45 without the scatter; 84 with a
 // table of columns looked up for every element).
 template <class T, int BM, int BN, int WM, int WN, int MS, int SG, int SC, int TM, int TN, class ACC>
 __device__ void store_tile(const PArgs& g, uint8_t* smem, ACC (&acc)[TM][TN], int i0, int j0, int tid, int wave, int lane)
@@ -470,11 +470,15 @@ __global__ __launch_bounds__(64 * WM * WN) void mx_kernel(const PArgs g)
 // instructions.  The one barrier of a unit stands where its last fragments have been read, two row groups before its last product:
 // behind it the first fragments of the next unit are read, and the unit after that may be requested.
 //
-// What it measured.  8192 x 8192 x 8192: 4 x 4 bits 242 us (4.5 PFLOP/s), 8 x 4 376 (2.9), 8 x 8 406 (2.7); the instructions alone, on
-// registers, hold 7.6 and 4.3 PFLOP/s at the clock that the chip then keeps (1.8 GHz of 2.4).  8192 x 4096 x 2048, one round of 256 tiles: 42,
-// 59 and 59 us.  What bounds it is the way of the operands: the requests alone take 0.33 us for what the instructions do in 0.48, the LDS
-// reads 0.2, and they hide each other in part (0.7 together).  Rows of 64 bytes a request, half a cache line, in four stages of a ring:
-// 72 us for 8 x 8 (70 % more time for the requests); scales fetched for one group of 512 at a time, 16 bytes of a line: 15 % of all requests.
+// What it measured.  8192 x 8192 x 8192: 4 x 4 bits 239 us (4.6 PFLOP/s), 8 x 4 374 (2.9), 8 x 8 403 (2.7); the instructions alone, on
+// registers, hold 7.6 and 4.3 PFLOP/s at the clock that the chip then keeps (1.8 GHz of 2.4).  8192 x 4096 x 2048, one round of 256 tiles: 37,
+// 54 and 57 us.  Taken apart, the requests alone take 0.33 us for what the instructions do in 0.48, the LDS reads 0.2, and they hide each
+// other in part (0.7 together).  Counters: at 8192 x 8192 x 8192 the matrix unit is busy 55, 70 and 67 % of the time (4 x 4, 8 x 4, 8 x 8), in the
+// one round 34 to 51; the LDS a fifth to a third of it, the queues of the memory requests are never full; wavefronts stand at waits and the barrier for
+// 36 to 41 % of their time and for their turn to issue another 33 to 45.  So no unit but the matrix unit is near full: it is the time until a unit
+// of the operands has landed, of which two places let one be on its way, and in one round the fill and the store.  Rows of 64 bytes a request, half a
+// cache line, in four stages of a ring: 72 us for 8 x 8 (70 % more time for the requests); scales fetched for one group of 512 at a time, 16 bytes
+// of a line: 15 % of all requests.
 // Offsets from uniform addresses and not pointers: with pointers the loop spilled.
 // ---------------------------------------------------------------------------
 template <int FA, int FB, int BM_, int BN_, int WM_, int WN_, int NBUF_> struct Ring {

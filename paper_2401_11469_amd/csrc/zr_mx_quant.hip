@@ -74,8 +74,8 @@ __global__ __launch_bounds__(256) void mx_rows_kernel(const T* __restrict__ src,
 // Rows of any alignment, and gathered columns: up to RB whole rows come into LDS in aligned 16-byte chunks, KL to a thread
 // (what lies before the first and behind the last whole chunk of a row by elements, one to a thread), the list beside them in 16
 // bits; all of it is requested at once.  The wavefronts then share out the segments of all rows.  ODD: some row does not begin and
-// end on 16-byte addresses (false is a variant for speed alone: 18.3 us against 19.7 at the size below).
-// (bf16 8192 x 2752, 2064 kept, into 8 bits: 18.3 us, 3.4 TB/s; 46 with the list read from memory by every lane.  A copy would
+// end on 16-byte addresses (false is a variant for speed alone: 17.4 us against 19.6 at the size below).
+// (bf16 8192 x 2752, 2064 kept, into 8 bits: 17.4 us, 3.6 TB/s; 46 with the list read from memory by every lane.  A copy would
 // take 12; bound by the vector instructions, 200 for 8 values of a lane, and the 2-byte LDS reads, half of them bank conflicts)
 template <class T, int FMT, int KL, int RB, bool ODD>
 __global__ __launch_bounds__(256) void mx_gather_kernel(const T* __restrict__ src, int64_t ld, int rows, int cols, const int32_t* __restrict__ keep,
@@ -195,7 +195,9 @@ __global__ __launch_bounds__(256) void mx_long_kernel(const T* __restrict__ src,
 // Blocks along the strided axis: a tile of 128 (kept) rows x 64 columns comes into LDS; each thread then takes one block of
 // one column (its lanes 64 neighbouring columns: no bank conflicts, no exchange between lanes), and the elements go through
 // LDS once more, so that each column's 64 or 128 bytes leave together.
-// (bf16 2752 x 4096, 2064 rows kept, into 8 bits 7.0 us, 3.7 TB/s; fp32 4096 x 11008 36.6 us, 6.2 TB/s; rows of 4097 12.3 us)
+// (bf16 2752 x 4096, 2064 rows kept, into 8 bits 7.2 us, 3.6 TB/s; fp32 4096 x 11008 36.4 us, 6.2 TB/s.  Rows of 4097 12.4 us: 64 columns lie
+// in nine chunks of two cache lines and not in eight of one, 45 % more requests and 1.8 times the vector instructions; wavefronts wait for memory
+// 72 % of the time, 67 where rows are aligned.)
 template <class T, int FMT, bool VEC>
 __global__ __launch_bounds__(256) void mx_cols_kernel(const T* __restrict__ src, int64_t ld, int rows, int cols, const int32_t* __restrict__ keep,
                                                       int n, uint8_t* __restrict__ q, int64_t ldq, uint8_t* __restrict__ s, int64_t lds)
