@@ -320,6 +320,92 @@ int zr_resized_linear_bwd_mx(const void* Xq, int64_t ldxq, const void* Xs, int64
                              const int32_t* keep_idx, int32_t n_keep, int mode, int w_layout, int dtype, int policy,
                              const void* prev_dX, const void* prev_dW, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- Around the products of a block: bias, activation, gate, dropout, residual, norms ----
+ *
+ * Dropout D with probability p: an element of row r and column c is dropped, i.e. becomes +0, where half c % 8 of the draw of its
+ * group of eight columns is below q = round(65536 p) (at most 65535); the others are multiplied by 65536 / (65536 - q).  The draw is
+ * Philox 4 x 32 with 7 rounds (Salmon et al. 2011), key = the seed, counter = (c / 8, r, low and high word of the offset); its four
+ * words are eight halves, the low one first.  No mask is stored: a call with the same rng, in the forward and the backward
+ * pass, draws the same.
+ *  rng: DEVICE pointer (8-byte aligned) to two uint64, seed and offset, read when the kernel runs: a captured graph draws anew
+ *  where the caller changes them between replays.  Calls that should differ differ in either.  Not read, and may be NULL, with
+ *  q = 0.  0 <= p < 1, else ZR_ERR_RATIO. */
+
+/* out = D(x), [rows x cols]; the backward pass is the same call on the gradient.  out may be x (same pitch).  One launch.
+ *  Errors: NULL, SHAPE, DTYPE, RATIO, LIMIT, HIP. */
+int zr_dropout(const void* x, int64_t ldx, void* out, int64_t ldo, int32_t rows, int32_t cols, double p, const uint64_t* rng,
+               int dtype, void* stream);
+
+/* Activations.  ZR_ACT_GELU: z Phi(z), Phi the normal distribution function; ZR_ACT_GELU_TANH:
+ * z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2; ZR_ACT_SILU: z / (1 + e^-z). */
+typedef enum { ZR_ACT_NONE = 0, ZR_ACT_RELU = 1, ZR_ACT_GELU = 2, ZR_ACT_GELU_TANH = 3, ZR_ACT_SILU = 4 } zr_act;
+
+/* zr_resized_linear_fwd with Zero imputation, and what follows the product in a block in the same pass:
+ *   Z = P + bias,  Y = residual + D(act(Z) * gate),   P = the result of zr_resized_linear_fwd
+ * (dropped columns of DROP_N: P = 0, so they hold what bias, activation and so on make of that).
+ *  bias [N]; gate, residual, Z [M x N] with their pitches; all may be NULL: bias and residual add nothing, gate is 1, Z is not
+ *  kept.  dtype: of all tensors.  Sums, activation and everything behind them are fp32, each output is rounded once.
+ *  keep_idx NULL: nothing is pruned, n_keep is ignored.  Y may be gate or residual (same pitch); Z must not overlap another tensor.
+ *  workspace: optional, of zr_act_fwd_workspace_bytes bytes, 16-byte aligned: room for what zr_resized_linear_fwd extracts.
+ *  Launches: 1, +1 with a workspace where kept columns are extracted (DROP_K), +1 for a remainder panel.
+ *  Errors: NULL, SHAPE, INDEX, DTYPE, MODE (also a bad w_layout or act), RATIO, LIMIT, HIP. */
+size_t zr_act_fwd_workspace_bytes(int32_t M, int32_t K, int32_t N, int32_t n_keep, int mode, int dtype);
+int zr_resized_linear_act_fwd(const void* X, int64_t ldx, const void* W, int64_t ldw, void* Y, int64_t ldy,
+                              int32_t M, int32_t K, int32_t N, const int32_t* keep_idx, int32_t n_keep, int mode, int w_layout, int dtype,
+                              const void* bias, int act, const void* gate, int64_t ldg, double p, const uint64_t* rng,
+                              const void* residual, int64_t ldr, void* Z, int64_t ldz,
+                              void* workspace, size_t workspace_bytes, void* stream);
+
+/* Its backward pass.  With T = D(dY) (the forward's p and rng):
+ *   dgate = T * act(Z),  dZ = T * gate * act'(Z),  dbias = column sums of dZ,  dX and dW = zr_resized_linear_bwd at dZ, Zero imputed
+ * (the gradient of the residual is dY).  act'(0) of ZR_ACT_RELU is 0.
+ *  Z [M x N]: the forward's, needed unless act is ZR_ACT_NONE and dgate is NULL.  gate: the forward's or NULL.
+ *  dX [M x K], dW (stored like W), dbias [N], dgate [M x N]: outputs, each may be NULL, not all.  dgate may be gate, Z or dY (same
+ *  pitch); no other output may overlap an input.  X is needed for dW, W for dX.
+ *  dZ is held in dtype between the two steps (bf16: one rounding more, before sums over all of its terms, as the matrix
+ *  instruction takes its operands in bf16); dbias adds up dZ before that rounding, in fp32.
+ *  workspace: of zr_act_bwd_workspace_bytes bytes, 16-byte aligned; needed where dZ is not dY itself (act, gate or p), or dbias is
+ *  wanted (else NULL is allowed).  Less will do, down to dZ ([M x N rounded up to 8] in dtype) and dbias's sums, with fewer ways open
+ *  to the products.  Errors: as above; SHAPE also for a workspace that is too small, NULL without one. */
+size_t zr_act_bwd_workspace_bytes(int32_t M, int32_t K, int32_t N, int32_t n_keep, int mode, int dtype);
+int zr_resized_linear_act_bwd(const void* X, int64_t ldx, const void* W, int64_t ldw, const void* dY, int64_t lddy,
+                              const void* Z, int64_t ldz, const void* gate, int64_t ldg,
+                              void* dX, int64_t lddx, void* dW, int64_t lddw, void* dbias, void* dgate, int64_t lddg,
+                              int32_t M, int32_t K, int32_t N, const int32_t* keep_idx, int32_t n_keep, int mode, int w_layout, int dtype,
+                              int act, double p, const uint64_t* rng, void* workspace, size_t workspace_bytes, void* stream);
+
+/* A block's output joins the residual stream, and the next block's input leaves it:
+ *   n = post(D(y + bias)),  x_out = x + scale * gate * n,  h = pre(x_out)
+ * for rows of `cols` features (after the all-reduce of a row-parallel projection every task calls it with the same rng).
+ *  norms: ZR_JOIN_POST and ZR_JOIN_PRE say which norms there are (without POST n is D(y + bias); without PRE there is no h, which
+ *  is then ignored).  norm: ZR_NORM_RMS v / sqrt(mean(v^2) + eps), ZR_NORM_LAYER (v - mean) / sqrt(variance + eps); then * weight
+ *  + bias, where those are given ([cols], NULL: 1 and 0).  eps >= 0 (else ZR_ERR_RATIO).
+ *  bias, gate [cols] or NULL (0, 1).  dtype: of all tensors and vectors; everything between is fp32, h is the norm of x_out before its
+ *  rounding.  x_out may be x or y, h may be y (same pitch); x_out and h must not overlap.  1 <= cols <= 16384 (else LIMIT).
+ *  One launch.  Errors: NULL, SHAPE, DTYPE, MODE (norm, norms), RATIO, LIMIT, HIP. */
+typedef enum { ZR_NORM_RMS = 0, ZR_NORM_LAYER = 1 } zr_norm;
+typedef enum { ZR_JOIN_POST = 1, ZR_JOIN_PRE = 2 } zr_join_norms;
+int zr_block_join_fwd(const void* y, int64_t ldy, const void* x, int64_t ldx, void* x_out, int64_t ldxo, void* h, int64_t ldh,
+                      int32_t rows, int32_t cols, int norms, int norm, double eps, double p, const uint64_t* rng, double scale,
+                      const void* bias, const void* gate, const void* post_w, const void* post_b, const void* pre_w, const void* pre_b,
+                      int dtype, void* stream);
+
+/* Its backward pass, from the gradients at x_out and h, x_out itself and y:
+ *   dx = dx_out + pre'(dh) is the gradient at x_out and at x;  dy, and the gradients of the vectors that are wanted ([cols], dtype).
+ *  dx_out: NULL stands for zeros (allowed with ZR_JOIN_PRE).  dh, x_out: needed with ZR_JOIN_PRE, else ignored.  y: needed with
+ *  ZR_JOIN_POST or dgate.  Outputs: each may be NULL, not all; dpost_* need ZR_JOIN_POST, dpre_* ZR_JOIN_PRE (else MODE).  dx may be dx_out, dh or
+ *  x_out, dy may be y (same pitch); dx and dy must not overlap.
+ *  The norms are taken again, of x_out as it was stored.  fp32 sums over the rows, in a fixed order: results repeat to the bit.
+ *  workspace: of zr_block_join_workspace_bytes(rows, cols) bytes, 16-byte aligned, where a vector's gradient is wanted (else NULL is allowed).
+ *  Launches: 1, +1 for the vectors.  Errors: as for the forward pass; SHAPE also for a workspace that is too small, NULL without one. */
+size_t zr_block_join_workspace_bytes(int32_t rows, int32_t cols);
+int zr_block_join_bwd(const void* dx_out, int64_t lddxo, const void* dh, int64_t lddh, const void* x_out, int64_t ldxo,
+                      const void* y, int64_t ldy, void* dx, int64_t lddx, void* dy, int64_t lddy,
+                      int32_t rows, int32_t cols, int norms, int norm, double eps, double p, const uint64_t* rng, double scale,
+                      const void* bias, const void* gate, const void* post_w, const void* post_b, const void* pre_w,
+                      void* dbias, void* dgate, void* dpost_w, void* dpost_b, void* dpre_w, void* dpre_b,
+                      void* workspace, size_t workspace_bytes, int dtype, void* stream);
+
 /* Weight-variation scores (Sec. 3.2 "Priority Pruning"; Algorithm 1):
  *   scores[i] = mean over the slice's elements of |W_t - W_prev|, for every index
  *   i of the pruned axis of W[K x N] (columns for ZR_DROP_N, rows for ZR_DROP_K;

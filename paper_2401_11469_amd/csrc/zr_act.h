@@ -1,0 +1,347 @@
+// What stands around the products of the layer: bias, activation, gate, dropout and residual, as device functions on
+// eight neighbouring columns of a row, and the launchers of the kernels that use them.
+//
+// Columns are taken in aligned groups of eight everywhere (columns 8 g .. 8 g + 7 of the whole row), because one call of the
+// generator gives the eight halves of a group: no element's draw depends on which kernel, tile or thread visits it.
+#pragma once
+
+#include "zr_common.h"
+
+namespace zr {
+
+// Applied to the result of a forward product before it is stored:
+//   z = sum + bias;  Z <- z;  out <- residual + D(act(z) * gate)
+struct Finish {
+    const void* bias;        // [N] or nullptr
+    const void* gate;        // [M x N] or nullptr
+    int64_t ldg;
+    const void* residual;    // [M x N] or nullptr
+    int64_t ldr;
+    void* Z;                 // [M x N] or nullptr
+    int64_t ldz;
+    const uint64_t* rng;     // seed, offset
+    uint32_t drop;           // an element is dropped where its half is below this; 0: none
+    float factor;            // what the others are multiplied by
+    int act;
+};
+
+// Probability to halves: round(65536 p), at most 65535, and the factor that keeps the mean.
+inline uint32_t drop_below(double p) { return (uint32_t)std::min(65535.0, std::floor(p * 65536.0 + 0.5)); }
+inline float kept_factor(uint32_t q) { return (float)(65536.0 / (65536.0 - (double)q)); }
+
+// ---- launchers ----------------------------------------------------------------
+// act_dz: what the backward pass of a Finish does to dY before the products, T = D(dY):
+//   dgate <- T act(Z);  dz <- T gate act'(Z);  partial[slab] <- column sums of dz over the slab's rows
+struct ActBack {
+    const void* dY; int64_t lddy;
+    const void* Z; int64_t ldz;            // nullptr: no activation and no gate gradient
+    const void* gate; int64_t ldg;
+    void* dgate; int64_t lddg;
+    void* dz; int64_t lddz;                // nullptr: not wanted
+    float* partial;                        // [slabs x N] or nullptr
+    const uint64_t* rng; uint32_t drop; float factor; int act;
+    int M, N;
+};
+int act_slabs(int M, int N);
+int launch_act_back(const ActBack& a, int dtype, hipStream_t stream);
+// out[v][c] = sum over slabs of partial[(v * slabs + slab) * n + c], in slab order, for `vectors` of them (out[v] nullptr: skipped)
+constexpr int MAX_SUMS = 6;
+struct SumOut { void* out[MAX_SUMS]; };
+int launch_sum_slabs(const float* partial, int slabs, int n, int vectors, const SumOut& out, int dtype, hipStream_t stream);
+int launch_dropout(const void* x, int64_t ldx, void* out, int64_t ldo, int rows, int cols, const uint64_t* rng, uint32_t drop,
+                   float factor, int dtype, hipStream_t stream);
+
+// A block's output joins the residual stream: t = D(y + bias), n = post(t), x_out = x + scale gate n, h = pre(x_out).
+struct Join {
+    const void* y; int64_t ldy;
+    const void* x; int64_t ldx;            // forward: the stream before; backward: behind the block (what h is the norm of)
+    void* x_out; int64_t ldxo;
+    void* h; int64_t ldh;
+    const void *bias, *gate, *post_w, *post_b, *pre_w, *pre_b;      // [cols] or nullptr
+    float scale, eps;
+    int post, pre, layer;                  // which norms there are; layer norms (else root mean square)
+    const uint64_t* rng; uint32_t drop; float factor;
+    int rows, cols;
+    // backward
+    const void* dx_out; int64_t lddxo;     // nullptr: zeros
+    const void* dh; int64_t lddh;
+    void* dx; int64_t lddx;
+    void* dy; int64_t lddy;
+    float* partial;                        // [vectors x slabs x cols]
+    int slabs;
+};
+int join_max_cols();
+int join_slabs(int rows, int cols);
+int launch_join(const Join& j, int dtype, hipStream_t stream);
+int launch_join_back(const Join& j, int dtype, hipStream_t stream);
+
+// products with a Finish (GemmDesc::finish set): any alignment, and fp32
+int launch_act_any(const GemmDesc& d, hipStream_t stream);
+int launch_act_f32(const GemmDesc& d, hipStream_t stream);
+
+// ---- device functions -----------------------------------------------------------
+namespace {
+
+typedef uint16_t Bf;
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u4_any __attribute__((ext_vector_type(4), aligned(2)));       // 16 bytes at any bf16 element
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef float f4_any __attribute__((ext_vector_type(4), aligned(4)));
+
+// round to nearest, ties to even (v_cvt_pk_bf16_f32)
+__device__ __forceinline__ uint32_t round_two(float a, float b)
+{
+    union { __bf16 h[2]; uint32_t u; } x;
+    x.h[0] = (__bf16)a;
+    x.h[1] = (__bf16)b;
+    return x.u;
+}
+
+__device__ __forceinline__ float one_of(const Bf* p) { return bf16_bits_to_f32(*p); }
+__device__ __forceinline__ float one_of(const float* p) { return *p; }
+__device__ __forceinline__ void put_one(Bf* p, float v) { *p = (Bf)round_two(v, 0.f); }
+__device__ __forceinline__ void put_one(float* p, float v) { *p = v; }
+
+// Eight values as they lie in memory, at any element address.
+template <typename T> struct Raw8;
+template <> struct Raw8<Bf> {
+    u4 v;
+    __device__ __forceinline__ void load(const Bf* p) { v = *(const u4_any*)p; }
+    __device__ __forceinline__ void values(float (&x)[8]) const
+    {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            x[2 * e] = __uint_as_float(v[e] << 16);
+            x[2 * e + 1] = __uint_as_float(v[e] & 0xffff0000u);
+        }
+    }
+    __device__ __forceinline__ void take(const float (&x)[8])
+    {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = round_two(x[2 * e], x[2 * e + 1]);
+    }
+    __device__ __forceinline__ void store(Bf* p) const { *(u4_any*)p = v; }
+    __device__ __forceinline__ void clear() { v = u4{0u, 0u, 0u, 0u}; }
+};
+template <> struct Raw8<float> {
+    f4 v[2];
+    __device__ __forceinline__ void load(const float* p) { v[0] = *(const f4_any*)p; v[1] = *(const f4_any*)(p + 4); }
+    __device__ __forceinline__ void values(float (&x)[8]) const
+    {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = v[e >> 2][e & 3];
+    }
+    __device__ __forceinline__ void take(const float (&x)[8])
+    {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e >> 2][e & 3] = x[e];
+    }
+    __device__ __forceinline__ void store(float* p) const { *(f4_any*)p = v[0]; *(f4_any*)(p + 4) = v[1]; }
+    __device__ __forceinline__ void clear() { v[0] = v[1] = f4{0.f, 0.f, 0.f, 0.f}; }
+};
+
+// Elements lo .. hi - 1 of the eight at p (the others: 0, and left as they are)
+template <typename T> __device__ __forceinline__ void load8(const T* p, int lo, int hi, float (&x)[8])
+{
+    if (lo == 0 && hi == 8) {
+        Raw8<T> r;
+        r.load(p);
+        r.values(x);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = e >= lo && e < hi ? one_of(p + e) : 0.f;
+    }
+}
+template <typename T> __device__ __forceinline__ void store8(T* p, int lo, int hi, const float (&x)[8])
+{
+    if (lo == 0 && hi == 8) {
+        Raw8<T> r;
+        r.take(x);
+        r.store(p);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e >= lo && e < hi) put_one(p + e, x[e]);
+    }
+}
+
+// Philox 4 x 32 of 7 rounds (Salmon, Moraes, Dror and Shaw, "Parallel random numbers: as easy as 1, 2, 3", 2011: the fewest that
+// passed all their tests), key = seed, counter = (group of eight columns, row, offset): eight halves for the group.
+// 14 products of 32 x 32 bits for eight elements, at a quarter of the rate of an addition.
+struct Draw {
+    uint32_t w[4];
+    __device__ __forceinline__ Draw(uint64_t seed, uint64_t offset, uint32_t row, uint32_t group)
+    {
+        uint32_t k0 = (uint32_t)seed, k1 = (uint32_t)(seed >> 32);
+        uint32_t c0 = group, c1 = row, c2 = (uint32_t)offset, c3 = (uint32_t)(offset >> 32);
+#pragma unroll
+        for (int i = 0; i < 7; ++i) {
+            const uint64_t a = (uint64_t)c0 * 0xD2511F53u, b = (uint64_t)c2 * 0xCD9E8D57u;
+            c0 = (uint32_t)(b >> 32) ^ c1 ^ k0;
+            c1 = (uint32_t)b;
+            c2 = (uint32_t)(a >> 32) ^ c3 ^ k1;
+            c3 = (uint32_t)a;
+            k0 += 0x9E3779B9u;
+            k1 += 0xBB67AE85u;
+        }
+        w[0] = c0; w[1] = c1; w[2] = c2; w[3] = c3;
+    }
+    __device__ __forceinline__ bool kept(int e, uint32_t drop) const
+    {
+        return (e & 1 ? w[e >> 1] >> 16 : w[e >> 1] & 0xffffu) >= drop;
+    }
+    // a dropped element is +0 whatever it was
+    __device__ __forceinline__ void apply(float (&x)[8], uint32_t drop, float factor) const
+    {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = kept(e, drop) ? x[e] * factor : 0.f;
+    }
+};
+
+// e^x: bf16 results take the hardware's power of two (off by about |x| 2^-24 in all), fp32 ones the library's
+template <bool EXACT> __device__ __forceinline__ float exp_of(float x)
+{
+    if constexpr (EXACT) return expf(x);
+    else return __builtin_amdgcn_exp2f(x * 1.44269504f);
+}
+template <bool EXACT> __device__ __forceinline__ float recip(float x)
+{
+    if constexpr (EXACT) return 1.f / x;
+    else return __builtin_amdgcn_rcpf(x);
+}
+template <bool EXACT> __device__ __forceinline__ float sigmoid_of(float x) { return recip<EXACT>(1.f + exp_of<EXACT>(-x)); }
+
+// The normal distribution function at z, and its density.  bf16 results: half of erfc by formula 7.1.26 of Abramowitz and Stegun
+// (a polynomial of fifth degree in 1 / (1 + 0.3275911 x), times e^(-x^2)), off by 7.5e-8 at most, where a bf16 result is off by
+// 2^-9 of itself; it decays as it should, so that small results keep their size.  fp32 results: the library's erfc.
+template <bool EXACT> __device__ __forceinline__ float normal_cdf(float z, float& density)
+{
+    const float e = exp_of<EXACT>(-0.5f * z * z);
+    density = 0.39894228f * e;
+    if constexpr (EXACT) return 0.5f * erfcf(-0.70710678f * z);
+    const float t = recip<EXACT>(fmaf(0.3275911f * 0.70710678f, fabsf(z), 1.f));
+    float s = 1.061405429f;
+    s = fmaf(s, t, -1.453152027f);
+    s = fmaf(s, t, 1.421413741f);
+    s = fmaf(s, t, -0.284496736f);
+    s = fmaf(s, t, 0.254829592f);
+    const float tail = 0.5f * s * t * e;
+    return z > 0.f ? 1.f - tail : tail;
+}
+
+// a = act(z), s = act'(z) (SLOPE)
+template <bool EXACT, bool SLOPE> __device__ __forceinline__ void act_one(int act, float z, float& a, float& s)
+{
+    if (act == ZR_ACT_RELU) {
+        a = z < 0.f ? 0.f : z;          // (NaN stays NaN)
+        s = z > 0.f ? 1.f : 0.f;
+    } else if (act == ZR_ACT_GELU) {
+        float density;
+        const float cdf = normal_cdf<EXACT>(z, density);
+        a = z * cdf;
+        if constexpr (SLOPE) s = fmaf(z, density, cdf);
+    } else if (act == ZR_ACT_GELU_TANH) {
+        // (1 + tanh u) / 2 is the sigmoid of 2 u, u = sqrt(2 / pi) (z + 0.044715 z^3)
+        const float zz = z * z, t = sigmoid_of<EXACT>(1.59576912f * z * fmaf(0.044715f, zz, 1.f));
+        a = z * t;
+        if constexpr (SLOPE) s = fmaf(z * t * (1.f - t), 1.59576912f * fmaf(0.134145f, zz, 1.f), t);
+    } else if (act == ZR_ACT_SILU) {
+        const float t = sigmoid_of<EXACT>(z);
+        a = z * t;
+        if constexpr (SLOPE) s = t * fmaf(z, 1.f - t, 1.f);
+    } else {
+        a = z;
+        s = 1.f;
+    }
+}
+// (the choice outside the loop: one uniform branch for eight elements)
+template <bool EXACT, bool SLOPE> __device__ __forceinline__ void act8(int act, const float (&z)[8], float (&a)[8], float (&s)[8])
+{
+    auto all = [&](int which) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) act_one<EXACT, SLOPE>(which, z[e], a[e], s[e]);
+    };
+    switch (act) {
+        case ZR_ACT_RELU: all(ZR_ACT_RELU); break;
+        case ZR_ACT_GELU: all(ZR_ACT_GELU); break;
+        case ZR_ACT_GELU_TANH: all(ZR_ACT_GELU_TANH); break;
+        case ZR_ACT_SILU: all(ZR_ACT_SILU); break;
+        default: all(ZR_ACT_NONE); break;
+    }
+}
+
+// Columns col + lo .. col + hi - 1 (col a multiple of 8) of one row of a product: z holds the sums.
+template <typename T>
+__device__ __forceinline__ void finish8(const Finish& f, T* out, int64_t ldo, int row, int col, int lo, int hi, float (&z)[8])
+{
+    constexpr bool EXACT = sizeof(T) == 4;
+    float x[8], a[8], unused[8];
+    if (f.bias) {
+        load8((const T*)f.bias + col, lo, hi, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) z[e] += x[e];
+    }
+    if (f.Z) store8((T*)f.Z + (size_t)row * (size_t)f.ldz + col, lo, hi, z);
+    act8<EXACT, false>(f.act, z, a, unused);
+    if (f.gate) {
+        load8((const T*)f.gate + (size_t)row * (size_t)f.ldg + col, lo, hi, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) a[e] *= x[e];
+    }
+    if (f.drop) Draw(f.rng[0], f.rng[1], (uint32_t)row, (uint32_t)col >> 3).apply(a, f.drop, f.factor);
+    if (f.residual) {
+        load8((const T*)f.residual + (size_t)row * (size_t)f.ldr + col, lo, hi, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) a[e] += x[e];
+    }
+    store8(out + (size_t)row * (size_t)ldo + col, lo, hi, a);
+}
+
+// Rows row0 .. row0 + rows - 1 of a tile whose sums lie in LDS (Cs, pitch CP floats), NT threads.
+// sidx == nullptr: the tile's columns are col0 .. col0 + cols - 1 (col0 a multiple of 8).  Otherwise sidx[j] is the original
+// column of the tile's column j, ascending, and the tile owns the original columns start .. end - 1: those without an entry have
+// the sum 0.  tab: TAB words of LDS.  Every thread of the workgroup calls it; LDS is free again after a barrier.
+template <int NT, int TAB, typename T>
+__device__ __forceinline__ void finish_tile(const Finish& f, T* out, int64_t ldo, const float* Cs, int CP, int row0, int rows, int col0,
+                                            int cols, const int* sidx, int start, int end, int* tab, int tid)
+{
+    static_assert(TAB % 8 == 0, "whole groups");
+    if (!sidx) {
+        const int groups = (cols + 7) >> 3;
+        for (int u = tid; u < rows * groups; u += NT) {
+            const int r = u / groups, j = 8 * (u - r * groups);
+            float z[8];
+            const float* c = Cs + r * CP + j;
+            const f4 z0 = *(const f4*)c, z1 = *(const f4*)(c + 4);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) z[e] = e < 4 ? z0[e & 3] : z1[e & 3];
+            finish8(f, out, ldo, row0 + r, col0 + j, 0, min(8, cols - j), z);
+        }
+        return;
+    }
+    for (int base = start & ~7; base < end; base += TAB) {
+        const int width = min(TAB, ((end + 7) & ~7) - base), groups = width >> 3;
+        for (int q = tid; q < TAB; q += NT) tab[q] = -1;
+        __syncthreads();
+        for (int q = tid; q < cols; q += NT) {
+            const int p = sidx[q] - base;
+            if (p >= 0 && p < width) tab[p] = q;
+        }
+        __syncthreads();
+        for (int u = tid; u < rows * groups; u += NT) {
+            const int r = u / groups, p = 8 * (u - r * groups), col = base + p;
+            float z[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int j = tab[p + e];
+                z[e] = j >= 0 ? Cs[r * CP + j] : 0.f;
+            }
+            finish8(f, out, ldo, row0 + r, col, max(start - col, 0), min(end - col, 8), z);
+        }
+        __syncthreads();
+    }
+}
+
+}  // namespace
+
+}  // namespace zr

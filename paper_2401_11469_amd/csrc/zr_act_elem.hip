@@ -1,0 +1,167 @@
+// Passes over [tokens x features] around the products (gfx950): dropout, what the backward pass of a product with an activation
+// does to dY before the products, and the sums over tokens that belong to both it and the norms.  HBM bound.
+#include "zr_act.h"
+
+namespace zr {
+
+namespace {
+
+// Threads of a workgroup over groups of eight columns and rows: `across` (a power of two) neighbours along a row.
+inline int lanes_across(int cols)
+{
+    int w = 1;
+    while (w < 64 && w * 8 < cols) w *= 2;
+    return w;
+}
+
+// ---------------------------------------------------------------------------
+// Dropout: out = D(x).  One read, one write, one draw for eight elements.
+// ---------------------------------------------------------------------------
+template <typename T>
+__global__ __launch_bounds__(256) void dropout_kernel(const T* x, int64_t ldx, T* out, int64_t ldo, int rows, int cols,
+                                                      const uint64_t* rng, uint32_t drop, float factor, int across, int rows_each)
+{
+    const int lane = threadIdx.x & (across - 1), sub = threadIdx.x / across, down = 256 / across;
+    const int group = (int)blockIdx.x * across + lane, col = 8 * group;
+    if (col >= cols) return;
+    const uint64_t seed = rng[0], offset = rng[1];
+    const int hi = min(8, cols - col);
+    const int64_t first = (int64_t)blockIdx.y * rows_each, last = min((int64_t)rows, first + rows_each);
+    for (int64_t r = first + sub; r < last; r += down) {
+        float v[8];
+        load8(x + r * ldx + col, 0, hi, v);
+        Draw(seed, offset, (uint32_t)r, (uint32_t)group).apply(v, drop, factor);
+        store8(out + r * ldo + col, 0, hi, v);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// dZ = D(dY) gate act'(Z), dgate = D(dY) act(Z), and the column sums of dZ
+// ---------------------------------------------------------------------------
+template <typename T>
+__global__ __launch_bounds__(256) void act_back_kernel(const ActBack a, int across, int rows_each)
+{
+    __shared__ float sums[256 * 8];
+    constexpr bool EXACT = sizeof(T) == 4;
+    const int lane = threadIdx.x & (across - 1), sub = threadIdx.x / across, down = 256 / across;
+    const int group = (int)blockIdx.x * across + lane, col = 8 * group;
+    const int hi = min(8, a.N - col);
+    const int64_t first = (int64_t)blockIdx.y * rows_each, last = min((int64_t)a.M, first + rows_each);
+    uint64_t seed = 0, offset = 0;
+    if (a.drop) { seed = a.rng[0]; offset = a.rng[1]; }
+    float total[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) total[e] = 0.f;
+    for (int64_t r = first + sub; r < last && hi > 0; r += down) {
+        float t[8], z[8], v[8], s[8], g[8];
+        load8((const T*)a.dY + r * a.lddy + col, 0, hi, t);
+        if (a.drop) Draw(seed, offset, (uint32_t)r, (uint32_t)group).apply(t, a.drop, a.factor);
+        if (a.Z) {
+            load8((const T*)a.Z + r * a.ldz + col, 0, hi, z);
+            act8<EXACT, true>(a.act, z, v, s);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) { v[e] = 0.f; s[e] = 1.f; }
+        }
+        if (a.gate) {
+            load8((const T*)a.gate + r * a.ldg + col, 0, hi, g);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s[e] *= g[e];
+        }
+        if (a.dgate) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] *= t[e];
+            store8((T*)a.dgate + r * a.lddg + col, 0, hi, v);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            t[e] *= s[e];
+            total[e] += t[e];
+        }
+        if (a.dz) store8((T*)a.dz + r * a.lddz + col, 0, hi, t);
+    }
+    if (!a.partial) return;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sums[(sub * across + lane) * 8 + e] = total[e];
+    __syncthreads();
+    float* dst = a.partial + (size_t)blockIdx.y * (size_t)a.N;
+    for (int q = threadIdx.x; q < across * 8; q += 256) {
+        const int c = (int)blockIdx.x * across * 8 + q;
+        if (c >= a.N) continue;
+        float v = 0.f;
+        for (int i = 0; i < down; ++i) v += sums[i * across * 8 + q];
+        dst[c] = v;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Sums over slabs: 64 columns to a workgroup, four wavefronts along the slabs, added in a fixed order
+// ---------------------------------------------------------------------------
+template <typename T>
+__global__ __launch_bounds__(256) void sum_slabs_kernel(const float* partial, int slabs, int n, const SumOut out)
+{
+    __shared__ float part[4][64];
+    void* dst = out.out[0];
+#pragma unroll
+    for (int v = 1; v < MAX_SUMS; ++v) dst = (int)blockIdx.y == v ? out.out[v] : dst;
+    if (!dst) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = (int)blockIdx.x * 64 + lane;
+    const float* p = partial + (size_t)blockIdx.y * (size_t)slabs * (size_t)n;
+    float v = 0.f;
+    if (c < n)
+        for (int s = wave; s < slabs; s += 4) v += p[(size_t)s * (size_t)n + c];
+    part[wave][lane] = v;
+    __syncthreads();
+    if (wave == 0 && c < n) put_one((T*)dst + c, (part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane]));
+}
+
+}  // namespace
+
+int launch_dropout(const void* x, int64_t ldx, void* out, int64_t ldo, int rows, int cols, const uint64_t* rng, uint32_t drop,
+                   float factor, int dtype, hipStream_t stream)
+{
+    const int across = lanes_across(cols), down = 256 / across;
+    const int wide = (cols + 8 * across - 1) / (8 * across);
+    // 2048 workgroups and more where there is work for them, at least one row a thread
+    const int64_t most = std::max<int64_t>(1, 4096 / wide);
+    const int rows_each = (int)std::max<int64_t>(down, (rows + most - 1) / most);
+    const dim3 grid((unsigned)wide, (unsigned)((rows + (int64_t)rows_each - 1) / rows_each));
+    if (dtype == ZR_BF16)
+        hipLaunchKernelGGL(dropout_kernel<Bf>, grid, dim3(256), 0, stream, (const Bf*)x, ldx, (Bf*)out, ldo, rows, cols, rng, drop, factor, across, rows_each);
+    else
+        hipLaunchKernelGGL(dropout_kernel<float>, grid, dim3(256), 0, stream, (const float*)x, ldx, (float*)out, ldo, rows, cols, rng, drop, factor, across, rows_each);
+    return hip_status(hipGetLastError());
+}
+
+// rows that a workgroup of act_back_kernel takes
+static int back_rows_each(int M, int N)
+{
+    const int across = lanes_across(N), down = 256 / across;
+    const int wide = (N + 8 * across - 1) / (8 * across);
+    const int most = std::max(1, std::min(256, 2048 / wide));
+    return std::max(down, (M + most - 1) / most);
+}
+int act_slabs(int M, int N)
+{
+    const int each = back_rows_each(M, N);
+    return (int)(((int64_t)M + each - 1) / each);
+}
+
+int launch_act_back(const ActBack& a, int dtype, hipStream_t stream)
+{
+    const int across = lanes_across(a.N);
+    const dim3 grid((unsigned)((a.N + 8 * across - 1) / (8 * across)), (unsigned)act_slabs(a.M, a.N));
+    if (dtype == ZR_BF16) hipLaunchKernelGGL(act_back_kernel<Bf>, grid, dim3(256), 0, stream, a, across, back_rows_each(a.M, a.N));
+    else hipLaunchKernelGGL(act_back_kernel<float>, grid, dim3(256), 0, stream, a, across, back_rows_each(a.M, a.N));
+    return hip_status(hipGetLastError());
+}
+
+int launch_sum_slabs(const float* partial, int slabs, int n, int vectors, const SumOut& out, int dtype, hipStream_t stream)
+{
+    const dim3 grid((unsigned)((n + 63) / 64), (unsigned)vectors);
+    if (dtype == ZR_BF16) hipLaunchKernelGGL(sum_slabs_kernel<Bf>, grid, dim3(256), 0, stream, partial, slabs, n, out);
+    else hipLaunchKernelGGL(sum_slabs_kernel<float>, grid, dim3(256), 0, stream, partial, slabs, n, out);
+    return hip_status(hipGetLastError());
+}
+
+}  // namespace zr

@@ -276,14 +276,26 @@ int zr_resized_linear_fwd(const void* X, int64_t ldx, const void* W, int64_t ldw
                           void* workspace, size_t workspace_bytes, void* stream)
 {
     if (!X || !W || !Y) return ZR_ERR_NULL;
-    int st = check_common(M, K, N, keep_idx, n_keep, mode, dtype, policy);
+    const int st = check_common(M, K, N, keep_idx, n_keep, mode, dtype, policy);
     if (st != ZR_OK) return st;
     if (w_layout != ZR_W_KN && w_layout != ZR_W_NK) return ZR_ERR_MODE;
     if (ldx < K || ldw < (w_layout == ZR_W_KN ? N : K) || ldy < N) return ZR_ERR_SHAPE;
+    return resized_linear_fwd(X, ldx, W, ldw, Y, ldy, M, K, N, keep_idx, n_keep, mode, w_layout, dtype, policy, prev_Y, nullptr,
+                              workspace, workspace_bytes, (hipStream_t)stream);
+}
+
+}  // extern "C"
+
+namespace zr {
+
+int resized_linear_fwd(const void* X, int64_t ldx, const void* W, int64_t ldw, void* Y, int64_t ldy, int32_t M, int32_t K, int32_t N,
+                       const int32_t* keep_idx, int32_t n_keep, int mode, int w_layout, int dtype, int policy, const void* prev_Y,
+                       const Finish* finish, void* workspace, size_t workspace_bytes, hipStream_t s)
+{
     const bool full = n_keep == (mode == ZR_DROP_N ? N : K);   // ascending + unique + full count = identity
     const bool needs_prev = mode == ZR_DROP_N && policy == ZR_IMPUTE_SAME && !full;
     if (needs_prev && !prev_Y) return ZR_ERR_POLICY;
-    hipStream_t s = (hipStream_t)stream;
+    int st;
     const int32_t* S = full ? nullptr : keep_idx;
     const bool average = mode == ZR_DROP_N && policy == ZR_IMPUTE_AVERAGE && !full;
     // (fp32 products leave no sums: their means come from the stand-alone pass)
@@ -291,6 +303,7 @@ int zr_resized_linear_fwd(const void* X, int64_t ldx, const void* W, int64_t ldw
 
     GemmDesc d;
     d.dtype = dtype;
+    d.finish = finish;
     d.out = Y; d.ldo = ldy; d.keep_idx = S; d.I = M;
     d.B = weight_fwd(W, ldw, K, N, mode, w_layout, S);
     if (mode == ZR_DROP_K) {
@@ -316,10 +329,6 @@ int zr_resized_linear_fwd(const void* X, int64_t ldx, const void* W, int64_t ldw
     if (average) return gemm_with_average(d, sums, Y, ldy, M, N, 1, keep_idx, n_keep, dtype, s);
     return launch_gemm(d, s);
 }
-
-}  // extern "C"
-
-namespace zr {
 
 int check_linear_bwd(const void* X, int64_t ldx, const void* W, int64_t ldw, const void* dY, int64_t lddy,
                      const void* dX, int64_t lddx, const void* dW, int64_t lddw, int32_t M, int32_t K, int32_t N,

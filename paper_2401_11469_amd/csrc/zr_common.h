@@ -89,6 +89,8 @@ struct Operand {
     bool zero_padded;
 };
 
+struct Finish;      // zr_act.h
+
 enum Epilogue { EPI_PLAIN = 0, EPI_COL_SCATTER = 1, EPI_ROW_SCATTER = 2 };
 
 struct GemmDesc {
@@ -123,6 +125,9 @@ struct GemmDesc {
     const GemmDesc* with = nullptr;
     // with `with`: nothing is computed, and launch_gemm returns -1, if one launch is not expected to be the shorter way
     bool only_together = false;
+    // bias, activation, gate, dropout and residual on the way out (plain epilogue and column scatter, whose other columns get what
+    // these make of a sum of 0); no prev, no accumulate, no sums
+    const Finish* finish = nullptr;
 };
 
 // State of the aids in zr_debug.h, per host thread.  Product calls only test `armed`.
@@ -242,6 +247,10 @@ inline double two_groups(int n1, double t1, int n2, double t2, int slots)
     return std::max(T, hi);
 }
 
+// the product of zr_resized_linear_fwd after its checks (keep_idx is not read where n_keep is the whole axis)
+int resized_linear_fwd(const void* X, int64_t ldx, const void* W, int64_t ldw, void* Y, int64_t ldy, int32_t M, int32_t K, int32_t N,
+                       const int32_t* keep_idx, int32_t n_keep, int mode, int w_layout, int dtype, int policy, const void* prev_Y,
+                       const Finish* finish, void* workspace, size_t workspace_bytes, hipStream_t stream);
 // zr_resized_linear_bwd on arguments of its own kind; x_kept (DROP_K): X holds the kept columns side by side, [M x ldx] with
 // zeros behind the last, ldx a multiple of 64.
 int resized_linear_bwd(const void* X, int64_t ldx, const void* W, int64_t ldw, const void* dY, int64_t lddy,

@@ -37,6 +37,7 @@
 #include <cstdio>
 #include <type_traits>
 
+#include "zr_act.h"
 #include "zr_common.h"
 
 namespace zr {
@@ -76,6 +77,9 @@ struct Args {
     int tiles_i, tiles_j;
     const float* prev;          // Same imputation source (layout of out) or nullptr
     int accumulate;             // add the old contents of out (plain epilogue)
+};
+struct FinishArgs : Args {
+    Finish f;
 };
 
 // ---------------------------------------------------------------------------
@@ -349,9 +353,9 @@ __device__ __forceinline__ f4 fragment(const float* lds, int row, int block, int
     return x;
 }
 
-// One workgroup's tile `lin` of a product.
-template <template <int> class LA_, template <int> class LB_, int R>
-__device__ __forceinline__ void f32_body(const Args& g, float* smem, const int lin)
+// One workgroup's tile `lin` of a product (FinishArgs: with bias, activation and so on before the results are stored).
+template <template <int> class LA_, template <int> class LB_, int R, class G = Args>
+__device__ __forceinline__ void f32_body(const G& g, float* smem, const int lin)
 {
     typedef LA_<R> LA;
     typedef LB_<R> LB;
@@ -498,6 +502,12 @@ __device__ __forceinline__ void f32_body(const Args& g, float* smem, const int l
     if (scatter_r && tid < rows_valid) sidx[tid] = clamp_idx(g.keep[i0 + tid], g.out_full);
     __syncthreads();
 
+    if constexpr (std::is_same_v<G, FinishArgs>) {
+        const int start = !scatter_c || j0 == 0 ? 0 : sidx[0];
+        const int end = !scatter_c ? 0 : j0 + R >= g.J ? g.out_full : clamp_idx(g.keep[j0 + R], g.out_full);
+        finish_tile<NT, TAB>(g.f, g.out, g.ldo, Cs, CP, i0, rows_valid, j0, cols_valid, scatter_c ? sidx : nullptr, start, end, sidx + 2 * R, tid);
+        return;
+    }
     if (scatter_c) {
         // The tile owns the original columns from its first kept column (0 for the first tile) up to
         // the next tile's first kept column (the full width for the last tile).  A table says which
@@ -646,6 +656,13 @@ __global__ __launch_bounds__(NT) void f32_kernel(const Args g)
     f32_body<LA, LB, R>(g, smem, (int)((blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8));
 }
 
+template <template <int> class LA, template <int> class LB, int R>
+__global__ __launch_bounds__(NT) void f32_act_kernel(const FinishArgs g)
+{
+    extern __shared__ __align__(16) float smem[];
+    f32_body<LA, LB, R>(g, smem, (int)((blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8));
+}
+
 // dX and dW of one backward call: the first per_w workgroups of every XCD are dW's, or with x_first the last ones.
 template <template <int> class XA, template <int> class XB, int XR, template <int> class WA, template <int> class WB, int WR>
 __global__ __launch_bounds__(NT) void f32_pair_kernel(const Args gx, const Args gw, const int per_x, const int per_w, const int x_first)
@@ -657,16 +674,17 @@ __global__ __launch_bounds__(NT) void f32_pair_kernel(const Args gx, const Args 
     else f32_body<XA, XB, XR>(gx, smem, xcd * per_x + qx);
 }
 
-template <template <int> class LA, template <int> class LB, int R>
-int launch_inst(const Args& a, hipStream_t stream)
+template <template <int> class LA, template <int> class LB, int R, class G>
+int launch_inst(const G& a, hipStream_t stream)
 {
     constexpr int smem = 2 * 2 * Geo<R>::WORDS * 4;
-    auto fn = f32_kernel<LA, LB, R>;
+    constexpr bool finishes = std::is_same_v<G, FinishArgs>;
+    const auto fn = [] { if constexpr (finishes) return f32_act_kernel<LA, LB, R>; else return f32_kernel<LA, LB, R>; }();
     static AttrFlags attr_set;      // per instantiation and device
     if (!ensure_max_dynamic_lds((const void*)fn, smem, &attr_set)) return ZR_ERR_HIP;
     if (debug_names_wanted())
-        snprintf(g_debug.last_kernel, sizeof(g_debug.last_kernel), "f32_kernel<%s, %s, %d>", LA<R>::NAME, LB<R>::NAME, R);
-    Args k = a;
+        snprintf(g_debug.last_kernel, sizeof(g_debug.last_kernel), "f32_%skernel<%s, %s, %d>", finishes ? "act_" : "", LA<R>::NAME, LB<R>::NAME, R);
+    G k = a;
     k.tiles_i = (a.I + R - 1) / R;
     k.tiles_j = (a.J + R - 1) / R;
     const int64_t tiles = (int64_t)k.tiles_i * k.tiles_j;
@@ -692,8 +710,8 @@ int tile_of(const Args& a)
     return t64 < 192 ? 32 : 64;
 }
 
-template <template <int> class LA, template <int> class LB>
-int launch_shape(const Args& a, hipStream_t stream)
+template <template <int> class LA, template <int> class LB, class G>
+int launch_shape(const G& a, hipStream_t stream)
 {
     switch (tile_of(a)) {
         case 128: return launch_inst<LA, LB, 128>(a, stream);
@@ -704,8 +722,8 @@ int launch_shape(const Args& a, hipStream_t stream)
 
 // The element loaders: a contraction of less than four is one stage of any tile shape; otherwise the
 // result has less than four rows or columns, and the narrowest tiles waste least.
-template <template <int> class LA, template <int> class LB>
-int launch_short(const Args& a, hipStream_t stream)
+template <template <int> class LA, template <int> class LB, class G>
+int launch_short(const G& a, hipStream_t stream)
 {
     return a.C < 4 ? launch_shape<LA, LB>(a, stream) : launch_inst<LA, LB, 32>(a, stream);
 }
@@ -841,6 +859,23 @@ int launch_gemm_f32_pair(const GemmDesc& dx, const GemmDesc& dw, hipStream_t str
     if (!xa && xb && !wa && wb) return launch_pair<PlainP, GatherQ, PlainQ, GatherQ>(x, w, p, stream);
     if (!xa && !xb && !wa && !wb) return launch_pair<PlainP, PlainQ, PlainQ, PlainQ>(x, w, p, stream);
     return -1;
+}
+
+int launch_act_f32(const GemmDesc& d, hipStream_t stream)
+{
+    if (d.I < 1 || d.J < 1 || d.C < 1) return ZR_ERR_SHAPE;
+    FinishArgs a;
+    (Args&)a = args_of(d);
+    a.f = *d.finish;
+    const bool ag = d.A.map_contig != nullptr, bg = d.B.map_contig != nullptr;
+    if (!d.A.c_contig) return ZR_ERR_MODE;
+    if (too_short(d, d.A) || too_short(d, d.B)) return d.B.c_contig ? launch_short<AnyP, AnyP>(a, stream) : launch_short<AnyP, AnyQ>(a, stream);
+    if (!d.B.c_contig) {            // weight stored [K x N]
+        if (ag) return bg ? ZR_ERR_MODE : launch_shape<GatherP, PlainQ>(a, stream);
+        return bg ? launch_shape<PlainP, GatherQ>(a, stream) : launch_shape<PlainP, PlainQ>(a, stream);
+    }
+    if (ag != bg) return ZR_ERR_MODE;
+    return ag ? launch_shape<GatherP, GatherP>(a, stream) : launch_shape<PlainP, PlainP>(a, stream);
 }
 
 int launch_gemm_f32(const GemmDesc& d, hipStream_t stream)

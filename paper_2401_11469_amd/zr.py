@@ -19,6 +19,8 @@ WS_FRESH, WS_HOLDS_FORWARD = 0, 1
 ZERO, AVERAGE, SAME = 0, 1, 2
 F32, BF16 = 0, 1
 MX_E4M3, MX_E2M1, MX_INT8 = 0, 1, 2
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = 0, 1, 2, 3, 4
+NORM_RMS, NORM_LAYER = 0, 1
 
 _LIB_PATH = os.environ.get("ZR_LIBZR_PATH") or os.path.join(os.path.dirname(os.path.abspath(__file__)), "libzr.so")
 if not os.path.exists(_LIB_PATH):
@@ -103,6 +105,26 @@ _lib.zr_resized_linear_bwd_mx.argtypes = [_vp, _i64, _vp, _i64, ctypes.c_int, _v
                                           _i32, _i32, _i32, _vp, _i32, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int,
                                           _vp, _vp, _vp, ctypes.c_size_t, _vp]
 _lib.zr_resized_linear_bwd_mx.restype = ctypes.c_int
+_int, _size = ctypes.c_int, ctypes.c_size_t
+_lib.zr_dropout.argtypes = [_vp, _i64, _vp, _i64, _i32, _i32, _f64, _vp, _int, _vp]
+_lib.zr_dropout.restype = _int
+for _f in (_lib.zr_act_fwd_workspace_bytes, _lib.zr_act_bwd_workspace_bytes):
+    _f.argtypes = [_i32, _i32, _i32, _i32, _int, _int]
+    _f.restype = _size
+_lib.zr_resized_linear_act_fwd.argtypes = [_vp, _i64, _vp, _i64, _vp, _i64, _i32, _i32, _i32, _vp, _i32, _int, _int, _int,
+                                           _vp, _int, _vp, _i64, _f64, _vp, _vp, _i64, _vp, _i64, _vp, _size, _vp]
+_lib.zr_resized_linear_act_fwd.restype = _int
+_lib.zr_resized_linear_act_bwd.argtypes = [_vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _i64,
+                                           _i32, _i32, _i32, _vp, _i32, _int, _int, _int, _int, _f64, _vp, _vp, _size, _vp]
+_lib.zr_resized_linear_act_bwd.restype = _int
+_lib.zr_block_join_workspace_bytes.argtypes = [_i32, _i32]
+_lib.zr_block_join_workspace_bytes.restype = _size
+_lib.zr_block_join_fwd.argtypes = [_vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _i32, _i32, _int, _int, _f64, _f64, _vp, _f64,
+                                   _vp, _vp, _vp, _vp, _vp, _vp, _int, _vp]
+_lib.zr_block_join_fwd.restype = _int
+_lib.zr_block_join_bwd.argtypes = [_vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _i32, _i32, _int, _int, _f64, _f64, _vp, _f64,
+                                   _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _size, _int, _vp]
+_lib.zr_block_join_bwd.restype = _int
 
 
 class ZrError(RuntimeError):
@@ -566,6 +588,218 @@ def resized_linear_bwd_mx(X: Optional[MX], W: torch.Tensor, dY: torch.Tensor, ke
     if st:
         raise ZrError(st)
     return dX, dW
+
+
+# ---- around the products of a block: bias, activation, gate, dropout, residual, norms ----
+def _vec(t: Optional[torch.Tensor], n: int, dt, here: int, name: str):
+    """Pointer of a vector of n values of dtype dt, None: None."""
+    if t is None:
+        return None
+    if t.dtype is not dt or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous() or t.get_device() != here:
+        raise ValueError(f"{name}: need a contiguous vector of {n} {dt} on the current GPU")
+    return t.data_ptr()
+
+
+def _like(t: Optional[torch.Tensor], shape, dt, here: int, name: str):
+    """(pointer, leading dimension) of a matrix of this shape and dtype, None: (None, 0)."""
+    if t is None:
+        return None, 0
+    if t.shape != shape or t.dtype is not dt:
+        raise ValueError(f"{name}: need {tuple(shape)} of {dt}")
+    return _grid(t, here, name)
+
+
+def _generator(rng: Optional[torch.Tensor], here: int):
+    """Pointer to seed and offset: two 64-bit integers in GPU memory."""
+    if rng is None:
+        return None
+    if rng.dtype not in (torch.int64, torch.uint64) or rng.numel() != 2 or not rng.is_contiguous() or rng.get_device() != here:
+        raise ValueError("rng: need two contiguous 64-bit integers, seed and offset, on the current GPU")
+    return rng.data_ptr()
+
+
+def _scratch(workspace: Optional[torch.Tensor], here: int):
+    if workspace is None:
+        return None, 0
+    if workspace.get_device() != here:
+        raise ValueError("workspace: must be on the current GPU")
+    return _ws(workspace)
+
+
+def dropout(x: torch.Tensor, p: float, rng: Optional[torch.Tensor], out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """x with elements dropped with probability p and the others scaled up; the same call on a gradient is the backward pass.
+    rng: seed and offset in GPU memory (zr.h says which draw an element looks at)."""
+    here = _here()
+    on = _on(stream, here)
+    xp, ldx = _grid(x, here, "x")
+    if out is None:
+        out = _empty(x.shape, x.dtype, x.device, stream)
+    op, ldo = _like(out, x.shape, x.dtype, here, "out")
+    st = _lib.zr_dropout(xp, ldx, op, ldo, x.shape[0], x.shape[1], p, _generator(rng, here), _code(x.dtype), on)
+    if st:
+        raise ZrError(st)
+    return out
+
+
+def act_workspace_bytes(M: int, K: int, N: int, n_keep: int, mode: int, dtype, backward: bool = False) -> int:
+    f = _lib.zr_act_bwd_workspace_bytes if backward else _lib.zr_act_fwd_workspace_bytes
+    return int(f(M, K, N, n_keep, mode, dtype if isinstance(dtype, int) else _code(dtype)))
+
+
+def _layer(X_shape, W: torch.Tensor, N: int, dt, w_layout: int):
+    K = W.shape[0] if w_layout == W_KN else W.shape[1]
+    if W.shape != ((K, N) if w_layout == W_KN else (N, K)) or W.dtype is not dt or (X_shape is not None and X_shape[1] != K):
+        raise ValueError("need X [M, K], W [K, N] (W_KN) or [N, K] (W_NK), all of one dtype")
+    return K
+
+
+def resized_linear_act_fwd(X: torch.Tensor, W: torch.Tensor, keep_idx: Optional[torch.Tensor] = None, mode: int = DROP_K,
+                           bias: Optional[torch.Tensor] = None, act: int = ACT_NONE, gate: Optional[torch.Tensor] = None, p: float = 0.0,
+                           rng: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None, Y: Optional[torch.Tensor] = None,
+                           Z: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None,
+                           w_layout: int = W_KN) -> torch.Tensor:
+    """Y = residual + dropout(act(X W + bias) * gate), with the kept list of resized_linear_fwd (None: nothing is pruned).
+    Z, where given, receives X W + bias for the backward pass.  workspace: optional, of act_workspace_bytes bytes."""
+    here = _here()
+    on = _on(stream, here)
+    xp, ldx = _grid(X, here, "X")
+    wp, ldw = _grid(W, here, "W")
+    M, dt = X.shape[0], X.dtype
+    N = W.shape[1] if w_layout == W_KN else W.shape[0]
+    K = _layer(X.shape, W, N, dt, w_layout)
+    kp, nk = _list(keep_idx, here)
+    if Y is None:
+        Y = _empty((M, N), dt, X.device, stream)
+    yp, ldy = _like(Y, (M, N), dt, here, "Y")
+    zp, ldz = _like(Z, (M, N), dt, here, "Z")
+    gp, ldg = _like(gate, (M, N), dt, here, "gate")
+    rp, ldr = _like(residual, (M, N), dt, here, "residual")
+    st = _lib.zr_resized_linear_act_fwd(xp, ldx, wp, ldw, yp, ldy, M, K, N, kp, nk, mode, w_layout, _code(dt),
+                                        _vec(bias, N, dt, here, "bias"), act, gp, ldg, p, _generator(rng, here), rp, ldr, zp, ldz,
+                                        *_scratch(workspace, here), on)
+    if st:
+        raise ZrError(st)
+    return Y
+
+
+def resized_linear_act_bwd(X: Optional[torch.Tensor], W: torch.Tensor, dY: torch.Tensor, keep_idx: Optional[torch.Tensor] = None,
+                           mode: int = DROP_K, act: int = ACT_NONE, Z: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
+                           p: float = 0.0, rng: Optional[torch.Tensor] = None, dX: Optional[torch.Tensor] = None,
+                           dW: Optional[torch.Tensor] = None, dbias: Optional[torch.Tensor] = None, dgate: Optional[torch.Tensor] = None,
+                           need_dX: bool = True, need_dW: bool = True, workspace: Optional[torch.Tensor] = None, stream=None,
+                           w_layout: int = W_KN) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor]]:
+    """The gradients of resized_linear_act_fwd: (dX, dW); dbias and dgate are computed where tensors for them are given.  The
+    residual's gradient is dY.  workspace: of act_workspace_bytes(backward=True) bytes (None: allocated)."""
+    here = _here()
+    on = _on(stream, here)
+    M, N = dY.shape
+    dt = dY.dtype
+    K = _layer(None, W, N, dt, w_layout)
+    kp, nk = _list(keep_idx, here)
+    xp, ldx = _like(X, (M, K), dt, here, "X")
+    wp, ldw = _grid(W, here, "W")
+    gyp, ldgy = _grid(dY, here, "dY")
+    zp, ldz = _like(Z, (M, N), dt, here, "Z")
+    gp, ldg = _like(gate, (M, N), dt, here, "gate")
+    dgp, lddg = _like(dgate, (M, N), dt, here, "dgate")
+    if not need_dX:
+        dX = None
+    elif dX is None:
+        dX = _empty((M, K), dt, dY.device, stream)
+    if not need_dW:
+        dW = None
+    elif dW is None:
+        dW = _empty(tuple(W.shape), dt, dY.device, stream)
+    dxp, lddx = _like(dX, (M, K), dt, here, "dX")
+    dwp, lddw = _like(dW, W.shape, dt, here, "dW")
+    if workspace is None:
+        n_keep = nk if kp is not None else N if mode == DROP_N else K
+        workspace = _empty(act_workspace_bytes(M, K, N, n_keep, mode, dt, True), torch.uint8, dY.device, stream, returned=False)
+    st = _lib.zr_resized_linear_act_bwd(xp, ldx, wp, ldw, gyp, ldgy, zp, ldz, gp, ldg, dxp, lddx, dwp, lddw,
+                                        _vec(dbias, N, dt, here, "dbias"), dgp, lddg, M, K, N, kp, nk, mode, w_layout, _code(dt), act, p,
+                                        _generator(rng, here), *_scratch(workspace, here), on)
+    if st:
+        raise ZrError(st)
+    return dX, dW
+
+
+def block_join_workspace_bytes(rows: int, cols: int) -> int:
+    return int(_lib.zr_block_join_workspace_bytes(rows, cols))
+
+
+def block_join_fwd(y: torch.Tensor, x: torch.Tensor, norm: int = NORM_RMS, post: bool = False, pre: bool = True, eps: float = 1e-5,
+                   p: float = 0.0, rng: Optional[torch.Tensor] = None, scale: float = 1.0, bias: Optional[torch.Tensor] = None,
+                   gate: Optional[torch.Tensor] = None, post_w: Optional[torch.Tensor] = None, post_b: Optional[torch.Tensor] = None,
+                   pre_w: Optional[torch.Tensor] = None, pre_b: Optional[torch.Tensor] = None, x_out: Optional[torch.Tensor] = None,
+                   h: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """x_out = x + scale * gate * post(dropout(y + bias)), h = pre(x_out) with the norms that are asked for: (x_out, h or None)."""
+    here = _here()
+    on = _on(stream, here)
+    yp, ldy = _grid(y, here, "y")
+    shape, dt = y.shape, y.dtype
+    rows, cols = shape
+    xp, ldx = _like(x, shape, dt, here, "x")
+    if x_out is None:
+        x_out = _empty(tuple(shape), dt, y.device, stream)
+    if not pre:
+        h = None
+    elif h is None:
+        h = _empty(tuple(shape), dt, y.device, stream)
+    op, ldo = _like(x_out, shape, dt, here, "x_out")
+    hp, ldh = _like(h, shape, dt, here, "h")
+    st = _lib.zr_block_join_fwd(yp, ldy, xp, ldx, op, ldo, hp, ldh, rows, cols, (1 if post else 0) | (2 if pre else 0), norm, eps, p,
+                                _generator(rng, here), scale, _vec(bias, cols, dt, here, "bias"), _vec(gate, cols, dt, here, "gate"),
+                                _vec(post_w, cols, dt, here, "post_w"), _vec(post_b, cols, dt, here, "post_b"),
+                                _vec(pre_w, cols, dt, here, "pre_w"), _vec(pre_b, cols, dt, here, "pre_b"), _code(dt), on)
+    if st:
+        raise ZrError(st)
+    return x_out, h
+
+
+def block_join_bwd(dx_out: Optional[torch.Tensor], dh: Optional[torch.Tensor], x_out: Optional[torch.Tensor], y: Optional[torch.Tensor],
+                   norm: int = NORM_RMS, post: bool = False, pre: bool = True, eps: float = 1e-5, p: float = 0.0,
+                   rng: Optional[torch.Tensor] = None, scale: float = 1.0, bias: Optional[torch.Tensor] = None,
+                   gate: Optional[torch.Tensor] = None, post_w: Optional[torch.Tensor] = None, post_b: Optional[torch.Tensor] = None,
+                   pre_w: Optional[torch.Tensor] = None, dx: Optional[torch.Tensor] = None, dy: Optional[torch.Tensor] = None,
+                   dbias: Optional[torch.Tensor] = None, dgate: Optional[torch.Tensor] = None, dpost_w: Optional[torch.Tensor] = None,
+                   dpost_b: Optional[torch.Tensor] = None, dpre_w: Optional[torch.Tensor] = None, dpre_b: Optional[torch.Tensor] = None,
+                   need_dx: bool = True, need_dy: bool = True, workspace: Optional[torch.Tensor] = None,
+                   stream=None) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor]]:
+    """The gradients of block_join_fwd from those at x_out (None: zeros) and h, x_out and y: (dx, dy); a vector's gradient is
+    computed where a tensor for it is given.  workspace: of block_join_workspace_bytes bytes (None: allocated where needed)."""
+    here = _here()
+    on = _on(stream, here)
+    first = next((t for t in (dx_out, dh) if t is not None), None)
+    if first is None:
+        raise ZrError(1)
+    shape, dt = first.shape, first.dtype
+    rows, cols = shape
+    gp, ldg = _like(dx_out, shape, dt, here, "dx_out")
+    hp, ldh = _like(dh, shape, dt, here, "dh")
+    xp, ldx = _like(x_out, shape, dt, here, "x_out")
+    yp, ldy = _like(y, shape, dt, here, "y")
+    if not need_dx:
+        dx = None
+    elif dx is None:
+        dx = _empty(tuple(shape), dt, first.device, stream)
+    if not need_dy:
+        dy = None
+    elif dy is None:
+        dy = _empty(tuple(shape), dt, first.device, stream)
+    dxp, lddx = _like(dx, shape, dt, here, "dx")
+    dyp, lddy = _like(dy, shape, dt, here, "dy")
+    sums = [_vec(t, cols, dt, here, n) for t, n in ((dbias, "dbias"), (dgate, "dgate"), (dpost_w, "dpost_w"), (dpost_b, "dpost_b"),
+                                                    (dpre_w, "dpre_w"), (dpre_b, "dpre_b"))]
+    if workspace is None and any(s is not None for s in sums):
+        workspace = _empty(block_join_workspace_bytes(rows, cols), torch.uint8, first.device, stream, returned=False)
+    st = _lib.zr_block_join_bwd(gp, ldg, hp, ldh, xp, ldx, yp, ldy, dxp, lddx, dyp, lddy, rows, cols,
+                                (1 if post else 0) | (2 if pre else 0), norm, eps, p, _generator(rng, here), scale,
+                                _vec(bias, cols, dt, here, "bias"), _vec(gate, cols, dt, here, "gate"),
+                                _vec(post_w, cols, dt, here, "post_w"), _vec(post_b, cols, dt, here, "post_b"),
+                                _vec(pre_w, cols, dt, here, "pre_w"), *sums, *_scratch(workspace, here), _code(dt), on)
+    if st:
+        raise ZrError(st)
+    return dx, dy
 
 
 def priority_scores(W_t: torch.Tensor, W_prev: torch.Tensor, mode: int,
