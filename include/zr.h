@@ -346,8 +346,10 @@ typedef enum { ZR_ACT_NONE = 0, ZR_ACT_RELU = 1, ZR_ACT_GELU = 2, ZR_ACT_GELU_TA
  *  bias [N]; gate, residual, Z [M x N] with their pitches; all may be NULL: bias and residual add nothing, gate is 1, Z is not
  *  kept.  dtype: of all tensors.  Sums, activation and everything behind them are fp32, each output is rounded once.
  *  keep_idx NULL: nothing is pruned, n_keep is ignored.  Y may be gate or residual (same pitch); Z must not overlap another tensor.
- *  workspace: optional, of zr_act_fwd_workspace_bytes bytes, 16-byte aligned: room for what zr_resized_linear_fwd extracts.
- *  Launches: 1, +1 with a workspace where kept columns are extracted (DROP_K), +1 for a remainder panel.
+ *  workspace: optional, of zr_act_fwd_workspace_bytes bytes, 16-byte aligned (less is used as far as it reaches), for what
+ *  zr_resized_linear_fwd extracts and for the slices of a split contraction, by the same rules; its contents are undefined
+ *  afterwards, and calls that share one must be ordered on one stream.  Results repeat to the bit for a given size of it.
+ *  Launches: 1, +1 with a workspace where kept columns are extracted (DROP_K), +1 for a remainder panel, +1 where the contraction is split.
  *  Errors: NULL, SHAPE, INDEX, DTYPE, MODE (also a bad w_layout or act), RATIO, LIMIT, HIP. */
 size_t zr_act_fwd_workspace_bytes(int32_t M, int32_t K, int32_t N, int32_t n_keep, int mode, int dtype);
 int zr_resized_linear_act_fwd(const void* X, int64_t ldx, const void* W, int64_t ldw, void* Y, int64_t ldy,

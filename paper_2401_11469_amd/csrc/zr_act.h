@@ -77,6 +77,7 @@ int launch_join_back(const Join& j, int dtype, hipStream_t stream);
 
 // products with a Finish (GemmDesc::finish set): any alignment, and fp32
 int launch_act_any(const GemmDesc& d, hipStream_t stream);
+int launch_act_fast(const GemmDesc& d, hipStream_t stream);     // bf16, 16-byte aligned rows; -1: not taken
 int launch_act_f32(const GemmDesc& d, hipStream_t stream);
 
 // ---- device functions -----------------------------------------------------------
@@ -190,6 +191,12 @@ struct Draw {
     {
         return (e & 1 ? w[e >> 1] >> 16 : w[e >> 1] & 0xffffu) >= drop;
     }
+    // (the same for an e that is not known at compile time: no indexed registers)
+    __device__ __forceinline__ bool kept_at(int e, uint32_t drop) const
+    {
+        const uint64_t low = w[0] | (uint64_t)w[1] << 32, high = w[2] | (uint64_t)w[3] << 32;
+        return (uint32_t)((e < 4 ? low : high) >> 16 * (e & 3) & 0xffffu) >= drop;
+    }
     // a dropped element is +0 whatever it was
     __device__ __forceinline__ void apply(float (&x)[8], uint32_t drop, float factor) const
     {
@@ -270,74 +277,140 @@ template <bool EXACT, bool SLOPE> __device__ __forceinline__ void act8(int act, 
     }
 }
 
-// Columns col + lo .. col + hi - 1 (col a multiple of 8) of one row of a product: z holds the sums.
+// The group of eight columns at col (a multiple of 8) of one row of a product: z holds the sums; bias, gate, residual what lies
+// there, requested before.
 template <typename T>
-__device__ __forceinline__ void finish8(const Finish& f, T* out, int64_t ldo, int row, int col, int lo, int hi, float (&z)[8])
+__device__ __forceinline__ void finish8(const Finish& f, T* out, int64_t ldo, int row, int col, float (&z)[8], const Raw8<T>& bias,
+                                        const Raw8<T>& gate, const Raw8<T>& residual)
 {
     constexpr bool EXACT = sizeof(T) == 4;
     float x[8], a[8], unused[8];
     if (f.bias) {
-        load8((const T*)f.bias + col, lo, hi, x);
+        bias.values(x);
 #pragma unroll
         for (int e = 0; e < 8; ++e) z[e] += x[e];
     }
-    if (f.Z) store8((T*)f.Z + (size_t)row * (size_t)f.ldz + col, lo, hi, z);
+    if (f.Z) store8((T*)f.Z + (size_t)row * (size_t)f.ldz + col, 0, 8, z);
     act8<EXACT, false>(f.act, z, a, unused);
     if (f.gate) {
-        load8((const T*)f.gate + (size_t)row * (size_t)f.ldg + col, lo, hi, x);
+        gate.values(x);
 #pragma unroll
         for (int e = 0; e < 8; ++e) a[e] *= x[e];
     }
     if (f.drop) Draw(f.rng[0], f.rng[1], (uint32_t)row, (uint32_t)col >> 3).apply(a, f.drop, f.factor);
     if (f.residual) {
-        load8((const T*)f.residual + (size_t)row * (size_t)f.ldr + col, lo, hi, x);
+        residual.values(x);
 #pragma unroll
         for (int e = 0; e < 8; ++e) a[e] += x[e];
     }
-    store8(out + (size_t)row * (size_t)ldo + col, lo, hi, a);
+    store8(out + (size_t)row * (size_t)ldo + col, 0, 8, a);
 }
 
-// Rows row0 .. row0 + rows - 1 of a tile whose sums lie in LDS (Cs, pitch CP floats), NT threads.
+// One element, the same way.
+template <typename T>
+__device__ __forceinline__ void finish1(const Finish& f, T* out, int64_t ldo, int row, int col, float z)
+{
+    float a, unused;
+    if (f.bias) z += one_of((const T*)f.bias + col);
+    if (f.Z) put_one((T*)f.Z + (size_t)row * (size_t)f.ldz + col, z);
+    act_one<sizeof(T) == 4, false>(f.act, z, a, unused);
+    if (f.gate) a *= one_of((const T*)f.gate + (size_t)row * (size_t)f.ldg + col);
+    if (f.drop) a = Draw(f.rng[0], f.rng[1], (uint32_t)row, (uint32_t)col >> 3).kept_at(col & 7, f.drop) ? a * f.factor : 0.f;
+    if (f.residual) a += one_of((const T*)f.residual + (size_t)row * (size_t)f.ldr + col);
+    put_one(out + (size_t)row * (size_t)ldo + col, a);
+}
+
+// Rows row0 .. row0 + rows - 1 of a tile of R columns whose sums lie in LDS (Cs, pitch CP floats), NT threads.
 // sidx == nullptr: the tile's columns are col0 .. col0 + cols - 1 (col0 a multiple of 8).  Otherwise sidx[j] is the original
 // column of the tile's column j, ascending, and the tile owns the original columns start .. end - 1: those without an entry have
-// the sum 0.  tab: TAB words of LDS.  Every thread of the workgroup calls it; LDS is free again after a barrier.
-template <int NT, int TAB, typename T>
+// the sum 0.  tab: TAB words of LDS, 16-byte aligned.  Every thread of the workgroup calls it; LDS is free again after a barrier.
+// Whole groups of eight leave as such, a thread requesting what it needs of U of them together; the elements of the groups that a
+// tile shares with its neighbours, or at the end of a row, go out one by one in a pass of their own (as a branch among the groups
+// they are in every wavefront's way: 8192 x 4096 x 2752 of 2064 kept, gated 170 us without the remainder panel's split, now 144 with).
+template <int NT, int R, int TAB, int U, typename T>
 __device__ __forceinline__ void finish_tile(const Finish& f, T* out, int64_t ldo, const float* Cs, int CP, int row0, int rows, int col0,
                                             int cols, const int* sidx, int start, int end, int* tab, int tid)
 {
     static_assert(TAB % 8 == 0, "whole groups");
+    // `count` whole groups, sums(r, col, z) gives those of row r; where(i, r, col) says where group i lies
+    auto whole = [&](int count, auto where, auto sums) {
+        for (int i0 = tid; i0 < count; i0 += NT * U) {
+            Raw8<T> b[U], g[U], r[U];
+            int at[U], col[U];
+#pragma unroll
+            for (int i = 0; i < U; ++i) where(min(i0 + NT * i, count - 1), at[i], col[i]);        // (past the end: the last one, not stored)
+            if (f.bias) {
+#pragma unroll
+                for (int i = 0; i < U; ++i) b[i].load((const T*)f.bias + col[i]);
+            }
+            if (f.gate) {
+#pragma unroll
+                for (int i = 0; i < U; ++i) g[i].load((const T*)f.gate + (size_t)(row0 + at[i]) * (size_t)f.ldg + col[i]);
+            }
+            if (f.residual) {
+#pragma unroll
+                for (int i = 0; i < U; ++i) r[i].load((const T*)f.residual + (size_t)(row0 + at[i]) * (size_t)f.ldr + col[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                if (i0 + NT * i >= count) break;
+                float z[8];
+                sums(at[i], col[i], z);
+                finish8(f, out, ldo, row0 + at[i], col[i], z, b[i], g[i], r[i]);
+            }
+        }
+    };
+    // elements [lo1, hi1) and [lo2, hi2) of every row
+    auto single = [&](int lo1, int hi1, int lo2, int hi2, auto sum) {
+        const int n1 = max(hi1 - lo1, 0), n = n1 + max(hi2 - lo2, 0);
+        for (int u = tid; u < rows * n; u += NT) {
+            const int r = u / n, e = u - r * n, col = e < n1 ? lo1 + e : lo2 + (e - n1);
+            finish1(f, out, ldo, row0 + r, col, sum(r, col));
+        }
+    };
     if (!sidx) {
-        const int groups = (cols + 7) >> 3;
-        for (int u = tid; u < rows * groups; u += NT) {
-            const int r = u / groups, j = 8 * (u - r * groups);
-            float z[8];
-            const float* c = Cs + r * CP + j;
+        constexpr int GROUPS = R / 8;
+        auto sums = [&](int r, int col, float (&z)[8]) {
+            const float* c = Cs + r * CP + col - col0;
             const f4 z0 = *(const f4*)c, z1 = *(const f4*)(c + 4);
 #pragma unroll
             for (int e = 0; e < 8; ++e) z[e] = e < 4 ? z0[e & 3] : z1[e & 3];
-            finish8(f, out, ldo, row0 + r, col0 + j, 0, min(8, cols - j), z);
-        }
+        };
+        const int groups = cols >> 3;
+        if (groups == GROUPS) whole(rows * GROUPS, [&](int i, int& r, int& col) { r = i / GROUPS; col = col0 + 8 * (i % GROUPS); }, sums);
+        else whole(rows * groups, [&](int i, int& r, int& col) { r = i / groups; col = col0 + 8 * (i - r * groups); }, sums);
+        single(col0 + 8 * groups, col0 + cols, 0, 0, [&](int r, int col) { return Cs[r * CP + col - col0]; });
         return;
     }
     for (int base = start & ~7; base < end; base += TAB) {
-        const int width = min(TAB, ((end + 7) & ~7) - base), groups = width >> 3;
+        const int lo = max(start, base), hi = min(end, base + TAB);
         for (int q = tid; q < TAB; q += NT) tab[q] = -1;
         __syncthreads();
         for (int q = tid; q < cols; q += NT) {
             const int p = sidx[q] - base;
-            if (p >= 0 && p < width) tab[p] = q;
+            if (p >= 0 && p < TAB) tab[p] = q;
         }
         __syncthreads();
-        for (int u = tid; u < rows * groups; u += NT) {
-            const int r = u / groups, p = 8 * (u - r * groups), col = base + p;
-            float z[8];
+        const int first = (lo + 7) & ~7, last = hi & ~7, groups = max(last - first, 0) >> 3;
+        // (count below 2^23, so the quotient is exact but for a last bit that the half step covers)
+        const float inv = 1.f / (float)max(groups, 1);
+        whole(rows * groups,
+              [&](int i, int& r, int& col) {
+                  r = (int)(((float)i + 0.5f) * inv);
+                  col = first + 8 * (i - r * groups);
+              },
+              [&](int r, int col, float (&z)[8]) {
+                  typedef int i4 __attribute__((ext_vector_type(4)));
+                  const i4 j0 = *(const i4*)(tab + col - base), j1 = *(const i4*)(tab + col - base + 4);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int j = tab[p + e];
-                z[e] = j >= 0 ? Cs[r * CP + j] : 0.f;
-            }
-            finish8(f, out, ldo, row0 + r, col, max(start - col, 0), min(end - col, 8), z);
-        }
+                  for (int e = 0; e < 8; ++e) {
+                      const int j = e < 4 ? j0[e & 3] : j1[e & 3];
+                      const float v = Cs[r * CP + max(j, 0)];
+                      z[e] = j >= 0 ? v : 0.f;
+                  }
+              });
+        const int mid = min(first, hi);
+        single(lo, mid, max(last, mid), hi, [&](int r, int col) { const int j = tab[col - base]; return j >= 0 ? Cs[r * CP + j] : 0.f; });
         __syncthreads();
     }
 }

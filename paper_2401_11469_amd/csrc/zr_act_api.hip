@@ -7,6 +7,7 @@ using namespace zr;
 namespace {
 
 constexpr int32_t kMaxExtent = 65535 * 32;      // as for the other calls
+constexpr size_t kSliceBytes = (size_t)64 << 20;
 
 bool valid_dtype(int dt) { return dt == ZR_F32 || dt == ZR_BF16; }
 size_t size_of(int dtype) { return dtype == ZR_BF16 ? 2 : 4; }
@@ -61,9 +62,9 @@ int zr_dropout(const void* x, int64_t ldx, void* out, int64_t ldo, int32_t rows,
 size_t zr_act_fwd_workspace_bytes(int32_t M, int32_t K, int32_t N, int32_t n_keep, int mode, int dtype)
 {
     if (M < 1 || K < 1 || N < 1 || n_keep < 1 || !valid_dtype(dtype)) return 0;
-    // the kept columns of X, which DROP_K multiplies (bf16)
+    // (bf16) the kept columns of X, which DROP_K multiplies, and the slices of a split contraction
     const size_t held = mode == ZR_DROP_K && n_keep < K && dtype == ZR_BF16 ? (size_t)M * (size_t)((n_keep + 63) / 64 * 64) * 2 : 0;
-    return held + 16;
+    return held + (dtype == ZR_BF16 ? kSliceBytes : 0) + 16;
 }
 
 int zr_resized_linear_act_fwd(const void* X, int64_t ldx, const void* W, int64_t ldw, void* Y, int64_t ldy,

@@ -209,7 +209,11 @@ bool ensure_max_dynamic_lds(const void* fn, int bytes, void* flags16)
 
 static int launch_gemm_untimed(const GemmDesc& d, hipStream_t stream)
 {
-    if (d.finish) return d.dtype == ZR_BF16 ? launch_act_any(d, stream) : d.dtype == ZR_F32 ? launch_act_f32(d, stream) : ZR_ERR_DTYPE;
+    if (d.finish) {
+        const int st = launch_act_fast(d, stream);
+        if (st >= 0) return st;
+        return d.dtype == ZR_BF16 ? launch_act_any(d, stream) : d.dtype == ZR_F32 ? launch_act_f32(d, stream) : ZR_ERR_DTYPE;
+    }
     const int fast = launch_gemm_fast(d, stream);   // bf16, 16-byte aligned rows
     if (fast >= 0) return fast;
     if (d.dtype == ZR_BF16) return launch_gemm_any(d, stream);

@@ -505,7 +505,7 @@ __device__ __forceinline__ void f32_body(const G& g, float* smem, const int lin)
     if constexpr (std::is_same_v<G, FinishArgs>) {
         const int start = !scatter_c || j0 == 0 ? 0 : sidx[0];
         const int end = !scatter_c ? 0 : j0 + R >= g.J ? g.out_full : clamp_idx(g.keep[j0 + R], g.out_full);
-        finish_tile<NT, TAB>(g.f, g.out, g.ldo, Cs, CP, i0, rows_valid, j0, cols_valid, scatter_c ? sidx : nullptr, start, end, sidx + 2 * R, tid);
+        finish_tile<NT, R, TAB, 2>(g.f, g.out, g.ldo, Cs, CP, i0, rows_valid, j0, cols_valid, scatter_c ? sidx : nullptr, start, end, sidx + 2 * R, tid);
         return;
     }
     if (scatter_c) {

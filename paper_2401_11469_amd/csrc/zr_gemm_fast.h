@@ -32,6 +32,7 @@
 #include <cstdlib>
 #include <type_traits>
 
+#include "zr_act.h"
 #include "zr_common.h"
 #include <cstring>
 
@@ -1096,16 +1097,27 @@ __device__ __forceinline__ void tile_at(const FArgs& g, int t, int& ti, int& tj)
     tj = within / rows_in;
 }
 
+// The end of a product with bias, activation and so on: the sums go through LDS in fp32, FROWS rows of the tile at a time (all, or
+// half of those of the tiles above 128 x 128), past the stages: the kept columns of the tile and finish_tile's table behind them.
+struct FinishFArgs : FArgs {
+    Finish f;
+};
+constexpr int FINISH_TAB = 512;
+template <int BM, int BN> constexpr int finish_rows() { return BM * BN > 128 * 128 ? BM / 2 : BM; }
+template <int BM, int BN> constexpr int finish_smem_bytes() { return (finish_rows<BM, BN>() * (BN + 4) + BN + FINISH_TAB) * 4; }
+
 // One workgroup's tile `lin` (of an XCD-aware numbering, see the kernels) of a product.
 // PHASE: 0 = the whole product; 1 = the first launch of a split contraction (a separate kernel, so
 // that the ordinary one keeps its register allocation).
 // PART: the dX or the dW of a pair, whose scatter is of columns, or of rows, and which leave no sums.
+// FinishFArgs: a forward product with bias, activation and so on before the results are stored.
 enum { PART_NONE, PART_DX, PART_DW };
-template <template <int, int> class LA_, template <int, int> class LB_, int BM, int BN, int WM, int WN, int PHASE, int PART = PART_NONE>
-__device__ __forceinline__ void fast_body(const FArgs& g, uint32_t* smem, const int lin)
+template <template <int, int> class LA_, template <int, int> class LB_, int BM, int BN, int WM, int WN, int PHASE, int PART = PART_NONE, class G = FArgs>
+__device__ __forceinline__ void fast_body(const G& g, uint32_t* smem, const int lin)
 {
     constexpr int NT = 64 * WM * WN;
-    constexpr bool COLS = PART != PART_DW, ROWS = PART != PART_DX, SUMS = PART == PART_NONE;
+    constexpr bool FINISHES = std::is_same_v<G, FinishFArgs>;
+    constexpr bool COLS = PART != PART_DW, ROWS = PART != PART_DX && !FINISHES, SUMS = PART == PART_NONE;
     typedef LA_<BM, NT> LA;
     typedef LB_<BN, NT> LB;
     // (not where both operands come through the transposing reads on a tile larger than
@@ -1275,6 +1287,34 @@ __device__ __forceinline__ void fast_body(const FArgs& g, uint32_t* smem, const 
     }
 
     // ---- epilogue -------------------------------------------------------------
+    if constexpr (FINISHES) {
+        constexpr int FROWS = finish_rows<BM, BN>(), FP = BN + 4;
+        static_assert(!LA::NEEDS_IDX && !LB::NEEDS_IDX && FROWS % MT == 0 && FROWS % (BM / WM) == 0, "whole wavefronts' rows");
+        // (half of the largest tiles' sums stay in registers meanwhile: three groups at a time there, four would spill)
+        float* Fs = (float*)smem;
+        int* sidx = (int*)(smem + FROWS * FP);
+        int* tab = sidx + BN;
+        const int cols_valid = min(BN, g.J - j0);
+        if (scatter_c && tid < cols_valid) sidx[tid] = clamp_idx(keep_mine, g.out_full);
+        __syncthreads();
+        const int start = !scatter_c || j0 == 0 ? 0 : sidx[0];
+        const int end = !scatter_c ? 0 : j0 + BN >= g.J ? g.out_full : clamp_idx(keep_next, g.out_full);
+        for (int r0 = 0; r0 < BM && i0 + r0 < g.I; r0 += FROWS) {
+            if (wr0 >= r0 && wr0 < r0 + FROWS) {
+#pragma unroll
+                for (int a = 0; a < TM; ++a)
+#pragma unroll
+                    for (int b = 0; b < TN; ++b)
+#pragma unroll
+                        for (int r = 0; r < AR; ++r) Fs[(acc_row(a, r) - r0) * FP + acc_col(b)] = acc[a][b][r];
+            }
+            __syncthreads();
+            finish_tile<NT, BN, FINISH_TAB, BM * BN == 256 * 256 ? 3 : 4>(g.f, g.out, g.ldo, Fs, FP, i0 + r0, min(FROWS, g.I - i0 - r0), j0, cols_valid,
+                                            scatter_c ? sidx : nullptr, start, end, tab, tid);
+            __syncthreads();
+        }
+        return;
+    }
     E* Cs = (E*)smem;
     const int rows_valid = min(BM, g.I - i0);
     const int cols_valid = min(BN, g.J - j0);
