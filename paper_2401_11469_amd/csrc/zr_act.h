@@ -69,6 +69,7 @@ struct Join {
     void* dy; int64_t lddy;
     float* partial;                        // [vectors x slabs x cols]
     int slabs;
+    int biases;                            // a gradient of bias, post_b or pre_b is wanted
 };
 int join_max_cols();
 int join_slabs(int rows, int cols);

@@ -215,6 +215,7 @@ int zr_block_join_bwd(const void* dx_out, int64_t lddxo, const void* dh, int64_t
     j.dx_out = dx_out; j.lddxo = lddxo; j.dh = dh; j.lddh = lddh; j.dx = dx; j.lddx = lddx; j.dy = dy; j.lddy = lddy;
     j.partial = vectors ? (float*)workspace : nullptr;
     j.slabs = join_slabs(rows, cols);
+    j.biases = dbias || dpost_b || dpre_b;
     hipStream_t s = (hipStream_t)stream;
     st = launch_join_back(j, dtype, s);
     if (st != ZR_OK || !vectors) return st;

@@ -95,12 +95,13 @@ __global__ __launch_bounds__(256) void act_back_kernel(const ActBack a, int acro
 }
 
 // ---------------------------------------------------------------------------
-// Sums over slabs: 64 columns to a workgroup, four wavefronts along the slabs, added in a fixed order
+// Sums over slabs: 64 columns to a workgroup, sixteen wavefronts along the slabs, added in a fixed order
 // ---------------------------------------------------------------------------
 template <typename T>
-__global__ __launch_bounds__(256) void sum_slabs_kernel(const float* partial, int slabs, int n, const SumOut out)
+__global__ __launch_bounds__(1024) void sum_slabs_kernel(const float* partial, int slabs, int n, const SumOut out)
 {
-    __shared__ float part[4][64];
+    constexpr int W = 16, U = 8;
+    __shared__ float part[W][64];
     void* dst = out.out[0];
 #pragma unroll
     for (int v = 1; v < MAX_SUMS; ++v) dst = (int)blockIdx.y == v ? out.out[v] : dst;
@@ -108,11 +109,21 @@ __global__ __launch_bounds__(256) void sum_slabs_kernel(const float* partial, in
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = (int)blockIdx.x * 64 + lane;
     const float* p = partial + (size_t)blockIdx.y * (size_t)slabs * (size_t)n;
     float v = 0.f;
-    if (c < n)
-        for (int s = wave; s < slabs; s += 4) v += p[(size_t)s * (size_t)n + c];
+    for (int s = wave; s < slabs && c < n; s += W * U) {
+        float x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) x[u] = p[(size_t)min(s + W * u, slabs - 1) * (size_t)n + c];
+#pragma unroll
+        for (int u = 0; u < U; ++u) v += s + W * u < slabs ? x[u] : 0.f;
+    }
     part[wave][lane] = v;
     __syncthreads();
-    if (wave == 0 && c < n) put_one((T*)dst + c, (part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane]));
+    if (wave == 0 && c < n) {
+        float sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < W; ++w) sum += part[w][lane];
+        put_one((T*)dst + c, sum);
+    }
 }
 
 }  // namespace
@@ -159,8 +170,8 @@ int launch_act_back(const ActBack& a, int dtype, hipStream_t stream)
 int launch_sum_slabs(const float* partial, int slabs, int n, int vectors, const SumOut& out, int dtype, hipStream_t stream)
 {
     const dim3 grid((unsigned)((n + 63) / 64), (unsigned)vectors);
-    if (dtype == ZR_BF16) hipLaunchKernelGGL(sum_slabs_kernel<Bf>, grid, dim3(256), 0, stream, partial, slabs, n, out);
-    else hipLaunchKernelGGL(sum_slabs_kernel<float>, grid, dim3(256), 0, stream, partial, slabs, n, out);
+    if (dtype == ZR_BF16) hipLaunchKernelGGL(sum_slabs_kernel<Bf>, grid, dim3(1024), 0, stream, partial, slabs, n, out);
+    else hipLaunchKernelGGL(sum_slabs_kernel<float>, grid, dim3(1024), 0, stream, partial, slabs, n, out);
     return hip_status(hipGetLastError());
 }
 

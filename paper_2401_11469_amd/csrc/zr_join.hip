@@ -16,6 +16,21 @@ namespace {
 
 constexpr int MAX_COLS = 16384;
 
+// Sum over a wavefront, for all of its lanes: within rows of 16 lanes, then across the rows (no LDS: a shuffle takes ten times as long).
+__device__ __forceinline__ float wave_sum(float v)
+{
+    auto step = [](float x, auto ctrl) {
+        return x + __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(x), decltype(ctrl)::value, 0xf, 0xf, false));
+    };
+    v = step(v, std::integral_constant<int, 0x111>());      // row_shr 1, 2, 4, 8
+    v = step(v, std::integral_constant<int, 0x112>());
+    v = step(v, std::integral_constant<int, 0x114>());
+    v = step(v, std::integral_constant<int, 0x118>());
+    v = step(v, std::integral_constant<int, 0x142>());      // row_bcast 15, 31
+    v = step(v, std::integral_constant<int, 0x143>());
+    return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), 63));
+}
+
 // Sums over the NT threads of a row, for every one of them.  One barrier a call: consecutive calls use two places in turn.
 template <int NT, int G> struct RowSums {
     static constexpr int WAVES = NT / 64;
@@ -23,11 +38,8 @@ template <int NT, int G> struct RowSums {
     int place = 0;
     __device__ __forceinline__ void two(float& a, float& b)
     {
-#pragma unroll
-        for (int off = 32; off; off >>= 1) {
-            a += __shfl_xor(a, off, 64);
-            b += __shfl_xor(b, off, 64);
-        }
+        a = wave_sum(a);
+        b = wave_sum(b);
         if constexpr (WAVES > 1) {
             const int wave = threadIdx.x >> 6, first = wave / WAVES * WAVES;
             if ((threadIdx.x & 63) == 0) { part[place][0][wave] = a; part[place][1][wave] = b; }
@@ -40,7 +52,105 @@ template <int NT, int G> struct RowSums {
     }
 };
 
+// rows that a workgroup takes at a time
 template <int NT> constexpr int groups_of() { return NT < 256 ? 256 / NT : 1; }
+
+// Where a thread's columns lie: groups of eight at col[k], of which hi[k] are within the row (negative or 0: none).
+// Loads are unconditional (a load under a branch is waited for where the branch ends): a group past the end, or that reaches past
+// it, is read from the row's last eight columns and moved into place.
+template <int NT, int NV> struct Columns {
+    int col[NV], hi[NV];
+    uint32_t from[NV];
+    bool ragged, narrow, edge;         // uniform: the last group is no whole one; rows of less than eight; threads without columns
+    __device__ __forceinline__ Columns(int cols, int tid)
+    {
+        narrow = cols < 8;
+        ragged = cols % 8 != 0 && !narrow;
+        edge = cols % (8 * NT * NV) != 0;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            col[k] = 8 * (tid + NT * k);
+            hi[k] = min(8, cols - col[k]);
+            from[k] = (uint32_t)max(0, min(col[k], cols - 8));
+        }
+    }
+    template <typename T> __device__ __forceinline__ void fetch(Raw8<T> (&r)[NV], const void* p, int64_t at) const
+    {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            if (narrow) {
+                float x[8];
+                load8((const T*)p + at, 0, max(hi[k], 0), x);
+                r[k].take(x);
+            } else {
+                r[k].load((const T*)p + at + from[k]);
+            }
+        }
+    }
+    // the values, 0 past the row's end
+    template <typename T> __device__ __forceinline__ void values(const Raw8<T> (&r)[NV], float (&x)[NV][8]) const
+    {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            r[k].values(x[k]);
+            if (ragged) {
+                const int s = col[k] - (int)from[k];
+#pragma unroll
+                for (int bit = 1; bit < 8; bit *= 2)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[k][e] = s & bit ? (e + bit < 8 ? x[k][e + bit] : 0.f) : x[k][e];
+            }
+            if (edge) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[k][e] = e < hi[k] ? x[k][e] : 0.f;
+            }
+        }
+    }
+    template <typename T> __device__ __forceinline__ void put(void* p, int64_t at, const float (&x)[NV][8]) const
+    {
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+            if (hi[k] > 0) store8((T*)p + at + (uint32_t)col[k], 0, hi[k], x[k]);
+    }
+};
+
+// A vector of the row's columns, in registers for all rows; one that is missing stands for `other`.
+template <typename T, int NV> struct Vector {
+    Raw8<T> r[NV];
+    bool there;
+    template <class C> __device__ __forceinline__ Vector(const void* p, const C& c) : there(p != nullptr)
+    {
+        if (there) {
+            c.template fetch<T>(r, p, 0);
+            float x[NV][8];
+            c.template values<T>(r, x);
+#pragma unroll
+            for (int k = 0; k < NV; ++k) r[k].take(x[k]);
+        }
+    }
+    __device__ __forceinline__ void times(float (&x)[NV][8]) const
+    {
+        if (!there) return;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            float v[8];
+            r[k].values(v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[k][e] *= v[e];
+        }
+    }
+    __device__ __forceinline__ void plus(float (&x)[NV][8]) const
+    {
+        if (!there) return;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            float v[8];
+            r[k].values(v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[k][e] += v[e];
+        }
+    }
+};
 
 // v <- (v - mean) r for both of two rows' worth of values (TWO), or the first alone; r for each
 template <int NV, bool TWO, class S>
@@ -81,79 +191,57 @@ __device__ __forceinline__ void normalise(float (&u)[NV][8], float (&v)[NV][8], 
         for (int e = 0; e < 8; ++e) { u[k][e] *= ru; if constexpr (TWO) v[k][e] *= rv; }
 }
 
-// x <- x * v[col ..] (add: + v), with a vector that may be missing
-template <typename T> __device__ __forceinline__ void times(float (&x)[8], const void* v, int col, int hi)
-{
-    if (!v || hi <= 0) return;
-    float w[8];
-    load8((const T*)v + col, 0, hi, w);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] *= w[e];
-}
-template <typename T> __device__ __forceinline__ void plus(float (&x)[8], const void* v, int col, int hi)
-{
-    if (!v || hi <= 0) return;
-    float w[8];
-    load8((const T*)v + col, 0, hi, w);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] += w[e];
-}
-template <typename T> __device__ __forceinline__ void row8(const void* p, int64_t ld, int64_t row, int col, int hi, float (&x)[8])
-{
-    if (p && hi > 0) load8((const T*)p + row * ld + col, 0, hi, x);
-    else
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = 0.f;
-}
-
 template <typename T, int NT, int NV, bool POST, bool PRE>
-__global__ __launch_bounds__(NT * groups_of<NT>()) void join_kernel(const Join j)
+__global__ __launch_bounds__(NT * groups_of<NT>(), NT * groups_of<NT>() / 256) void join_kernel(const Join j)
 {
     constexpr int G = groups_of<NT>();
-    __shared__ float part[2][2][NT * G / 64];
+    __shared__ __align__(16) float part[2][2][NT * G / 64];
     RowSums<NT, G> sums{part};
-    const int tid = threadIdx.x % NT;
-    int col[NV], hi[NV];
-#pragma unroll
-    for (int k = 0; k < NV; ++k) { col[k] = 8 * (tid + NT * k); hi[k] = min(8, j.cols - col[k]); }
+    const Columns<NT, NV> c(j.cols, threadIdx.x % NT);
+    const int mine = G == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / NT);        // (a row is a wavefront's or more: scalar addresses)
+    const Vector<T, NV> bias(j.bias, c), gate(j.gate, c), post_w(POST ? j.post_w : nullptr, c), post_b(POST ? j.post_b : nullptr, c);
+    const Vector<T, NV> pre_w(PRE ? j.pre_w : nullptr, c), pre_b(PRE ? j.pre_b : nullptr, c);
     uint64_t seed = 0, offset = 0;
     if (j.drop) { seed = j.rng[0]; offset = j.rng[1]; }
-    for (int64_t base = (int64_t)blockIdx.x * G; base < j.rows; base += (int64_t)gridDim.x * G) {
-        const int64_t row = base + threadIdx.x / NT;
+    const int64_t step = (int64_t)gridDim.x * G;
+    int64_t base = (int64_t)blockIdx.x * G;
+    Raw8<T> ry[NV], rx[NV];
+    auto fetch = [&](int64_t from) {
+        const int64_t row = min(from + mine, (int64_t)j.rows - 1);
+        c.template fetch<T>(ry, j.y, row * j.ldy);
+        c.template fetch<T>(rx, j.x, row * j.ldx);
+    };
+    fetch(base);
+    for (; base < j.rows; base += step) {
+        const int64_t row = base + mine;
         const bool on = row < j.rows;
         float t[NV][8], x[NV][8], r, unused;
+        c.template values<T>(ry, t);
+        c.template values<T>(rx, x);
+        // the next row's values travel while this one's are used (past the last row: the last one's again)
+        fetch(base + step);
+        bias.plus(t);
+        if (j.drop) {
 #pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            const int h = on ? hi[k] : 0;
-            row8<T>(j.y, j.ldy, row, col[k], h, t[k]);
-            row8<T>(j.x, j.ldx, row, col[k], h, x[k]);
-            plus<T>(t[k], j.bias, col[k], h);
-            if (j.drop) Draw(seed, offset, (uint32_t)row, (uint32_t)col[k] >> 3).apply(t[k], j.drop, j.factor);
+            for (int k = 0; k < NV; ++k) Draw(seed, offset, (uint32_t)row, (uint32_t)c.col[k] >> 3).apply(t[k], j.drop, j.factor);
         }
         if constexpr (POST) {
-            normalise<NV, false>(t, t, r, unused, hi, j.cols, j.layer, j.eps, sums);
-#pragma unroll
-            for (int k = 0; k < NV; ++k) {
-                times<T>(t[k], j.post_w, col[k], hi[k]);
-                plus<T>(t[k], j.post_b, col[k], hi[k]);
-            }
+            normalise<NV, false>(t, t, r, unused, c.hi, j.cols, j.layer, j.eps, sums);
+            post_w.times(t);
+            post_b.plus(t);
         }
+        gate.times(t);
 #pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            times<T>(t[k], j.gate, col[k], hi[k]);
+        for (int k = 0; k < NV; ++k)
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[k][e] = fmaf(j.scale, t[k][e], x[k][e]);
-            if (on && hi[k] > 0) store8((T*)j.x_out + row * j.ldxo + col[k], 0, hi[k], x[k]);
-        }
+        if (on) c.template put<T>(j.x_out, row * j.ldxo, x);
         if constexpr (PRE) {
             // (of the sums as they are, before they are rounded into x_out; columns past the end are zeros all the way)
-            normalise<NV, false>(x, x, r, unused, hi, j.cols, j.layer, j.eps, sums);
-#pragma unroll
-            for (int k = 0; k < NV; ++k) {
-                times<T>(x[k], j.pre_w, col[k], hi[k]);
-                plus<T>(x[k], j.pre_b, col[k], hi[k]);
-                if (on && hi[k] > 0) store8((T*)j.h + row * j.ldh + col[k], 0, hi[k], x[k]);
-            }
+            normalise<NV, false>(x, x, r, unused, c.hi, j.cols, j.layer, j.eps, sums);
+            pre_w.times(x);
+            pre_b.plus(x);
+            if (on) c.template put<T>(j.h, row * j.ldh, x);
         }
     }
 }
@@ -176,120 +264,148 @@ __device__ __forceinline__ void norm_back(float (&g)[NV][8], const float (&hat)[
         for (int e = 0; e < 8; ++e) g[k][e] = e < hi[k] ? r * (g[k][e] - b - hat[k][e] * a) : 0.f;
 }
 
-template <typename T, int NT, int NV, bool POST, bool PRE>
-__global__ __launch_bounds__(NT * groups_of<NT>()) void join_back_kernel(const Join j)
+template <int NV> __device__ __forceinline__ void add_product(float (&total)[NV][8], const float (&a)[NV][8], const float (&b)[NV][8])
+{
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) total[k][e] = fmaf(a[k][e], b[k][e], total[k][e]);
+}
+template <int NV> __device__ __forceinline__ void add(float (&total)[NV][8], const float (&a)[NV][8])
+{
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) total[k][e] += a[k][e];
+}
+
+// wavefronts to a SIMD that the registers have to leave room for
+template <int NT, int NV, bool BIASES> constexpr int back_waves() { return NT * NV > 1024 ? 4 : BIASES ? 2 : NT <= 256 ? 3 : 2; }
+
+// BIASES: gradients of bias, post_b or pre_b are wanted (without them a third of the registers for sums goes, and two rows of up to
+// 4096 columns fit a compute unit at a time)
+template <typename T, int NT, int NV, bool POST, bool PRE, bool BIASES>
+__global__ __launch_bounds__(NT * groups_of<NT>(), (back_waves<NT, NV, BIASES>())) void join_back_kernel(const Join j)
 {
     constexpr int G = groups_of<NT>(), BLOCK = NT * G;
-    __shared__ float part[2][2][BLOCK / 64];
+    __shared__ __align__(16) float part[2][2][BLOCK / 64];
     RowSums<NT, G> sums{part};
-    const int tid = threadIdx.x % NT;
-    int col[NV], hi[NV];
-#pragma unroll
-    for (int k = 0; k < NV; ++k) { col[k] = 8 * (tid + NT * k); hi[k] = min(8, j.cols - col[k]); }
+    const Columns<NT, NV> c(j.cols, threadIdx.x % NT);
+    const int mine = G == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / NT);        // (a row is a wavefront's or more: scalar addresses)
+    const Vector<T, NV> bias(j.bias, c), gate(j.gate, c), post_w(POST ? j.post_w : nullptr, c), post_b(POST ? j.post_b : nullptr, c);
+    const Vector<T, NV> pre_w(PRE ? j.pre_w : nullptr, c);
     uint64_t seed = 0, offset = 0;
     if (j.drop) { seed = j.rng[0]; offset = j.rng[1]; }
-    // gradients of the vectors: bias, gate, weight and bias of the post norm, of the pre norm
-    constexpr int SETS = 2 + (POST ? 2 : 0) + (PRE ? 2 : 0), AT_POST = 2, AT_PRE = POST ? 4 : 2;
-    float total[SETS][NV][8];
+    // gradients of the vectors, where their sums lie in j.partial: bias, gate, weight and bias of the post norm, of the pre norm
+    float total[6][NV][8];
 #pragma unroll
-    for (int s = 0; s < SETS; ++s)
+    for (int s = 0; s < 6; ++s)
 #pragma unroll
         for (int k = 0; k < NV; ++k)
 #pragma unroll
             for (int e = 0; e < 8; ++e) total[s][k][e] = 0.f;
 
-    for (int64_t base = (int64_t)blockIdx.x * G; base < j.rows; base += (int64_t)gridDim.x * G) {
-        const int64_t row = base + threadIdx.x / NT;
-        const bool on = row < j.rows;
-        float t[NV][8], x[NV][8], d[NV][8], g[NV][8], rt = 0.f, rx = 0.f;
-#pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            const int h = on ? hi[k] : 0;
-            row8<T>(j.dx_out, j.lddxo, row, col[k], h, d[k]);
-            if constexpr (PRE) {
-                row8<T>(j.x, j.ldx, row, col[k], h, x[k]);
-                row8<T>(j.dh, j.lddh, row, col[k], h, g[k]);
-            }
-            row8<T>(j.y, j.ldy, row, col[k], h, t[k]);
-            plus<T>(t[k], j.bias, col[k], h);
-            if (j.drop) Draw(seed, offset, (uint32_t)row, (uint32_t)col[k] >> 3).apply(t[k], j.drop, j.factor);
-        }
-        if constexpr (POST && PRE) normalise<NV, true>(x, t, rx, rt, hi, j.cols, j.layer, j.eps, sums);
-        else if constexpr (PRE) normalise<NV, false>(x, x, rx, rt, hi, j.cols, j.layer, j.eps, sums);
-        else if constexpr (POST) normalise<NV, false>(t, t, rt, rx, hi, j.cols, j.layer, j.eps, sums);
+    const int64_t step = (int64_t)gridDim.x * G;
+    int64_t base = (int64_t)blockIdx.x * G;
+    Raw8<T> rd[NV], rh[NV], rx[NV], ry[NV];
+    auto fetch = [&](int64_t from) {
+        const int64_t row = min(from + mine, (int64_t)j.rows - 1);
+        if (j.dx_out) c.template fetch<T>(rd, j.dx_out, row * j.lddxo);
         if constexpr (PRE) {
+            c.template fetch<T>(rh, j.dh, row * j.lddh);
+            c.template fetch<T>(rx, j.x, row * j.ldx);
+        }
+        if (j.y) c.template fetch<T>(ry, j.y, row * j.ldy);
+    };
 #pragma unroll
-            for (int k = 0; k < NV; ++k) {
+    for (int k = 0; k < NV; ++k) { rd[k].clear(); ry[k].clear(); }
+    fetch(base);
+    for (; base < j.rows; base += step) {
+        const int64_t row = base + mine;
+        const bool on = row < j.rows;
+        float t[NV][8], x[NV][8], d[NV][8], g[NV][8], rt = 0.f, rr = 0.f;
+        c.template values<T>(rd, d);
+        if constexpr (PRE) {
+            c.template values<T>(rh, g);
+            c.template values<T>(rx, x);
+        }
+        c.template values<T>(ry, t);
+        fetch(base + step);
+        if constexpr (G > 1) {
+            // (a group of threads behind the last row has that row's values again, and adds nothing)
+            if (!on) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    total[AT_PRE][k][e] = on ? fmaf(g[k][e], x[k][e], total[AT_PRE][k][e]) : total[AT_PRE][k][e];
-                    total[AT_PRE + 1][k][e] += g[k][e];
-                }
-                times<T>(g[k], j.pre_w, col[k], hi[k]);
+                for (int k = 0; k < NV; ++k)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) { d[k][e] = 0.f; g[k][e] = 0.f; }
             }
-            norm_back<NV>(g, x, rx, hi, j.cols, j.layer, sums);
+        }
+        bias.plus(t);
+        if (j.drop) {
 #pragma unroll
-            for (int k = 0; k < NV; ++k)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) d[k][e] += g[k][e];
+            for (int k = 0; k < NV; ++k) Draw(seed, offset, (uint32_t)row, (uint32_t)c.col[k] >> 3).apply(t[k], j.drop, j.factor);
+        }
+        if constexpr (POST && PRE) normalise<NV, true>(x, t, rr, rt, c.hi, j.cols, j.layer, j.eps, sums);
+        else if constexpr (PRE) normalise<NV, false>(x, x, rr, rt, c.hi, j.cols, j.layer, j.eps, sums);
+        else if constexpr (POST) normalise<NV, false>(t, t, rt, rr, c.hi, j.cols, j.layer, j.eps, sums);
+        if constexpr (PRE) {
+            add_product<NV>(total[4], g, x);
+            if constexpr (BIASES) add<NV>(total[5], g);
+            pre_w.times(g);
+            norm_back<NV>(g, x, rr, c.hi, j.cols, j.layer, sums);
+            add<NV>(d, g);
         }
         // d: the gradient at x_out and at x; t: D(y + bias), or what the post norm makes of it before its weight
+        if (j.dx && on) c.template put<T>(j.dx, row * j.lddx, d);
+        float n[NV][8];
 #pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            if (on && hi[k] > 0 && j.dx) store8((T*)j.dx + row * j.lddx + col[k], 0, hi[k], d[k]);
-            float n[8];
+        for (int k = 0; k < NV; ++k)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) { d[k][e] = on ? j.scale * d[k][e] : 0.f; n[e] = t[k][e]; }
-            if constexpr (POST) {
-                times<T>(n, j.post_w, col[k], hi[k]);
-                plus<T>(n, j.post_b, col[k], hi[k]);
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) total[1][k][e] = on ? fmaf(d[k][e], n[e], total[1][k][e]) : total[1][k][e];
-            times<T>(d[k], j.gate, col[k], hi[k]);
-            if constexpr (POST) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    total[AT_POST][k][e] = on ? fmaf(d[k][e], t[k][e], total[AT_POST][k][e]) : total[AT_POST][k][e];
-                    total[AT_POST + 1][k][e] += d[k][e];
-                }
-                times<T>(d[k], j.post_w, col[k], hi[k]);
-            }
+            for (int e = 0; e < 8; ++e) { d[k][e] *= j.scale; n[k][e] = t[k][e]; }
+        if constexpr (POST) {
+            post_w.times(n);
+            post_b.plus(n);
         }
-        if constexpr (POST) norm_back<NV>(d, t, rt, hi, j.cols, j.layer, sums);
-#pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            if (j.drop) Draw(seed, offset, (uint32_t)row, (uint32_t)col[k] >> 3).apply(d[k], j.drop, j.factor);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) total[0][k][e] += on ? d[k][e] : 0.f;
-            if (on && hi[k] > 0 && j.dy) store8((T*)j.dy + row * j.lddy + col[k], 0, hi[k], d[k]);
+        add_product<NV>(total[1], d, n);
+        gate.times(d);
+        if constexpr (POST) {
+            add_product<NV>(total[2], d, t);
+            if constexpr (BIASES) add<NV>(total[3], d);
+            post_w.times(d);
+            norm_back<NV>(d, t, rt, c.hi, j.cols, j.layer, sums);
         }
+        if (j.drop) {
+#pragma unroll
+            for (int k = 0; k < NV; ++k) Draw(seed, offset, (uint32_t)row, (uint32_t)c.col[k] >> 3).apply(d[k], j.drop, j.factor);
+        }
+        if constexpr (BIASES) add<NV>(total[0], d);
+        if (j.dy && on) c.template put<T>(j.dy, row * j.lddy, d);
     }
 
     if (!j.partial) return;
     // the G rows' sums of a workgroup, in their order
-    __shared__ float all[G > 1 ? BLOCK * 8 : 1];
+    __shared__ __align__(16) float all[G > 1 ? BLOCK * 8 : 4];
 #pragma unroll
-    for (int s = 0; s < SETS; ++s) {
-        const int at = s < 2 ? s : POST && s < 4 ? s : 4 + (s & 1);
-        float* dst = j.partial + ((size_t)at * (size_t)j.slabs + blockIdx.x) * (size_t)j.cols;
+    for (int s = 0; s < 6; ++s) {
+        if constexpr (!BIASES) { if (s == 0 || s == 3 || s == 5) continue; }
+        if ((s == 2 || s == 3) && !POST) continue;
+        if (s >= 4 && !PRE) continue;
+        float* dst = j.partial + ((size_t)s * (size_t)j.slabs + blockIdx.x) * (size_t)j.cols;
+        if constexpr (G > 1) {
 #pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            float v[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = total[s][k][e];
-            if constexpr (G > 1) {
+            for (int k = 0; k < NV; ++k) {
                 __syncthreads();
-                store8(all + threadIdx.x * 8, 0, 8, v);
+                store8(all + threadIdx.x * 8, 0, 8, total[s][k]);
                 __syncthreads();
-                if (threadIdx.x >= NT) continue;
+                if (threadIdx.x < NT)
 #pragma unroll
-                for (int q = 1; q < G; ++q)
+                    for (int q = 1; q < G; ++q)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] += all[(threadIdx.x + NT * q) * 8 + e];
+                        for (int e = 0; e < 8; ++e) total[s][k][e] += all[(threadIdx.x + NT * q) * 8 + e];
             }
-            if (hi[k] > 0) store8(dst + col[k], 0, hi[k], v);
+            if (threadIdx.x >= NT) continue;
         }
+        c.template put<float>(dst, 0, total[s]);
     }
 }
 
@@ -297,25 +413,29 @@ template <typename T, int NT, int NV, bool BACK>
 int launch_shape(const Join& j, int blocks, hipStream_t stream)
 {
     constexpr int threads = NT * groups_of<NT>();
-    auto go = [&](auto post, auto pre) {
-        constexpr bool POST = decltype(post)::value, PRE = decltype(pre)::value;
-        if constexpr (BACK) hipLaunchKernelGGL((join_back_kernel<T, NT, NV, POST, PRE>), dim3((unsigned)blocks), dim3(threads), 0, stream, j);
+    auto go = [&](auto post, auto pre, auto biases) {
+        constexpr bool POST = decltype(post)::value, PRE = decltype(pre)::value, BIASES = decltype(biases)::value;
+        if constexpr (BACK) hipLaunchKernelGGL((join_back_kernel<T, NT, NV, POST, PRE, BIASES>), dim3((unsigned)blocks), dim3(threads), 0, stream, j);
         else hipLaunchKernelGGL((join_kernel<T, NT, NV, POST, PRE>), dim3((unsigned)blocks), dim3(threads), 0, stream, j);
     };
     const std::true_type yes;
     const std::false_type no;
-    if (j.post && j.pre) go(yes, yes);
-    else if (j.post) go(yes, no);
-    else if (j.pre) go(no, yes);
-    else go(no, no);
+    auto norms = [&](auto biases) {
+        if (j.post && j.pre) go(yes, yes, biases);
+        else if (j.post) go(yes, no, biases);
+        else if (j.pre) go(no, yes, biases);
+        else go(no, no, biases);
+    };
+    if (BACK && j.biases) norms(yes);
+    else norms(no);
     return hip_status(hipGetLastError());
 }
 
-// workgroups of a launch for rows of `cols` columns, `rows_at_once` rows each at a time
+// threads to a row, and rows that a workgroup takes at a time
 struct Shape { int threads, rows_at_once; };
 Shape shape_of(int cols)
 {
-    const int nt = cols <= 1024 ? 64 : cols <= 2048 ? 128 : cols <= 4096 ? 256 : cols <= 8192 ? 512 : 1024;
+    const int nt = cols <= 512 ? 64 : cols <= 1024 ? 128 : cols <= 2048 ? 256 : cols <= 4096 ? 512 : 1024;
     return Shape{nt, nt < 256 ? 256 / nt : 1};
 }
 
@@ -323,28 +443,30 @@ template <bool BACK, typename T>
 int launch_any(const Join& j, int blocks, hipStream_t stream)
 {
     if (j.cols <= 512) return launch_shape<T, 64, 1, BACK>(j, blocks, stream);
-    if (j.cols <= 1024) return launch_shape<T, 64, 2, BACK>(j, blocks, stream);
-    if (j.cols <= 2048) return launch_shape<T, 128, 2, BACK>(j, blocks, stream);
-    if (j.cols <= 4096) return launch_shape<T, 256, 2, BACK>(j, blocks, stream);
-    if (j.cols <= 8192) return launch_shape<T, 512, 2, BACK>(j, blocks, stream);
+    if (j.cols <= 1024) return launch_shape<T, 128, 1, BACK>(j, blocks, stream);
+    if (j.cols <= 2048) return launch_shape<T, 256, 1, BACK>(j, blocks, stream);
+    if (j.cols <= 4096) return launch_shape<T, 512, 1, BACK>(j, blocks, stream);
+    if (j.cols <= 8192) return launch_shape<T, 1024, 1, BACK>(j, blocks, stream);
     return launch_shape<T, 1024, 2, BACK>(j, blocks, stream);
+}
+
+// workgroups of a launch that has so many wavefronts to a compute unit
+int blocks_of(int rows, int cols, int waves_per_unit)
+{
+    const Shape s = shape_of(cols);
+    const int64_t all = ((int64_t)rows + s.rows_at_once - 1) / s.rows_at_once;
+    return (int)std::min<int64_t>(all, std::max(1, 256 * waves_per_unit / (s.threads * s.rows_at_once / 64)));
 }
 
 }  // namespace
 
 int join_max_cols() { return MAX_COLS; }
 
-int join_slabs(int rows, int cols)
-{
-    const Shape s = shape_of(cols);
-    const int64_t all = ((int64_t)rows + s.rows_at_once - 1) / s.rows_at_once;
-    return (int)std::min<int64_t>(all, s.threads <= 256 ? 512 : 256);
-}
+int join_slabs(int rows, int cols) { return blocks_of(rows, cols, 16); }
 
 int launch_join(const Join& j, int dtype, hipStream_t stream)
 {
-    const Shape s = shape_of(j.cols);
-    const int blocks = (int)std::min<int64_t>(((int64_t)j.rows + s.rows_at_once - 1) / s.rows_at_once, 2048);
+    const int blocks = blocks_of(j.rows, j.cols, 16);
     return dtype == ZR_BF16 ? launch_any<false, Bf>(j, blocks, stream) : launch_any<false, float>(j, blocks, stream);
 }
 
