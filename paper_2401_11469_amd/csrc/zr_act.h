@@ -72,7 +72,8 @@ struct Join {
     int biases;                            // a gradient of bias, post_b or pre_b is wanted
 };
 int join_max_cols();
-int join_slabs(int rows, int cols);
+int join_most_slabs(int rows, int cols);                // of any backward call of this size
+int join_slabs(const Join& j);                          // of this one
 int launch_join(const Join& j, int dtype, hipStream_t stream);
 int launch_join_back(const Join& j, int dtype, hipStream_t stream);
 
@@ -197,6 +198,14 @@ struct Draw {
     {
         const uint64_t low = w[0] | (uint64_t)w[1] << 32, high = w[2] | (uint64_t)w[3] << 32;
         return (uint32_t)((e < 4 ? low : high) >> 16 * (e & 3) & 0xffffu) >= drop;
+    }
+    // bit e: element e is kept
+    __device__ __forceinline__ uint32_t bits(uint32_t drop) const
+    {
+        uint32_t b = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) b |= kept(e, drop) ? 1u << e : 0u;
+        return b;
     }
     // a dropped element is +0 whatever it was
     __device__ __forceinline__ void apply(float (&x)[8], uint32_t drop, float factor) const

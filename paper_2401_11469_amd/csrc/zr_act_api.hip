@@ -179,7 +179,7 @@ int zr_block_join_fwd(const void* y, int64_t ldy, const void* x, int64_t ldx, vo
 size_t zr_block_join_workspace_bytes(int32_t rows, int32_t cols)
 {
     if (rows < 1 || cols < 1 || cols > join_max_cols()) return 0;
-    return (size_t)MAX_SUMS * (size_t)join_slabs(rows, cols) * (size_t)cols * 4;
+    return (size_t)MAX_SUMS * (size_t)join_most_slabs(rows, cols) * (size_t)cols * 4;
 }
 
 int zr_block_join_bwd(const void* dx_out, int64_t lddxo, const void* dh, int64_t lddh, const void* x_out, int64_t ldxo,
@@ -214,8 +214,8 @@ int zr_block_join_bwd(const void* dx_out, int64_t lddxo, const void* dh, int64_t
     j.rng = rng; j.factor = kept_factor(j.drop); j.rows = rows; j.cols = cols;
     j.dx_out = dx_out; j.lddxo = lddxo; j.dh = dh; j.lddh = lddh; j.dx = dx; j.lddx = lddx; j.dy = dy; j.lddy = lddy;
     j.partial = vectors ? (float*)workspace : nullptr;
-    j.slabs = join_slabs(rows, cols);
     j.biases = dbias || dpost_b || dpre_b;
+    j.slabs = join_slabs(j);
     hipStream_t s = (hipStream_t)stream;
     st = launch_join_back(j, dtype, s);
     if (st != ZR_OK || !vectors) return st;

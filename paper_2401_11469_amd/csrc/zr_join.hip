@@ -114,42 +114,43 @@ template <int NT, int NV> struct Columns {
     }
 };
 
-// A vector of the row's columns, in registers for all rows; one that is missing stands for `other`.
-template <typename T, int NV> struct Vector {
-    Raw8<T> r[NV];
-    bool there;
-    template <class C> __device__ __forceinline__ Vector(const void* p, const C& c) : there(p != nullptr)
+// A vector of the row's columns; one that is missing changes nothing.  In registers for all rows, or (LEAN: rows of more columns than
+// the registers have room for) read again wherever it is used.
+template <typename T, int NT, int NV, bool LEAN> struct Vector {
+    Raw8<T> r[LEAN ? 1 : NV];
+    const void* p;
+    const Columns<NT, NV>& c;
+    __device__ __forceinline__ Vector(const void* p_, const Columns<NT, NV>& c_) : p(p_), c(c_)
     {
-        if (there) {
-            c.template fetch<T>(r, p, 0);
-            float x[NV][8];
-            c.template values<T>(r, x);
+        if constexpr (!LEAN) {
+            if (p) {
+                c.template fetch<T>(r, p, 0);
+                float x[NV][8];
+                c.template values<T>(r, x);
 #pragma unroll
-            for (int k = 0; k < NV; ++k) r[k].take(x[k]);
+                for (int k = 0; k < NV; ++k) r[k].take(x[k]);
+            }
         }
     }
-    __device__ __forceinline__ void times(float (&x)[NV][8]) const
+    template <class F> __device__ __forceinline__ void with(float (&x)[NV][8], F f) const
     {
-        if (!there) return;
+        if (!p) return;
+        float v[NV][8];
+        if constexpr (LEAN) {
+            Raw8<T> now[NV];
+            c.template fetch<T>(now, p, 0);
+            c.template values<T>(now, v);
+        } else {
 #pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            float v[8];
-            r[k].values(v);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[k][e] *= v[e];
+            for (int k = 0; k < NV; ++k) r[k].values(v[k]);
         }
-    }
-    __device__ __forceinline__ void plus(float (&x)[NV][8]) const
-    {
-        if (!there) return;
 #pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            float v[8];
-            r[k].values(v);
+        for (int k = 0; k < NV; ++k)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[k][e] += v[e];
-        }
+            for (int e = 0; e < 8; ++e) x[k][e] = f(x[k][e], v[k][e]);
     }
+    __device__ __forceinline__ void times(float (&x)[NV][8]) const { with(x, [](float a, float b) { return a * b; }); }
+    __device__ __forceinline__ void plus(float (&x)[NV][8]) const { with(x, [](float a, float b) { return a + b; }); }
 };
 
 // v <- (v - mean) r for both of two rows' worth of values (TWO), or the first alone; r for each
@@ -192,15 +193,17 @@ __device__ __forceinline__ void normalise(float (&u)[NV][8], float (&v)[NV][8], 
 }
 
 template <typename T, int NT, int NV, bool POST, bool PRE>
-__global__ __launch_bounds__(NT * groups_of<NT>(), NT * groups_of<NT>() / 256) void join_kernel(const Join j)
+__global__ __launch_bounds__(NT * groups_of<NT>(), (NT == 640 ? 5 : 4)) void join_kernel(const Join j)
 {
     constexpr int G = groups_of<NT>();
     __shared__ __align__(16) float part[2][2][NT * G / 64];
     RowSums<NT, G> sums{part};
     const Columns<NT, NV> c(j.cols, threadIdx.x % NT);
     const int mine = G == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / NT);        // (a row is a wavefront's or more: scalar addresses)
-    const Vector<T, NV> bias(j.bias, c), gate(j.gate, c), post_w(POST ? j.post_w : nullptr, c), post_b(POST ? j.post_b : nullptr, c);
-    const Vector<T, NV> pre_w(PRE ? j.pre_w : nullptr, c), pre_b(PRE ? j.pre_b : nullptr, c);
+    constexpr bool LEAN = NT * NV > 1024;
+    typedef Vector<T, NT, NV, LEAN> V;
+    const V bias(j.bias, c), gate(j.gate, c), post_w(POST ? j.post_w : nullptr, c), post_b(POST ? j.post_b : nullptr, c);
+    const V pre_w(PRE ? j.pre_w : nullptr, c), pre_b(PRE ? j.pre_b : nullptr, c);
     uint64_t seed = 0, offset = 0;
     if (j.drop) { seed = j.rng[0]; offset = j.rng[1]; }
     const int64_t step = (int64_t)gridDim.x * G;
@@ -211,15 +214,16 @@ __global__ __launch_bounds__(NT * groups_of<NT>(), NT * groups_of<NT>() / 256) v
         c.template fetch<T>(ry, j.y, row * j.ldy);
         c.template fetch<T>(rx, j.x, row * j.ldx);
     };
-    fetch(base);
+    if constexpr (!LEAN) fetch(base);
     for (; base < j.rows; base += step) {
+        if constexpr (LEAN) fetch(base);
         const int64_t row = base + mine;
         const bool on = row < j.rows;
         float t[NV][8], x[NV][8], r, unused;
         c.template values<T>(ry, t);
         c.template values<T>(rx, x);
         // the next row's values travel while this one's are used (past the last row: the last one's again)
-        fetch(base + step);
+        if constexpr (!LEAN) fetch(base + step);
         bias.plus(t);
         if (j.drop) {
 #pragma unroll
@@ -280,20 +284,25 @@ template <int NV> __device__ __forceinline__ void add(float (&total)[NV][8], con
 }
 
 // wavefronts to a SIMD that the registers have to leave room for
-template <int NT, int NV, bool BIASES> constexpr int back_waves() { return NT * NV > 1024 ? 4 : BIASES ? 2 : NT <= 256 ? 3 : 2; }
+template <typename T, int NT, bool POST, bool PRE, bool BIASES> constexpr int back_waves()
+{
+    return NT > 640 ? 4 : NT > 512 ? 3 : NT == 512 || BIASES || (POST && PRE && sizeof(T) == 4) ? 2 : 3;
+}
 
 // BIASES: gradients of bias, post_b or pre_b are wanted (without them a third of the registers for sums goes, and two rows of up to
 // 4096 columns fit a compute unit at a time)
 template <typename T, int NT, int NV, bool POST, bool PRE, bool BIASES>
-__global__ __launch_bounds__(NT * groups_of<NT>(), (back_waves<NT, NV, BIASES>())) void join_back_kernel(const Join j)
+__global__ __launch_bounds__(NT * groups_of<NT>(), (back_waves<T, NT, POST, PRE, BIASES>())) void join_back_kernel(const Join j)
 {
     constexpr int G = groups_of<NT>(), BLOCK = NT * G;
     __shared__ __align__(16) float part[2][2][BLOCK / 64];
     RowSums<NT, G> sums{part};
     const Columns<NT, NV> c(j.cols, threadIdx.x % NT);
     const int mine = G == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / NT);        // (a row is a wavefront's or more: scalar addresses)
-    const Vector<T, NV> bias(j.bias, c), gate(j.gate, c), post_w(POST ? j.post_w : nullptr, c), post_b(POST ? j.post_b : nullptr, c);
-    const Vector<T, NV> pre_w(PRE ? j.pre_w : nullptr, c);
+    constexpr bool LEAN = NT * NV > 640 || (NT == 640 && sizeof(T) == 4);
+    typedef Vector<T, NT, NV, LEAN> V;
+    const V bias(j.bias, c), gate(j.gate, c), post_w(POST ? j.post_w : nullptr, c), post_b(POST ? j.post_b : nullptr, c);
+    const V pre_w(PRE ? j.pre_w : nullptr, c);
     uint64_t seed = 0, offset = 0;
     if (j.drop) { seed = j.rng[0]; offset = j.rng[1]; }
     // gradients of the vectors, where their sums lie in j.partial: bias, gate, weight and bias of the post norm, of the pre norm
@@ -319,8 +328,9 @@ __global__ __launch_bounds__(NT * groups_of<NT>(), (back_waves<NT, NV, BIASES>()
     };
 #pragma unroll
     for (int k = 0; k < NV; ++k) { rd[k].clear(); ry[k].clear(); }
-    fetch(base);
+    if constexpr (!LEAN) fetch(base);
     for (; base < j.rows; base += step) {
+        if constexpr (LEAN) fetch(base);
         const int64_t row = base + mine;
         const bool on = row < j.rows;
         float t[NV][8], x[NV][8], d[NV][8], g[NV][8], rt = 0.f, rr = 0.f;
@@ -330,7 +340,7 @@ __global__ __launch_bounds__(NT * groups_of<NT>(), (back_waves<NT, NV, BIASES>()
             c.template values<T>(rx, x);
         }
         c.template values<T>(ry, t);
-        fetch(base + step);
+        if constexpr (!LEAN) fetch(base + step);
         if constexpr (G > 1) {
             // (a group of threads behind the last row has that row's values again, and adds nothing)
             if (!on) {
@@ -341,9 +351,17 @@ __global__ __launch_bounds__(NT * groups_of<NT>(), (back_waves<NT, NV, BIASES>()
             }
         }
         bias.plus(t);
+        uint32_t kept[NV];
+        auto drop = [&](float (&v)[NV][8]) {
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[k][e] = kept[k] >> e & 1 ? v[k][e] * j.factor : 0.f;
+        };
         if (j.drop) {
 #pragma unroll
-            for (int k = 0; k < NV; ++k) Draw(seed, offset, (uint32_t)row, (uint32_t)c.col[k] >> 3).apply(t[k], j.drop, j.factor);
+            for (int k = 0; k < NV; ++k) kept[k] = Draw(seed, offset, (uint32_t)row, (uint32_t)c.col[k] >> 3).bits(j.drop);
+            drop(t);
         }
         if constexpr (POST && PRE) normalise<NV, true>(x, t, rr, rt, c.hi, j.cols, j.layer, j.eps, sums);
         else if constexpr (PRE) normalise<NV, false>(x, x, rr, rt, c.hi, j.cols, j.layer, j.eps, sums);
@@ -374,10 +392,7 @@ __global__ __launch_bounds__(NT * groups_of<NT>(), (back_waves<NT, NV, BIASES>()
             post_w.times(d);
             norm_back<NV>(d, t, rt, c.hi, j.cols, j.layer, sums);
         }
-        if (j.drop) {
-#pragma unroll
-            for (int k = 0; k < NV; ++k) Draw(seed, offset, (uint32_t)row, (uint32_t)c.col[k] >> 3).apply(d[k], j.drop, j.factor);
-        }
+        if (j.drop) drop(d);
         if constexpr (BIASES) add<NV>(total[0], d);
         if (j.dy && on) c.template put<T>(j.dy, row * j.lddy, d);
     }
@@ -426,53 +441,75 @@ int launch_shape(const Join& j, int blocks, hipStream_t stream)
         else if (j.pre) go(no, yes, biases);
         else go(no, no, biases);
     };
-    if (BACK && j.biases) norms(yes);
-    else norms(no);
+    if constexpr (!BACK) {
+        if constexpr (NT * NV == 1024 && NT == 512) return ZR_ERR_SHAPE;       // (a shape of the backward pass)
+        else norms(no);
+    } else if constexpr (NT == 512 && NV == 2) {
+        norms(yes);
+    } else if constexpr (NT == 640 || (NT == 1024 && NV == 1)) {
+        norms(no);
+    } else {
+        if (j.biases) norms(yes);
+        else norms(no);
+    }
     return hip_status(hipGetLastError());
 }
 
-// threads to a row, and rows that a workgroup takes at a time
-struct Shape { int threads, rows_at_once; };
+// Threads to a row, rows that a workgroup takes at a time, and workgroups to a compute unit, which is how many of them its registers
+// hold: a launch is that many, each with its share of the rows.  (Backward, 8192 x 4096, two norms, us by wavefronts to a unit: 8
+// 98, 12 127, 16 105, 24 112; 12608 x 1024: 43, 42, 50, 48.)
+struct Shape { int threads, rows_at_once, per_unit; };
 Shape shape_of(int cols)
 {
-    const int nt = cols <= 512 ? 64 : cols <= 1024 ? 128 : cols <= 2048 ? 256 : cols <= 4096 ? 512 : 1024;
-    return Shape{nt, nt < 256 ? 256 / nt : 1};
+    const int nt = cols <= 512 ? 64 : cols <= 1024 ? 128 : cols <= 2048 ? 256 : cols <= 4096 ? 512 : cols <= 5120 ? 640 : 1024;
+    return Shape{nt, nt < 256 ? 256 / nt : 1, nt <= 256 ? 4 : nt <= 640 ? 2 : 1};
+}
+Shape back_shape_of(const Join& j)
+{
+    Shape s = shape_of(j.cols);
+    if (s.threads <= 256) s.per_unit = j.biases ? 2 : 3;
+    else if (s.threads == 512) s.per_unit = j.biases || (j.post && j.pre) ? 1 : 2;
+    else s.per_unit = 1;
+    // six vectors' sums of more than 4096 columns: two groups to a thread of twice the registers
+    if (j.biases && j.cols > 4096 && j.cols <= 8192) s.threads = 512;
+    return s;
+}
+int blocks_of(int rows, const Shape& s)
+{
+    return (int)std::min<int64_t>(((int64_t)rows + s.rows_at_once - 1) / s.rows_at_once, 256 * s.per_unit);
 }
 
 template <bool BACK, typename T>
-int launch_any(const Join& j, int blocks, hipStream_t stream)
+int launch_any(const Join& j, const Shape& s, int blocks, hipStream_t stream)
 {
-    if (j.cols <= 512) return launch_shape<T, 64, 1, BACK>(j, blocks, stream);
-    if (j.cols <= 1024) return launch_shape<T, 128, 1, BACK>(j, blocks, stream);
-    if (j.cols <= 2048) return launch_shape<T, 256, 1, BACK>(j, blocks, stream);
-    if (j.cols <= 4096) return launch_shape<T, 512, 1, BACK>(j, blocks, stream);
-    if (j.cols <= 8192) return launch_shape<T, 1024, 1, BACK>(j, blocks, stream);
-    return launch_shape<T, 1024, 2, BACK>(j, blocks, stream);
-}
-
-// workgroups of a launch that has so many wavefronts to a compute unit
-int blocks_of(int rows, int cols, int waves_per_unit)
-{
-    const Shape s = shape_of(cols);
-    const int64_t all = ((int64_t)rows + s.rows_at_once - 1) / s.rows_at_once;
-    return (int)std::min<int64_t>(all, std::max(1, 256 * waves_per_unit / (s.threads * s.rows_at_once / 64)));
+    switch (s.threads) {
+        case 64: return launch_shape<T, 64, 1, BACK>(j, blocks, stream);
+        case 128: return launch_shape<T, 128, 1, BACK>(j, blocks, stream);
+        case 256: return launch_shape<T, 256, 1, BACK>(j, blocks, stream);
+        case 512: return j.cols <= 4096 ? launch_shape<T, 512, 1, BACK>(j, blocks, stream) : launch_shape<T, 512, 2, BACK>(j, blocks, stream);
+        case 640: return launch_shape<T, 640, 1, BACK>(j, blocks, stream);
+        default: return j.cols <= 8192 ? launch_shape<T, 1024, 1, BACK>(j, blocks, stream) : launch_shape<T, 1024, 2, BACK>(j, blocks, stream);
+    }
 }
 
 }  // namespace
 
 int join_max_cols() { return MAX_COLS; }
 
-int join_slabs(int rows, int cols) { return blocks_of(rows, cols, 16); }
+int join_most_slabs(int rows, int cols) { return blocks_of(rows, shape_of(cols)); }
+int join_slabs(const Join& j) { return blocks_of(j.rows, back_shape_of(j)); }
 
 int launch_join(const Join& j, int dtype, hipStream_t stream)
 {
-    const int blocks = blocks_of(j.rows, j.cols, 16);
-    return dtype == ZR_BF16 ? launch_any<false, Bf>(j, blocks, stream) : launch_any<false, float>(j, blocks, stream);
+    const Shape s = shape_of(j.cols);
+    const int blocks = blocks_of(j.rows, s);
+    return dtype == ZR_BF16 ? launch_any<false, Bf>(j, s, blocks, stream) : launch_any<false, float>(j, s, blocks, stream);
 }
 
 int launch_join_back(const Join& j, int dtype, hipStream_t stream)
 {
-    return dtype == ZR_BF16 ? launch_any<true, Bf>(j, j.slabs, stream) : launch_any<true, float>(j, j.slabs, stream);
+    const Shape s = back_shape_of(j);
+    return dtype == ZR_BF16 ? launch_any<true, Bf>(j, s, j.slabs, stream) : launch_any<true, float>(j, s, j.slabs, stream);
 }
 
 }  // namespace zr
