@@ -78,6 +78,8 @@ int launch_join(const Join& j, int dtype, hipStream_t stream);
 int launch_join_back(const Join& j, int dtype, hipStream_t stream);
 
 // products with a Finish (GemmDesc::finish set): any alignment, and fp32
+constexpr int ACT_FEW = 16;     // rows of X up to which launch_act_few takes a product
+int launch_act_few(const GemmDesc& d, hipStream_t stream);      // bf16, few rows; -1: not taken
 int launch_act_any(const GemmDesc& d, hipStream_t stream);
 int launch_act_fast(const GemmDesc& d, hipStream_t stream);     // bf16, 16-byte aligned rows; -1: not taken
 int launch_act_f32(const GemmDesc& d, hipStream_t stream);

@@ -2,6 +2,7 @@
 // products (paper Sec. 3.1) onto the canonical gather-fused GEMM.
 #include <cmath>
 
+#include "zr_act.h"
 #include "zr_common.h"
 
 using namespace zr;
@@ -308,7 +309,9 @@ int resized_linear_fwd(const void* X, int64_t ldx, const void* W, int64_t ldw, v
     d.B = weight_fwd(W, ldw, K, N, mode, w_layout, S);
     if (mode == ZR_DROP_K) {
         // Y[m,j] = sum_{c<n'} X[m,S[c]] * W[S[c],j]
-        const Extract ex = plan_extract(X, ldx, M, K, n_keep, dtype, workspace, workspace_bytes);
+        // (a few rows with an end of their own are gathered on the way: another launch would cost more)
+        Extract ex{false, 0};
+        if (!finish || M > ACT_FEW) ex = plan_extract(X, ldx, M, K, n_keep, dtype, workspace, workspace_bytes);
         if (ex.use) {
             st = launch_compact_cols(X, ldx, M, K, keep_idx, n_keep, workspace, ex.width, ex.width, s);
             if (st != ZR_OK) return st;

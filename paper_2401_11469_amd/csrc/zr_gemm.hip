@@ -210,7 +210,8 @@ bool ensure_max_dynamic_lds(const void* fn, int bytes, void* flags16)
 static int launch_gemm_untimed(const GemmDesc& d, hipStream_t stream)
 {
     if (d.finish) {
-        const int st = launch_act_fast(d, stream);
+        int st = launch_act_few(d, stream);
+        if (st < 0) st = launch_act_fast(d, stream);
         if (st >= 0) return st;
         return d.dtype == ZR_BF16 ? launch_act_any(d, stream) : d.dtype == ZR_F32 ? launch_act_f32(d, stream) : ZR_ERR_DTYPE;
     }

@@ -193,7 +193,7 @@ __device__ __forceinline__ void normalise(float (&u)[NV][8], float (&v)[NV][8], 
 }
 
 template <typename T, int NT, int NV, bool POST, bool PRE>
-__global__ __launch_bounds__(NT * groups_of<NT>(), (NT == 640 ? 5 : 4)) void join_kernel(const Join j)
+__global__ __launch_bounds__(NT * groups_of<NT>(), 4) void join_kernel(const Join j)
 {
     constexpr int G = groups_of<NT>();
     __shared__ __align__(16) float part[2][2][NT * G / 64];
@@ -306,6 +306,27 @@ __global__ __launch_bounds__(NT * groups_of<NT>(), (back_waves<T, NT, POST, PRE,
     uint64_t seed = 0, offset = 0;
     if (j.drop) { seed = j.rng[0]; offset = j.rng[1]; }
     // gradients of the vectors, where their sums lie in j.partial: bias, gate, weight and bias of the post norm, of the pre norm
+    // (IN_LDS: those of the biases of wide rows lie in LDS, four columns of every thread side by side)
+    constexpr bool IN_LDS = BIASES && NT > 512 && NV == 1;
+    extern __shared__ __align__(16) float biases[];
+    auto add_bias = [&](int s, float (&sum)[NV][8], const float (&v)[NV][8]) {
+        if constexpr (!IN_LDS) {
+            add<NV>(sum, v);
+        } else {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                f4* at = (f4*)(biases + ((s * 2 + h) * NT + threadIdx.x) * 4);
+                f4 old = *at;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) old[e] += v[0][4 * h + e];
+                *at = old;
+            }
+        }
+    };
+    if constexpr (IN_LDS) {
+#pragma unroll
+        for (int q = 0; q < 6; ++q) *(f4*)(biases + (q * NT + threadIdx.x) * 4) = f4{0.f, 0.f, 0.f, 0.f};
+    }
     float total[6][NV][8];
 #pragma unroll
     for (int s = 0; s < 6; ++s)
@@ -368,7 +389,7 @@ __global__ __launch_bounds__(NT * groups_of<NT>(), (back_waves<T, NT, POST, PRE,
         else if constexpr (POST) normalise<NV, false>(t, t, rt, rr, c.hi, j.cols, j.layer, j.eps, sums);
         if constexpr (PRE) {
             add_product<NV>(total[4], g, x);
-            if constexpr (BIASES) add<NV>(total[5], g);
+            if constexpr (BIASES) add_bias(2, total[5], g);
             pre_w.times(g);
             norm_back<NV>(g, x, rr, c.hi, j.cols, j.layer, sums);
             add<NV>(d, g);
@@ -388,16 +409,26 @@ __global__ __launch_bounds__(NT * groups_of<NT>(), (back_waves<T, NT, POST, PRE,
         gate.times(d);
         if constexpr (POST) {
             add_product<NV>(total[2], d, t);
-            if constexpr (BIASES) add<NV>(total[3], d);
+            if constexpr (BIASES) add_bias(1, total[3], d);
             post_w.times(d);
             norm_back<NV>(d, t, rt, c.hi, j.cols, j.layer, sums);
         }
         if (j.drop) drop(d);
-        if constexpr (BIASES) add<NV>(total[0], d);
+        if constexpr (BIASES) add_bias(0, total[0], d);
         if (j.dy && on) c.template put<T>(j.dy, row * j.lddy, d);
     }
 
     if (!j.partial) return;
+    if constexpr (IN_LDS) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                total[0][0][4 * h + e] = biases[(h * NT + threadIdx.x) * 4 + e];
+                total[3][0][4 * h + e] = biases[((2 + h) * NT + threadIdx.x) * 4 + e];
+                total[5][0][4 * h + e] = biases[((4 + h) * NT + threadIdx.x) * 4 + e];
+            }
+    }
     // the G rows' sums of a workgroup, in their order
     __shared__ __align__(16) float all[G > 1 ? BLOCK * 8 : 4];
 #pragma unroll
@@ -428,9 +459,18 @@ template <typename T, int NT, int NV, bool BACK>
 int launch_shape(const Join& j, int blocks, hipStream_t stream)
 {
     constexpr int threads = NT * groups_of<NT>();
+    bool ok = true;
     auto go = [&](auto post, auto pre, auto biases) {
         constexpr bool POST = decltype(post)::value, PRE = decltype(pre)::value, BIASES = decltype(biases)::value;
-        if constexpr (BACK) hipLaunchKernelGGL((join_back_kernel<T, NT, NV, POST, PRE, BIASES>), dim3((unsigned)blocks), dim3(threads), 0, stream, j);
+        if constexpr (BACK) {
+            constexpr int lds = BIASES && NT > 512 && NV == 1 ? 6 * NT * 16 : 0;
+            const auto fn = join_back_kernel<T, NT, NV, POST, PRE, BIASES>;
+            if constexpr (lds > 0) {
+                static AttrFlags attr_set;
+                if (!ensure_max_dynamic_lds((const void*)fn, lds, &attr_set)) { ok = false; return; }
+            }
+            hipLaunchKernelGGL(fn, dim3((unsigned)blocks), dim3(threads), lds, stream, j);
+        }
         else hipLaunchKernelGGL((join_kernel<T, NT, NV, POST, PRE>), dim3((unsigned)blocks), dim3(threads), 0, stream, j);
     };
     const std::true_type yes;
@@ -441,22 +481,16 @@ int launch_shape(const Join& j, int blocks, hipStream_t stream)
         else if (j.pre) go(no, yes, biases);
         else go(no, no, biases);
     };
-    if constexpr (!BACK) {
-        if constexpr (NT * NV == 1024 && NT == 512) return ZR_ERR_SHAPE;       // (a shape of the backward pass)
-        else norms(no);
-    } else if constexpr (NT == 512 && NV == 2) {
-        norms(yes);
-    } else if constexpr (NT == 640 || (NT == 1024 && NV == 1)) {
-        norms(no);
-    } else {
-        if (j.biases) norms(yes);
-        else norms(no);
-    }
+    if constexpr (!BACK) norms(no);
+    else if constexpr (NT * NV == 1024) { if (j.biases == (NT == 512)) norms(std::integral_constant<bool, NT == 512>()); else return ZR_ERR_SHAPE; }
+    else if (j.biases) norms(yes);
+    else norms(no);
+    if (!ok) return ZR_ERR_HIP;
     return hip_status(hipGetLastError());
 }
 
-// Threads to a row, rows that a workgroup takes at a time, and workgroups to a compute unit, which is how many of them its registers
-// hold: a launch is that many, each with its share of the rows.  (Backward, 8192 x 4096, two norms, us by wavefronts to a unit: 8
+// Threads to a row (a group of eight columns each, two in the widest rows), rows that a workgroup takes at a time, and workgroups to a
+// compute unit, which is how many of them its registers hold: a launch is that many, each with its share of the rows.  (Backward, 8192 x 4096, two norms, us by wavefronts to a unit: 8
 // 98, 12 127, 16 105, 24 112; 12608 x 1024: 43, 42, 50, 48.)
 struct Shape { int threads, rows_at_once, per_unit; };
 Shape shape_of(int cols)
@@ -470,8 +504,9 @@ Shape back_shape_of(const Join& j)
     if (s.threads <= 256) s.per_unit = j.biases ? 2 : 3;
     else if (s.threads == 512) s.per_unit = j.biases || (j.post && j.pre) ? 1 : 2;
     else s.per_unit = 1;
-    // six vectors' sums of more than 4096 columns: two groups to a thread of twice the registers
-    if (j.biases && j.cols > 4096 && j.cols <= 8192) s.threads = 512;
+    // six vectors' sums: two groups of columns to a thread of twice the registers (4096 x 8192, layer norms, dropout, all gradients:
+    // 171 us, 204 on 1024 threads with three of the sums in LDS; 8192 x 5120 on 640 threads 288 and 218)
+    if (j.biases && j.cols > 5120 && j.cols <= 8192) s.threads = 512;
     return s;
 }
 int blocks_of(int rows, const Shape& s)
@@ -486,7 +521,10 @@ int launch_any(const Join& j, const Shape& s, int blocks, hipStream_t stream)
         case 64: return launch_shape<T, 64, 1, BACK>(j, blocks, stream);
         case 128: return launch_shape<T, 128, 1, BACK>(j, blocks, stream);
         case 256: return launch_shape<T, 256, 1, BACK>(j, blocks, stream);
-        case 512: return j.cols <= 4096 ? launch_shape<T, 512, 1, BACK>(j, blocks, stream) : launch_shape<T, 512, 2, BACK>(j, blocks, stream);
+        case 512:
+            if constexpr (BACK)
+                if (j.cols > 4096) return launch_shape<T, 512, 2, true>(j, blocks, stream);
+            return launch_shape<T, 512, 1, BACK>(j, blocks, stream);
         case 640: return launch_shape<T, 640, 1, BACK>(j, blocks, stream);
         default: return j.cols <= 8192 ? launch_shape<T, 1024, 1, BACK>(j, blocks, stream) : launch_shape<T, 1024, 2, BACK>(j, blocks, stream);
     }
