@@ -47,6 +47,7 @@ int launch_act_back(const ActBack& a, int dtype, hipStream_t stream);
 // out[v][c] = sum over slabs of partial[(v * slabs + slab) * n + c], in slab order, for `vectors` of them (out[v] nullptr: skipped)
 constexpr int MAX_SUMS = 6;
 struct SumOut { void* out[MAX_SUMS]; };
+enum { SUM_BIAS, SUM_GATE, SUM_POST_W, SUM_POST_B, SUM_PRE_W, SUM_PRE_B };       // of a join's vectors
 int launch_sum_slabs(const float* partial, int slabs, int n, int vectors, const SumOut& out, int dtype, hipStream_t stream);
 int launch_dropout(const void* x, int64_t ldx, void* out, int64_t ldo, int rows, int cols, const uint64_t* rng, uint32_t drop,
                    float factor, int dtype, hipStream_t stream);
@@ -69,7 +70,7 @@ struct Join {
     void* dy; int64_t lddy;
     float* partial;                        // [vectors x slabs x cols]
     int slabs;
-    int biases;                            // a gradient of bias, post_b or pre_b is wanted
+    int biases;                            // sums of d, dh or dy are wanted: a gradient of bias, post_b or pre_b, or of the gate beside a post_b
 };
 int join_max_cols();
 int join_most_slabs(int rows, int cols);                // of any backward call of this size
@@ -79,6 +80,7 @@ int launch_join_back(const Join& j, int dtype, hipStream_t stream);
 
 // products with a Finish (GemmDesc::finish set): any alignment, and fp32
 constexpr int ACT_FEW = 16;     // rows of X up to which launch_act_few takes a product
+constexpr int ACT_FEW_GATHERED = 4;     // and up to which it is left to gather the kept columns of X
 int launch_act_few(const GemmDesc& d, hipStream_t stream);      // bf16, few rows; -1: not taken
 int launch_act_any(const GemmDesc& d, hipStream_t stream);
 int launch_act_fast(const GemmDesc& d, hipStream_t stream);     // bf16, 16-byte aligned rows; -1: not taken

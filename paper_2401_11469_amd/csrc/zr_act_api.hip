@@ -214,7 +214,7 @@ int zr_block_join_bwd(const void* dx_out, int64_t lddxo, const void* dh, int64_t
     j.rng = rng; j.factor = kept_factor(j.drop); j.rows = rows; j.cols = cols;
     j.dx_out = dx_out; j.lddxo = lddxo; j.dh = dh; j.lddh = lddh; j.dx = dx; j.lddx = lddx; j.dy = dy; j.lddy = lddy;
     j.partial = vectors ? (float*)workspace : nullptr;
-    j.biases = dbias || dpost_b || dpre_b;
+    j.biases = dbias || dpost_b || dpre_b || (dgate && post && post_b);
     j.slabs = join_slabs(j);
     hipStream_t s = (hipStream_t)stream;
     st = launch_join_back(j, dtype, s);

@@ -309,9 +309,9 @@ int resized_linear_fwd(const void* X, int64_t ldx, const void* W, int64_t ldw, v
     d.B = weight_fwd(W, ldw, K, N, mode, w_layout, S);
     if (mode == ZR_DROP_K) {
         // Y[m,j] = sum_{c<n'} X[m,S[c]] * W[S[c],j]
-        // (a few rows with an end of their own are gathered on the way: another launch would cost more)
+        // (a few rows with an end of their own are gathered on the way: 1 x 2752 x 4096 of 2064 kept 11 us, but 16 rows 29, 11 after it)
         Extract ex{false, 0};
-        if (!finish || M > ACT_FEW) ex = plan_extract(X, ldx, M, K, n_keep, dtype, workspace, workspace_bytes);
+        if (!finish || M > ACT_FEW_GATHERED) ex = plan_extract(X, ldx, M, K, n_keep, dtype, workspace, workspace_bytes);
         if (ex.use) {
             st = launch_compact_cols(X, ldx, M, K, keep_idx, n_keep, workspace, ex.width, ex.width, s);
             if (st != ZR_OK) return st;

@@ -50,6 +50,19 @@ template <int NT, int G> struct RowSums {
             place ^= 1;
         }
     }
+    __device__ __forceinline__ void one(float& a)
+    {
+        a = wave_sum(a);
+        if constexpr (WAVES > 1) {
+            const int wave = threadIdx.x >> 6, first = wave / WAVES * WAVES;
+            if ((threadIdx.x & 63) == 0) part[place][0][wave] = a;
+            __syncthreads();
+            a = 0.f;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) a += part[place][0][first + w];
+            place ^= 1;
+        }
+    }
 };
 
 // rows that a workgroup takes at a time
@@ -153,9 +166,19 @@ template <typename T, int NT, int NV, bool LEAN> struct Vector {
     __device__ __forceinline__ void plus(float (&x)[NV][8]) const { with(x, [](float a, float b) { return a + b; }); }
 };
 
+// 0 past the row's end
+template <int NV, class C> __device__ __forceinline__ void mask(float (&x)[NV][8], const C& c)
+{
+    if (!c.edge) return;
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[k][e] = e < c.hi[k] ? x[k][e] : 0.f;
+}
+
 // v <- (v - mean) r for both of two rows' worth of values (TWO), or the first alone; r for each
-template <int NV, bool TWO, class S>
-__device__ __forceinline__ void normalise(float (&u)[NV][8], float (&v)[NV][8], float& ru, float& rv, const int (&hi)[NV], int cols,
+template <int NV, bool TWO, class C, class S>
+__device__ __forceinline__ void normalise(float (&u)[NV][8], float (&v)[NV][8], float& ru, float& rv, const C& c, int cols,
                                           int layer, float eps, S& sums)
 {
     const float inv = 1.f / (float)cols;
@@ -171,9 +194,11 @@ __device__ __forceinline__ void normalise(float (&u)[NV][8], float (&v)[NV][8], 
         for (int k = 0; k < NV; ++k)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                u[k][e] = e < hi[k] ? u[k][e] - a : 0.f;
-                if constexpr (TWO) v[k][e] = e < hi[k] ? v[k][e] - b : 0.f;
+                u[k][e] -= a;
+                if constexpr (TWO) v[k][e] -= b;
             }
+        mask<NV>(u, c);
+        if constexpr (TWO) mask<NV>(v, c);
     }
     float a = 0.f, b = 0.f;
 #pragma unroll
@@ -230,7 +255,7 @@ __global__ __launch_bounds__(NT * groups_of<NT>(), 4) void join_kernel(const Joi
             for (int k = 0; k < NV; ++k) Draw(seed, offset, (uint32_t)row, (uint32_t)c.col[k] >> 3).apply(t[k], j.drop, j.factor);
         }
         if constexpr (POST) {
-            normalise<NV, false>(t, t, r, unused, c.hi, j.cols, j.layer, j.eps, sums);
+            normalise<NV, false>(t, t, r, unused, c, j.cols, j.layer, j.eps, sums);
             post_w.times(t);
             post_b.plus(t);
         }
@@ -242,7 +267,7 @@ __global__ __launch_bounds__(NT * groups_of<NT>(), 4) void join_kernel(const Joi
         if (on) c.template put<T>(j.x_out, row * j.ldxo, x);
         if constexpr (PRE) {
             // (of the sums as they are, before they are rounded into x_out; columns past the end are zeros all the way)
-            normalise<NV, false>(x, x, r, unused, c.hi, j.cols, j.layer, j.eps, sums);
+            normalise<NV, false>(x, x, r, unused, c, j.cols, j.layer, j.eps, sums);
             pre_w.times(x);
             pre_b.plus(x);
             if (on) c.template put<T>(j.h, row * j.ldh, x);
@@ -250,22 +275,23 @@ __global__ __launch_bounds__(NT * groups_of<NT>(), 4) void join_kernel(const Joi
     }
 }
 
-// The gradient at the values of a norm: g <- r (g - hat mean(g hat) [- mean(g)]); 0 past the row's end, where g and hat are
-template <int NV, class S>
-__device__ __forceinline__ void norm_back(float (&g)[NV][8], const float (&hat)[NV][8], float r, const int (&hi)[NV], int cols, int layer, S& sums)
+// With a = mean(g hat) and b = mean(g) (layer norms; else 0), the gradient at the values of a norm is r (g - b - hat a) =
+// r g - (b r) - hat (a r).  a r and b r:
+template <int NV, bool LAYER, class S>
+__device__ __forceinline__ void norm_back(const float (&g)[NV][8], const float (&hat)[NV][8], float r, int cols, float& ar, float& br, S& sums)
 {
     float a = 0.f, b = 0.f;
 #pragma unroll
     for (int k = 0; k < NV; ++k)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) { a = fmaf(g[k][e], hat[k][e], a); b += g[k][e]; }
-    sums.two(a, b);
-    a /= (float)cols;
-    b = layer ? b / (float)cols : 0.f;
-#pragma unroll
-    for (int k = 0; k < NV; ++k)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) g[k][e] = e < hi[k] ? r * (g[k][e] - b - hat[k][e] * a) : 0.f;
+        for (int e = 0; e < 8; ++e) {
+            a = fmaf(g[k][e], hat[k][e], a);
+            if constexpr (LAYER) b += g[k][e];
+        }
+    if constexpr (LAYER) sums.two(a, b);
+    else sums.one(a);
+    ar = a / (float)cols * r;
+    br = b / (float)cols * r;
 }
 
 template <int NV> __device__ __forceinline__ void add_product(float (&total)[NV][8], const float (&a)[NV][8], const float (&b)[NV][8])
@@ -283,57 +309,87 @@ template <int NV> __device__ __forceinline__ void add(float (&total)[NV][8], con
         for (int e = 0; e < 8; ++e) total[k][e] += a[k][e];
 }
 
-// wavefronts to a SIMD that the registers have to leave room for
-template <typename T, int NT, bool POST, bool PRE, bool BIASES> constexpr int back_waves()
+// A vector's values, `other` where it is missing
+template <typename T, int NV, class C> __device__ __forceinline__ void vector_of(float (&x)[NV][8], const void* p, float other, const C& c)
 {
-    return NT > 640 ? 4 : NT > 512 ? 3 : NT == 512 || BIASES || (POST && PRE && sizeof(T) == 4) ? 2 : 3;
+    if (p) {
+        Raw8<T> r[NV];
+        c.template fetch<T>(r, p, 0);
+        c.template values<T>(r, x);
+    } else {
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[k][e] = other;
+    }
 }
 
-// BIASES: gradients of bias, post_b or pre_b are wanted (without them a third of the registers for sums goes, and two rows of up to
-// 4096 columns fit a compute unit at a time)
-template <typename T, int NT, int NV, bool POST, bool PRE, bool BIASES>
-__global__ __launch_bounds__(NT * groups_of<NT>(), (back_waves<T, NT, POST, PRE, BIASES>())) void join_back_kernel(const Join j)
+// wavefronts to a SIMD that the registers have to leave room for
+template <typename T, int NT, bool BIASES> constexpr int back_waves()
+{
+    return NT > 640 ? 4 : NT > 512 ? 3 : NT == 512 || BIASES ? 2 : 3;
+}
+
+// With d the gradient at x_out, which is the one at x, and t = D(y + bias) or, behind a post norm, its normalised value:
+//   dgate = scale (post_w A + post_b B),  dpost_w = scale gate A,  dpost_b = scale gate B,   A = sum d t,  B = sum d  over the rows,
+// and what the post norm passes back is scale times its gradient for d gate post_w: two sums and one product for an element where
+// the formulas have three and four.
+// BIASES: B, or a gradient of bias or pre_b, is wanted.
+template <typename T, int NT, int NV, bool POST, bool PRE, bool LAYER, bool BIASES>
+__global__ __launch_bounds__(NT * groups_of<NT>(), (back_waves<T, NT, BIASES>())) void join_back_kernel(const Join j)
 {
     constexpr int G = groups_of<NT>(), BLOCK = NT * G;
     __shared__ __align__(16) float part[2][2][BLOCK / 64];
     RowSums<NT, G> sums{part};
     const Columns<NT, NV> c(j.cols, threadIdx.x % NT);
     const int mine = G == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / NT);        // (a row is a wavefront's or more: scalar addresses)
-    constexpr bool LEAN = NT * NV > 640 || (NT == 640 && sizeof(T) == 4);
-    typedef Vector<T, NT, NV, LEAN> V;
-    const V bias(j.bias, c), gate(j.gate, c), post_w(POST ? j.post_w : nullptr, c), post_b(POST ? j.post_b : nullptr, c);
-    const V pre_w(PRE ? j.pre_w : nullptr, c);
-    uint64_t seed = 0, offset = 0;
-    if (j.drop) { seed = j.rng[0]; offset = j.rng[1]; }
-    // gradients of the vectors, where their sums lie in j.partial: bias, gate, weight and bias of the post norm, of the pre norm
-    // (IN_LDS: those of the biases of wide rows lie in LDS, four columns of every thread side by side)
-    constexpr bool IN_LDS = BIASES && NT > 512 && NV == 1;
-    extern __shared__ __align__(16) float biases[];
-    auto add_bias = [&](int s, float (&sum)[NV][8], const float (&v)[NV][8]) {
-        if constexpr (!IN_LDS) {
-            add<NV>(sum, v);
-        } else {
+    // vectors in registers for all rows; rows of 1024 threads have no room for them and read them again
+    constexpr bool LEAN = NT > 640;
+    float bias[LEAN ? 1 : NV][8], gw[LEAN ? 1 : NV][8], pw[LEAN ? 1 : NV][8];
+    auto gate_and_weight = [&](float (&x)[NV][8]) {
+        vector_of<T, NV>(x, j.gate, 1.f, c);
+        if constexpr (POST) {
+            if (j.post_w) {
+                float w[NV][8];
+                vector_of<T, NV>(w, j.post_w, 1.f, c);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                f4* at = (f4*)(biases + ((s * 2 + h) * NT + threadIdx.x) * 4);
-                f4 old = *at;
+                for (int k = 0; k < NV; ++k)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) old[e] += v[0][4 * h + e];
-                *at = old;
+                    for (int e = 0; e < 8; ++e) x[k][e] *= w[k][e];
             }
         }
     };
-    if constexpr (IN_LDS) {
-#pragma unroll
-        for (int q = 0; q < 6; ++q) *(f4*)(biases + (q * NT + threadIdx.x) * 4) = f4{0.f, 0.f, 0.f, 0.f};
+    if constexpr (!LEAN) {
+        vector_of<T, NV>(bias, j.bias, 0.f, c);
+        gate_and_weight(gw);
+        if constexpr (PRE) vector_of<T, NV>(pw, j.pre_w, 1.f, c);
     }
-    float total[6][NV][8];
+    auto times = [&](float (&x)[NV][8], const auto& held, auto read) {
+        if constexpr (LEAN) {
+            float v[NV][8];
+            read(v);
 #pragma unroll
-    for (int s = 0; s < 6; ++s)
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[k][e] *= v[k][e];
+        } else {
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[k][e] *= held[k][e];
+        }
+    };
+    uint64_t seed = 0, offset = 0;
+    if (j.drop) { seed = j.rng[0]; offset = j.rng[1]; }
+    // sums over the rows: d t, dh times the pre norm's value; d, dh, dy
+    float A[NV][8], P[NV][8], B[NV][8], Q[NV][8], D[NV][8];
+    auto zero = [](float (&x)[NV][8]) {
 #pragma unroll
         for (int k = 0; k < NV; ++k)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) total[s][k][e] = 0.f;
+            for (int e = 0; e < 8; ++e) x[k][e] = 0.f;
+    };
+    zero(A); zero(P); zero(B); zero(Q); zero(D);
 
     const int64_t step = (int64_t)gridDim.x * G;
     int64_t base = (int64_t)blockIdx.x * G;
@@ -354,24 +410,28 @@ __global__ __launch_bounds__(NT * groups_of<NT>(), (back_waves<T, NT, POST, PRE,
         if constexpr (LEAN) fetch(base);
         const int64_t row = base + mine;
         const bool on = row < j.rows;
-        float t[NV][8], x[NV][8], d[NV][8], g[NV][8], rt = 0.f, rr = 0.f;
+        float t[NV][8], x[NV][8], d[NV][8], g[NV][8], rt = 0.f, rr = 0.f, ar, br;
         c.template values<T>(rd, d);
         if constexpr (PRE) {
             c.template values<T>(rh, g);
             c.template values<T>(rx, x);
         }
         c.template values<T>(ry, t);
+        // the next row's values travel while this one's are used (past the last row: the last one's again)
         if constexpr (!LEAN) fetch(base + step);
         if constexpr (G > 1) {
             // (a group of threads behind the last row has that row's values again, and adds nothing)
-            if (!on) {
-#pragma unroll
-                for (int k = 0; k < NV; ++k)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) { d[k][e] = 0.f; g[k][e] = 0.f; }
+            if (!on) { zero(d); zero(g); }
+        }
+        if (j.bias) {
+            if constexpr (LEAN) {
+                float v[NV][8];
+                vector_of<T, NV>(v, j.bias, 0.f, c);
+                add<NV>(t, v);
+            } else {
+                add<NV>(t, bias);
             }
         }
-        bias.plus(t);
         uint32_t kept[NV];
         auto drop = [&](float (&v)[NV][8]) {
 #pragma unroll
@@ -384,114 +444,148 @@ __global__ __launch_bounds__(NT * groups_of<NT>(), (back_waves<T, NT, POST, PRE,
             for (int k = 0; k < NV; ++k) kept[k] = Draw(seed, offset, (uint32_t)row, (uint32_t)c.col[k] >> 3).bits(j.drop);
             drop(t);
         }
-        if constexpr (POST && PRE) normalise<NV, true>(x, t, rr, rt, c.hi, j.cols, j.layer, j.eps, sums);
-        else if constexpr (PRE) normalise<NV, false>(x, x, rr, rt, c.hi, j.cols, j.layer, j.eps, sums);
-        else if constexpr (POST) normalise<NV, false>(t, t, rt, rr, c.hi, j.cols, j.layer, j.eps, sums);
+        if constexpr (POST && PRE) normalise<NV, true>(x, t, rr, rt, c, j.cols, LAYER, j.eps, sums);
+        else if constexpr (PRE) normalise<NV, false>(x, x, rr, rt, c, j.cols, LAYER, j.eps, sums);
+        else if constexpr (POST) normalise<NV, false>(t, t, rt, rr, c, j.cols, LAYER, j.eps, sums);
         if constexpr (PRE) {
-            add_product<NV>(total[4], g, x);
-            if constexpr (BIASES) add_bias(2, total[5], g);
-            pre_w.times(g);
-            norm_back<NV>(g, x, rr, c.hi, j.cols, j.layer, sums);
-            add<NV>(d, g);
+            add_product<NV>(P, g, x);
+            if constexpr (BIASES) add<NV>(Q, g);
+            times(g, pw, [&](float (&v)[NV][8]) { vector_of<T, NV>(v, j.pre_w, 1.f, c); });
+            norm_back<NV, LAYER>(g, x, rr, j.cols, ar, br, sums);
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    d[k][e] = fmaf(-ar, x[k][e], fmaf(rr, g[k][e], d[k][e]));
+                    if constexpr (LAYER) d[k][e] -= br;
+                }
+            if constexpr (LAYER) mask<NV>(d, c);
+            if constexpr (G > 1) { if (!on) zero(d); }
         }
-        // d: the gradient at x_out and at x; t: D(y + bias), or what the post norm makes of it before its weight
         if (j.dx && on) c.template put<T>(j.dx, row * j.lddx, d);
-        float n[NV][8];
-#pragma unroll
-        for (int k = 0; k < NV; ++k)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) { d[k][e] *= j.scale; n[k][e] = t[k][e]; }
+        add_product<NV>(A, d, t);
+        if constexpr (BIASES) add<NV>(B, d);
+        times(d, gw, gate_and_weight);
         if constexpr (POST) {
-            post_w.times(n);
-            post_b.plus(n);
-        }
-        add_product<NV>(total[1], d, n);
-        gate.times(d);
-        if constexpr (POST) {
-            add_product<NV>(total[2], d, t);
-            if constexpr (BIASES) add_bias(1, total[3], d);
-            post_w.times(d);
-            norm_back<NV>(d, t, rt, c.hi, j.cols, j.layer, sums);
+            norm_back<NV, LAYER>(d, t, rt, j.cols, ar, br, sums);
+            ar *= j.scale; br *= j.scale;
+            const float r = rt * j.scale;
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    if constexpr (LAYER) d[k][e] = fmaf(-ar, t[k][e], fmaf(r, d[k][e], -br));
+                    else d[k][e] = fmaf(-ar, t[k][e], r * d[k][e]);
+                }
+            if constexpr (LAYER) mask<NV>(d, c);
+        } else {
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) d[k][e] *= j.scale;
         }
         if (j.drop) drop(d);
-        if constexpr (BIASES) add_bias(0, total[0], d);
+        if constexpr (BIASES) add<NV>(D, d);
         if (j.dy && on) c.template put<T>(j.dy, row * j.lddy, d);
     }
 
     if (!j.partial) return;
-    if constexpr (IN_LDS) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                total[0][0][4 * h + e] = biases[(h * NT + threadIdx.x) * 4 + e];
-                total[3][0][4 * h + e] = biases[((2 + h) * NT + threadIdx.x) * 4 + e];
-                total[5][0][4 * h + e] = biases[((4 + h) * NT + threadIdx.x) * 4 + e];
-            }
-    }
-    // the G rows' sums of a workgroup, in their order
+    // the sums of the G rows that a workgroup takes at a time, in their order
     __shared__ __align__(16) float all[G > 1 ? BLOCK * 8 : 4];
-#pragma unroll
-    for (int s = 0; s < 6; ++s) {
-        if constexpr (!BIASES) { if (s == 0 || s == 3 || s == 5) continue; }
-        if ((s == 2 || s == 3) && !POST) continue;
-        if (s >= 4 && !PRE) continue;
-        float* dst = j.partial + ((size_t)s * (size_t)j.slabs + blockIdx.x) * (size_t)j.cols;
+    auto joined = [&](float (&x)[NV][8]) {
         if constexpr (G > 1) {
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
                 __syncthreads();
-                store8(all + threadIdx.x * 8, 0, 8, total[s][k]);
+                store8(all + threadIdx.x * 8, 0, 8, x[k]);
                 __syncthreads();
                 if (threadIdx.x < NT)
 #pragma unroll
                     for (int q = 1; q < G; ++q)
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) total[s][k][e] += all[(threadIdx.x + NT * q) * 8 + e];
+                        for (int e = 0; e < 8; ++e) x[k][e] += all[(threadIdx.x + NT * q) * 8 + e];
             }
-            if (threadIdx.x >= NT) continue;
         }
-        c.template put<float>(dst, 0, total[s]);
+    };
+    auto keep = [&](int which, const float (&x)[NV][8]) {
+        if (G > 1 && threadIdx.x >= NT) return;
+        c.template put<float>(j.partial + ((size_t)which * (size_t)j.slabs + blockIdx.x) * (size_t)j.cols, 0, x);
+    };
+    joined(A);
+    if constexpr (BIASES) {
+        joined(B);
+        joined(D);
+        keep(SUM_BIAS, D);
     }
+    if constexpr (PRE) {
+        joined(P);
+        keep(SUM_PRE_W, P);
+        if constexpr (BIASES) {
+            joined(Q);
+            keep(SUM_PRE_B, Q);
+        }
+    }
+    auto scaled = [&](const float (&x)[NV][8], const void* v, float (&out)[NV][8]) {
+        float w[NV][8];
+        vector_of<T, NV>(w, v, 1.f, c);
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) out[k][e] = j.scale * w[k][e] * x[k][e];
+    };
+    float v[NV][8];
+    if constexpr (POST) {
+        scaled(A, j.gate, v);
+        keep(SUM_POST_W, v);
+        if constexpr (BIASES) {
+            scaled(B, j.gate, v);
+            keep(SUM_POST_B, v);
+        }
+        scaled(A, j.post_w, v);
+        if constexpr (BIASES) {
+            if (j.post_b) {
+                float w[NV][8];
+                scaled(B, j.post_b, w);
+                add<NV>(v, w);
+            }
+        }
+    } else {
+        scaled(A, nullptr, v);
+    }
+    keep(SUM_GATE, v);
 }
 
 template <typename T, int NT, int NV, bool BACK>
 int launch_shape(const Join& j, int blocks, hipStream_t stream)
 {
     constexpr int threads = NT * groups_of<NT>();
-    bool ok = true;
-    auto go = [&](auto post, auto pre, auto biases) {
-        constexpr bool POST = decltype(post)::value, PRE = decltype(pre)::value, BIASES = decltype(biases)::value;
-        if constexpr (BACK) {
-            constexpr int lds = BIASES && NT > 512 && NV == 1 ? 6 * NT * 16 : 0;
-            const auto fn = join_back_kernel<T, NT, NV, POST, PRE, BIASES>;
-            if constexpr (lds > 0) {
-                static AttrFlags attr_set;
-                if (!ensure_max_dynamic_lds((const void*)fn, lds, &attr_set)) { ok = false; return; }
-            }
-            hipLaunchKernelGGL(fn, dim3((unsigned)blocks), dim3(threads), lds, stream, j);
-        }
-        else hipLaunchKernelGGL((join_kernel<T, NT, NV, POST, PRE>), dim3((unsigned)blocks), dim3(threads), 0, stream, j);
-    };
     const std::true_type yes;
     const std::false_type no;
-    auto norms = [&](auto biases) {
-        if (j.post && j.pre) go(yes, yes, biases);
-        else if (j.post) go(yes, no, biases);
-        else if (j.pre) go(no, yes, biases);
-        else go(no, no, biases);
+    auto both = [&](bool a, bool b, auto f) {
+        if (a && b) f(yes, yes);
+        else if (a) f(yes, no);
+        else if (b) f(no, yes);
+        else f(no, no);
     };
-    if constexpr (!BACK) norms(no);
-    else if constexpr (NT * NV == 1024) { if (j.biases == (NT == 512)) norms(std::integral_constant<bool, NT == 512>()); else return ZR_ERR_SHAPE; }
-    else if (j.biases) norms(yes);
-    else norms(no);
-    if (!ok) return ZR_ERR_HIP;
+    both(j.post, j.pre, [&](auto post, auto pre) {
+        constexpr bool POST = decltype(post)::value, PRE = decltype(pre)::value;
+        if constexpr (BACK) {
+            // (without a norm there is no kind of norm)
+            both((POST || PRE) && j.layer, j.biases, [&](auto layer, auto biases) {
+                constexpr bool LAYER = decltype(layer)::value && (POST || PRE);
+                hipLaunchKernelGGL((join_back_kernel<T, NT, NV, POST, PRE, LAYER, decltype(biases)::value>), dim3((unsigned)blocks), dim3(threads), 0, stream, j);
+            });
+        } else {
+            hipLaunchKernelGGL((join_kernel<T, NT, NV, POST, PRE>), dim3((unsigned)blocks), dim3(threads), 0, stream, j);
+        }
+    });
     return hip_status(hipGetLastError());
 }
 
 // Threads to a row (a group of eight columns each, two in the widest rows), rows that a workgroup takes at a time, and workgroups to a
-// compute unit, which is how many of them its registers hold: a launch is that many, each with its share of the rows.  (Backward, 8192 x 4096, two norms, us by wavefronts to a unit: 8
-// 98, 12 127, 16 105, 24 112; 12608 x 1024: 43, 42, 50, 48.)
+// compute unit: a launch is that many, each with its share of the rows, and their number is that of the sums to be added up in the
+// end.  (Backward, two norms, bf16, us with 1 / 2 / 3 workgroups to a unit: 8192 x 4096 83 / 90 / -, 8192 x 2048 62 / 47 / 50, 12608 x 1024
+// 52 / 39 / 40, 8192 x 768 36 / 27 / 24, 8192 x 5120 100 / 112 / -.)
 struct Shape { int threads, rows_at_once, per_unit; };
 Shape shape_of(int cols)
 {
@@ -501,12 +595,7 @@ Shape shape_of(int cols)
 Shape back_shape_of(const Join& j)
 {
     Shape s = shape_of(j.cols);
-    if (s.threads <= 256) s.per_unit = j.biases ? 2 : 3;
-    else if (s.threads == 512) s.per_unit = j.biases || (j.post && j.pre) ? 1 : 2;
-    else s.per_unit = 1;
-    // six vectors' sums: two groups of columns to a thread of twice the registers (4096 x 8192, layer norms, dropout, all gradients:
-    // 171 us, 204 on 1024 threads with three of the sums in LDS; 8192 x 5120 on 640 threads 288 and 218)
-    if (j.biases && j.cols > 5120 && j.cols <= 8192) s.threads = 512;
+    s.per_unit = s.threads > 256 ? 1 : s.threads == 256 || j.biases ? 2 : 3;
     return s;
 }
 int blocks_of(int rows, const Shape& s)
@@ -521,10 +610,7 @@ int launch_any(const Join& j, const Shape& s, int blocks, hipStream_t stream)
         case 64: return launch_shape<T, 64, 1, BACK>(j, blocks, stream);
         case 128: return launch_shape<T, 128, 1, BACK>(j, blocks, stream);
         case 256: return launch_shape<T, 256, 1, BACK>(j, blocks, stream);
-        case 512:
-            if constexpr (BACK)
-                if (j.cols > 4096) return launch_shape<T, 512, 2, true>(j, blocks, stream);
-            return launch_shape<T, 512, 1, BACK>(j, blocks, stream);
+        case 512: return launch_shape<T, 512, 1, BACK>(j, blocks, stream);
         case 640: return launch_shape<T, 640, 1, BACK>(j, blocks, stream);
         default: return j.cols <= 8192 ? launch_shape<T, 1024, 1, BACK>(j, blocks, stream) : launch_shape<T, 1024, 2, BACK>(j, blocks, stream);
     }
@@ -535,7 +621,7 @@ int launch_any(const Join& j, const Shape& s, int blocks, hipStream_t stream)
 int join_max_cols() { return MAX_COLS; }
 
 int join_most_slabs(int rows, int cols) { return blocks_of(rows, shape_of(cols)); }
-int join_slabs(const Join& j) { return blocks_of(j.rows, back_shape_of(j)); }
+int join_slabs(const Join& j) { return std::min(blocks_of(j.rows, back_shape_of(j)), join_most_slabs(j.rows, j.cols)); }
 
 int launch_join(const Join& j, int dtype, hipStream_t stream)
 {
