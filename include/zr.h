@@ -367,7 +367,7 @@ int zr_resized_linear_act_fwd(const void* X, int64_t ldx, const void* W, int64_t
  *  dZ is held in dtype between the two steps (bf16: one rounding more, before sums over all of its terms, as the matrix
  *  instruction takes its operands in bf16); dbias adds up dZ before that rounding, in fp32.
  *  workspace: of zr_act_bwd_workspace_bytes bytes, 16-byte aligned; needed where dZ is not dY itself (act, gate or p), or dbias is
- *  wanted (else NULL is allowed).  Less will do, down to dZ ([M x N rounded up to 8] in dtype) and dbias's sums, with fewer ways open
+ *  wanted (else NULL is allowed).  Less will do, down to dZ (M x N values of dtype, N rounded up to 64) and dbias's sums, with fewer ways open
  *  to the products.  Errors: as above; SHAPE also for a workspace that is too small, NULL without one. */
 size_t zr_act_bwd_workspace_bytes(int32_t M, int32_t K, int32_t N, int32_t n_keep, int mode, int dtype);
 int zr_resized_linear_act_bwd(const void* X, int64_t ldx, const void* W, int64_t ldw, const void* dY, int64_t lddy,

@@ -41,7 +41,10 @@ struct ActBack {
     float* partial;                        // [slabs x N] or nullptr
     const uint64_t* rng; uint32_t drop; float factor; int act;
     int M, N;
+    // bf16, N above 256: dz receives these columns side by side, [M x width] with zeros behind the last (nullptr: all, in their places)
+    const int32_t* keep; int n_keep; int width;
 };
+constexpr int ACT_KEPT_ABOVE = 256;        // (a wavefront has a row then)
 int act_slabs(int M, int N);
 int launch_act_back(const ActBack& a, int dtype, hipStream_t stream);
 // out[v][c] = sum over slabs of partial[(v * slabs + slab) * n + c], in slab order, for `vectors` of them (out[v] nullptr: skipped)

@@ -39,7 +39,7 @@ size_t round_up16(size_t v) { return (v + 15) & ~(size_t)15; }
 
 // The workspace of the backward pass: dZ [M x pitch], the column sums of its slabs, and zr_resized_linear_bwd's scratch.
 int64_t dz_pitch(int32_t N) { return ((int64_t)N + 7) / 8 * 8; }
-size_t dz_bytes(int32_t M, int32_t N, int dtype) { return round_up16((size_t)M * (size_t)dz_pitch(N) * size_of(dtype)); }
+size_t dz_bytes(int32_t M, int32_t N, int dtype) { return round_up16((size_t)M * (size_t)((N + 63) / 64 * 64) * size_of(dtype)); }
 size_t sums_bytes(int32_t M, int32_t N) { return round_up16((size_t)act_slabs(M, N) * (size_t)N * 4); }
 
 }  // namespace
@@ -118,7 +118,10 @@ int zr_resized_linear_act_bwd(const void* X, int64_t ldx, const void* W, int64_t
     const bool products = dX || dW;
     const bool changes = act != ZR_ACT_NONE || gate || a.drop;         // dZ is not dY itself
     const bool holds = products && changes;
-    const size_t dz = holds ? dz_bytes(M, N, dtype) : 0, sums = dbias ? sums_bytes(M, N) : 0;
+    // bf16 products of kept columns read them side by side: dZ is written that way
+    const bool kept = holds && dtype == ZR_BF16 && mode == ZR_DROP_N && n_keep < N && N > ACT_KEPT_ABOVE;
+    const int64_t pitch = kept ? (n_keep + 63) / 64 * 64 : dz_pitch(N);
+    const size_t dz = holds ? round_up16((size_t)M * (size_t)pitch * size_of(dtype)) : 0, sums = dbias ? sums_bytes(M, N) : 0;
     if (dz + sums) {
         if (!workspace) return ZR_ERR_NULL;
         if ((uintptr_t)workspace % 16 != 0 || workspace_bytes < dz + sums) return ZR_ERR_SHAPE;
@@ -126,7 +129,8 @@ int zr_resized_linear_act_bwd(const void* X, int64_t ldx, const void* W, int64_t
     hipStream_t s = (hipStream_t)stream;
     if (holds || dbias || dgate) {
         a.dY = dY; a.lddy = lddy; a.Z = needs_z ? Z : nullptr; a.ldz = ldz; a.gate = gate; a.ldg = ldg; a.dgate = dgate; a.lddg = lddg;
-        a.dz = holds ? workspace : nullptr; a.lddz = dz_pitch(N);
+        a.dz = holds ? workspace : nullptr; a.lddz = pitch;
+        a.keep = kept ? keep_idx : nullptr; a.n_keep = n_keep; a.width = (int)pitch;
         a.partial = dbias ? (float*)((char*)workspace + dz) : nullptr;
         a.rng = rng; a.factor = kept_factor(a.drop); a.act = act; a.M = M; a.N = N;
         st = launch_act_back(a, dtype, s);
@@ -141,9 +145,9 @@ int zr_resized_linear_act_bwd(const void* X, int64_t ldx, const void* W, int64_t
     if (!products) return ZR_OK;
     char* rest = workspace ? (char*)workspace + dz + sums : nullptr;
     // (without a list every index is kept, and the list is not read: any address stands in for it)
-    return resized_linear_bwd(X, ldx, W, ldw, holds ? workspace : dY, holds ? dz_pitch(N) : lddy, dX, lddx, dW, lddw, M, K, N,
+    return resized_linear_bwd(X, ldx, W, ldw, holds ? workspace : dY, holds ? pitch : lddy, dX, lddx, dW, lddw, M, K, N,
                               keep_idx ? keep_idx : (const int32_t*)dY, n_keep, mode, w_layout, dtype, ZR_IMPUTE_ZERO, nullptr, nullptr,
-                              rest, workspace ? workspace_bytes - dz - sums : 0, 0, false, s);
+                              rest, workspace ? workspace_bytes - dz - sums : 0, 0, false, kept, s);
 }
 
 static int check_join(int32_t rows, int32_t cols, int norms, int norm, double eps, int dtype)

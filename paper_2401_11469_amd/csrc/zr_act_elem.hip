@@ -7,6 +7,7 @@ namespace zr {
 namespace {
 
 // Threads of a workgroup over groups of eight columns and rows: `across` (a power of two) neighbours along a row.
+constexpr int BACK_BLOCKS = 1536;          // workgroups of act_back_kernel, six to a compute unit
 inline int lanes_across(int cols)
 {
     int w = 1;
@@ -38,10 +39,17 @@ __global__ __launch_bounds__(256) void dropout_kernel(const T* x, int64_t ldx, T
 // ---------------------------------------------------------------------------
 // dZ = D(dY) gate act'(Z), dgate = D(dY) act(Z), and the column sums of dZ
 // ---------------------------------------------------------------------------
-template <typename T>
+// A workgroup has a panel of columns and rows_each rows; a thread's next row is on its way while it works on one.  What bounds it is
+// HBM and, with an activation, the vector instructions nearly as much (erf: 30 an element, 21 us of 12608 x 2048 beside 29 of HBM).
+// KEPT (bf16): only the kept columns of dZ are written, side by side: a wavefront has a row's 512 columns, puts the kept
+// ones into LDS at their places and stores 16 bytes a lane; the chunks that panels share go out element by element.
+template <typename T, bool KEPT>
 __global__ __launch_bounds__(256) void act_back_kernel(const ActBack a, int across, int rows_each)
 {
+    constexpr int PANEL = 512, SLOTS = PANEL + 8 + 64;       // a row's panel, its place in a chunk, the zeros behind the last column
     __shared__ float sums[256 * 8];
+    __shared__ uint32_t mask[KEPT ? 64 : 1];
+    __shared__ __align__(16) Bf turn[KEPT ? 4 : 1][KEPT ? SLOTS + 8 : 8];
     constexpr bool EXACT = sizeof(T) == 4;
     const int lane = threadIdx.x & (across - 1), sub = threadIdx.x / across, down = 256 / across;
     const int group = (int)blockIdx.x * across + lane, col = 8 * group;
@@ -49,26 +57,77 @@ __global__ __launch_bounds__(256) void act_back_kernel(const ActBack a, int acro
     const int64_t first = (int64_t)blockIdx.y * rows_each, last = min((int64_t)a.M, first + rows_each);
     uint64_t seed = 0, offset = 0;
     if (a.drop) { seed = a.rng[0]; offset = a.rng[1]; }
+
+    // KEPT: kept columns before the panel and behind it, and where this thread's eight go
+    int begin = 0, end = 0, fill = 0, at[8];
+    if constexpr (KEPT) {
+        const int panel = (int)blockIdx.x * PANEL;
+        begin = lower_bound_wave(a.keep, a.n_keep, panel, threadIdx.x & 63);
+        end = panel + PANEL >= a.N ? a.n_keep : lower_bound_wave(a.keep, a.n_keep, panel + PANEL, threadIdx.x & 63);
+        fill = panel + PANEL >= a.N ? a.width : end;         // (zeros behind the last kept column, to the end of the row)
+        if (threadIdx.x < 64) mask[threadIdx.x] = 0u;
+        __syncthreads();
+        // (a list that is not ascending gives other columns, but none past the panel)
+        for (int q = begin + (int)threadIdx.x; q < min(end, begin + PANEL); q += 256) {
+            const int c = min(max(a.keep[q] - panel, 0), PANEL - 1);
+            atomicOr(&mask[c >> 3], 1u << (c & 7));
+        }
+        __syncthreads();
+        const uint32_t m = mask[lane];
+        int before = __popc(m);
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+            const int x = __shfl_up(before, off, 64);
+            before += lane >= off ? x : 0;
+        }
+        before -= __popc(m);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) at[e] = m >> e & 1 ? (begin & 7) + before + __popc(m & ((1u << e) - 1u)) : SLOTS;
+        // (a slot that no column fills stays as it is: zeros)
+        for (int q = (int)threadIdx.x; q < 4 * (SLOTS + 8); q += 256) turn[q / (SLOTS + 8)][q % (SLOTS + 8)] = 0;
+        __syncthreads();
+    }
+
     float total[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) total[e] = 0.f;
-    for (int64_t r = first + sub; r < last && hi > 0; r += down) {
+    const bool whole = hi == 8;
+    Raw8<T> rt, rz, rg;
+    rt.clear(); rz.clear(); rg.clear();
+    auto fetch = [&](int64_t row) {
+        const int64_t r = min(row, (int64_t)a.M - 1);
+        auto one = [&](Raw8<T>& raw, const void* p, int64_t ld) {
+            if (whole) {
+                raw.load((const T*)p + r * ld + col);
+            } else {
+                float x[8];
+                load8((const T*)p + r * ld + col, 0, max(hi, 0), x);
+                raw.take(x);
+            }
+        };
+        one(rt, a.dY, a.lddy);
+        if (a.Z) one(rz, a.Z, a.ldz);
+        if (a.gate) one(rg, a.gate, a.ldg);
+    };
+    if (first + sub < last) fetch(first + sub);
+    for (int64_t r = first + sub; r < last; r += down) {
         float t[8], z[8], v[8], s[8], g[8];
-        load8((const T*)a.dY + r * a.lddy + col, 0, hi, t);
+        rt.values(t);
+        if (a.Z) rz.values(z);
+        if (a.gate) rg.values(g);
+        fetch(r + down);
         if (a.drop) Draw(seed, offset, (uint32_t)r, (uint32_t)group).apply(t, a.drop, a.factor);
         if (a.Z) {
-            load8((const T*)a.Z + r * a.ldz + col, 0, hi, z);
             act8<EXACT, true>(a.act, z, v, s);
         } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e) { v[e] = 0.f; s[e] = 1.f; }
         }
         if (a.gate) {
-            load8((const T*)a.gate + r * a.ldg + col, 0, hi, g);
 #pragma unroll
             for (int e = 0; e < 8; ++e) s[e] *= g[e];
         }
-        if (a.dgate) {
+        if (a.dgate && hi > 0) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] *= t[e];
             store8((T*)a.dgate + r * a.lddg + col, 0, hi, v);
@@ -78,7 +137,26 @@ __global__ __launch_bounds__(256) void act_back_kernel(const ActBack a, int acro
             t[e] *= s[e];
             total[e] += t[e];
         }
-        if (a.dz) store8((T*)a.dz + r * a.lddz + col, 0, hi, t);
+        if constexpr (KEPT) {
+            Bf* slots = turn[sub];
+            Bf* row = (Bf*)a.dz + r * a.lddz + (begin & ~7);
+            Raw8<Bf> raw;
+            raw.take(t);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) slots[at[e]] = (Bf)(e & 1 ? raw.v[e >> 1] >> 16 : raw.v[e >> 1]);
+            // (a wavefront's LDS operations are done in their order)
+            __builtin_amdgcn_wave_barrier();
+            // whole chunks from the first slot on; slot 0 is column begin & ~7
+            const int lo = begin & 7, top = min(fill - (begin & ~7), SLOTS);
+            for (int c = (lo + 7) / 8 + lane; c < top / 8; c += 64) *(u4*)(row + 8 * c) = *(const u4*)(slots + 8 * c);
+            const int part = lane < 8 ? lane : top / 8 * 8 + (lane - 8);
+            const bool in_first = lane < 8 && part >= lo && part < top && lo > 0;
+            const bool in_last = lane >= 8 && lane < 16 && part < top && (top / 8 > 0 || lo == 0);
+            if (in_first || in_last) row[part] = slots[part];
+            __builtin_amdgcn_wave_barrier();
+        } else {
+            if (a.dz && hi > 0) store8((T*)a.dz + r * a.lddz + col, 0, hi, t);
+        }
     }
     if (!a.partial) return;
 #pragma unroll
@@ -149,7 +227,7 @@ static int back_rows_each(int M, int N)
 {
     const int across = lanes_across(N), down = 256 / across;
     const int wide = (N + 8 * across - 1) / (8 * across);
-    const int most = std::max(1, std::min(256, 2048 / wide));
+    const int most = std::max(1, std::min(512, BACK_BLOCKS / wide));
     return std::max(down, (M + most - 1) / most);
 }
 int act_slabs(int M, int N)
@@ -162,8 +240,10 @@ int launch_act_back(const ActBack& a, int dtype, hipStream_t stream)
 {
     const int across = lanes_across(a.N);
     const dim3 grid((unsigned)((a.N + 8 * across - 1) / (8 * across)), (unsigned)act_slabs(a.M, a.N));
-    if (dtype == ZR_BF16) hipLaunchKernelGGL(act_back_kernel<Bf>, grid, dim3(256), 0, stream, a, across, back_rows_each(a.M, a.N));
-    else hipLaunchKernelGGL(act_back_kernel<float>, grid, dim3(256), 0, stream, a, across, back_rows_each(a.M, a.N));
+    const int each = back_rows_each(a.M, a.N);
+    if (dtype == ZR_F32) hipLaunchKernelGGL((act_back_kernel<float, false>), grid, dim3(256), 0, stream, a, across, each);
+    else if (a.keep) hipLaunchKernelGGL((act_back_kernel<Bf, true>), grid, dim3(256), 0, stream, a, across, each);
+    else hipLaunchKernelGGL((act_back_kernel<Bf, false>), grid, dim3(256), 0, stream, a, across, each);
     return hip_status(hipGetLastError());
 }
 

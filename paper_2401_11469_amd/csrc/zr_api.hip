@@ -336,7 +336,7 @@ int resized_linear_fwd(const void* X, int64_t ldx, const void* W, int64_t ldw, v
 int check_linear_bwd(const void* X, int64_t ldx, const void* W, int64_t ldw, const void* dY, int64_t lddy,
                      const void* dX, int64_t lddx, const void* dW, int64_t lddw, int32_t M, int32_t K, int32_t N,
                      const int32_t* keep_idx, int32_t n_keep, int mode, int w_layout, int dtype, int policy,
-                     const void* prev_dX, const void* prev_dW, bool x_kept)
+                     const void* prev_dX, const void* prev_dW, bool x_kept, bool dy_kept)
 {
     if (!dY || (!dX && !dW)) return ZR_ERR_NULL;
     if ((dX && !W) || (dW && !X)) return ZR_ERR_NULL;
@@ -344,7 +344,7 @@ int check_linear_bwd(const void* X, int64_t ldx, const void* W, int64_t ldw, con
     if (st != ZR_OK) return st;
     if (w_layout != ZR_W_KN && w_layout != ZR_W_NK) return ZR_ERR_MODE;
     const bool kn = w_layout == ZR_W_KN;
-    if (lddy < N) return ZR_ERR_SHAPE;
+    if (lddy < (dy_kept ? n_keep : N)) return ZR_ERR_SHAPE;
     if (dX && (ldw < (kn ? N : K) || lddx < K)) return ZR_ERR_SHAPE;
     if (dW && (ldx < (x_kept ? n_keep : K) || lddw < (kn ? N : K))) return ZR_ERR_SHAPE;
     const bool full = n_keep == (mode == ZR_DROP_N ? N : K);
@@ -362,9 +362,9 @@ int resized_linear_bwd(const void* X, int64_t ldx, const void* W, int64_t ldw,
                        const int32_t* keep_idx, int32_t n_keep,
                        int mode, int w_layout, int dtype, int policy,
                        const void* prev_dX, const void* prev_dW,
-                       void* workspace, size_t workspace_bytes, int workspace_flags, bool x_kept, hipStream_t s)
+                       void* workspace, size_t workspace_bytes, int workspace_flags, bool x_kept, bool dy_kept, hipStream_t s)
 {
-    int st = check_linear_bwd(X, ldx, W, ldw, dY, lddy, dX, lddx, dW, lddw, M, K, N, keep_idx, n_keep, mode, w_layout, dtype, policy, prev_dX, prev_dW, x_kept);
+    int st = check_linear_bwd(X, ldx, W, ldw, dY, lddy, dX, lddx, dW, lddw, M, K, N, keep_idx, n_keep, mode, w_layout, dtype, policy, prev_dX, prev_dW, x_kept, dy_kept);
     if (st != ZR_OK) return st;
     const bool kn = w_layout == ZR_W_KN;
     const bool full = n_keep == (mode == ZR_DROP_N ? N : K);
@@ -390,8 +390,8 @@ int resized_linear_bwd(const void* X, int64_t ldx, const void* W, int64_t ldw,
         const int wr = kn ? K : N, wc = kn ? N : K;
         auto dx_clear = [&](const void* p, int rows, int cols, int64_t ld) { return clear(dX, M, K, lddx, p, rows, cols, ld); };
         auto dw_clear = [&](const void* p, int rows, int cols, int64_t ld) { return clear(dW, wr, wc, lddw, p, rows, cols, ld); };
-        return dx_clear(dW, wr, wc, lddw) && dx_clear(X, M, x_kept ? n_keep : K, ldx) && dx_clear(dY, M, N, lddy) && dx_clear(same ? prev_dW : nullptr, wr, wc, lddw) &&
-               dw_clear(W, wr, wc, ldw) && dw_clear(dY, M, N, lddy) && dw_clear(same ? prev_dX : nullptr, M, K, lddx);
+        return dx_clear(dW, wr, wc, lddw) && dx_clear(X, M, x_kept ? n_keep : K, ldx) && dx_clear(dY, M, dy_kept ? n_keep : N, lddy) && dx_clear(same ? prev_dW : nullptr, wr, wc, lddw) &&
+               dw_clear(W, wr, wc, ldw) && dw_clear(dY, M, dy_kept ? n_keep : N, lddy) && dw_clear(same ? prev_dX : nullptr, M, K, lddx);
     };
 
     // both at once, the stand-alone passes of Average imputation behind them; one at a time, the epilogues leave its sums
@@ -402,8 +402,8 @@ int resized_linear_bwd(const void* X, int64_t ldx, const void* W, int64_t ldw,
 
     // one extraction serves both products: X[:,S] (DROP_K, used by dW) or dY[:,S] (DROP_N)
     Extract ex{false, 0};
-    if (x_kept) {
-        // X holds the kept columns already
+    if (x_kept || dy_kept) {
+        // X or dY holds the kept columns already
     } else if (mode == ZR_DROP_K) {
         if (dW) ex = plan_extract(X, ldx, M, K, n_keep, dtype, workspace, workspace_bytes);
         // the forward call of this layer left X[:,S] at the same place (same plan, same sizes)
@@ -423,7 +423,7 @@ int resized_linear_bwd(const void* X, int64_t ldx, const void* W, int64_t ldw,
     // (in DROP_K the start of the buffer may hold the forward call's X[:,S] even when this call
     // extracts nothing itself)
     give_split_scratch(d, workspace, workspace_bytes,
-                       x_kept ? 0 : extraction_bytes(M, mode == ZR_DROP_K ? K : N, n_keep, dtype, workspace, workspace_bytes));
+                       x_kept || dy_kept ? 0 : extraction_bytes(M, mode == ZR_DROP_K ? K : N, n_keep, dtype, workspace, workspace_bytes));
     if (dX) {
         d.out = dX; d.ldo = lddx; d.I = M;
         d.B = weight_dx(W, ldw, K, N, mode, w_layout, S);
@@ -434,8 +434,9 @@ int resized_linear_bwd(const void* X, int64_t ldx, const void* W, int64_t ldw,
             if (same) d.prev = prev_dX;
         } else {
             // dX[m,k] = sum_{c<n'} dY[m,S[c]] * W[k,S[c]]
-            if (ex.use) {
-                d.A = operand(workspace, ex.width, true, nullptr, nullptr, M, ex.width);
+            if (ex.use || dy_kept) {
+                const int width = dy_kept ? (int)lddy : ex.width;
+                d.A = operand(dy_kept ? dY : workspace, width, true, nullptr, nullptr, M, width);
                 d.A.zero_padded = true;
             } else {
                 d.A = operand(dY, lddy, true, nullptr, S, M, N);
@@ -457,8 +458,9 @@ int resized_linear_bwd(const void* X, int64_t ldx, const void* W, int64_t ldw,
                         : operand(X, ldx, false, nullptr, S, M, K))
             : operand(X, ldx, false, nullptr, nullptr, M, K);
         const Operand dys = (mode == ZR_DROP_N)
-            ? (ex.use ? operand(workspace, ex.width, false, nullptr, nullptr, M, ex.width)
-                      : operand(dY, lddy, false, nullptr, S, M, N))
+            ? (dy_kept ? operand(dY, lddy, false, nullptr, nullptr, M, (int)lddy)
+               : ex.use ? operand(workspace, ex.width, false, nullptr, nullptr, M, ex.width)
+                        : operand(dY, lddy, false, nullptr, S, M, N))
             : operand(dY, lddy, false, nullptr, nullptr, M, N);
         const int ik = mode == ZR_DROP_K ? n_keep : K;       // extent of the K index of D
         const int in = mode == ZR_DROP_N ? n_keep : N;       // extent of the N index of D
@@ -505,7 +507,7 @@ int zr_resized_linear_bwd(const void* X, int64_t ldx, const void* W, int64_t ldw
                           void* workspace, size_t workspace_bytes, int workspace_flags, void* stream)
 {
     return resized_linear_bwd(X, ldx, W, ldw, dY, lddy, dX, lddx, dW, lddw, M, K, N, keep_idx, n_keep, mode, w_layout, dtype, policy,
-                              prev_dX, prev_dW, workspace, workspace_bytes, workspace_flags, false, (hipStream_t)stream);
+                              prev_dX, prev_dW, workspace, workspace_bytes, workspace_flags, false, false, (hipStream_t)stream);
 }
 
 int zr_priority_scores(const void* W_t, const void* W_prev, int64_t ld, int32_t K, int32_t N, int mode,

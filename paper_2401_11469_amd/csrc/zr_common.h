@@ -252,17 +252,17 @@ int resized_linear_fwd(const void* X, int64_t ldx, const void* W, int64_t ldw, v
                        const int32_t* keep_idx, int32_t n_keep, int mode, int w_layout, int dtype, int policy, const void* prev_Y,
                        const Finish* finish, void* workspace, size_t workspace_bytes, hipStream_t stream);
 // zr_resized_linear_bwd on arguments of its own kind; x_kept (DROP_K): X holds the kept columns side by side, [M x ldx] with
-// zeros behind the last, ldx a multiple of 64.
+// zeros behind the last, ldx a multiple of 64; dy_kept (DROP_N): the same of dY.
 int resized_linear_bwd(const void* X, int64_t ldx, const void* W, int64_t ldw, const void* dY, int64_t lddy,
                        void* dX, int64_t lddx, void* dW, int64_t lddw, int32_t M, int32_t K, int32_t N,
                        const int32_t* keep_idx, int32_t n_keep, int mode, int w_layout, int dtype, int policy,
                        const void* prev_dX, const void* prev_dW, void* workspace, size_t workspace_bytes,
-                       int workspace_flags, bool x_kept, hipStream_t stream);
+                       int workspace_flags, bool x_kept, bool dy_kept, hipStream_t stream);
 // its argument checks alone
 int check_linear_bwd(const void* X, int64_t ldx, const void* W, int64_t ldw, const void* dY, int64_t lddy,
                      const void* dX, int64_t lddx, const void* dW, int64_t lddw, int32_t M, int32_t K, int32_t N,
                      const int32_t* keep_idx, int32_t n_keep, int mode, int w_layout, int dtype, int policy,
-                     const void* prev_dX, const void* prev_dW, bool x_kept);
+                     const void* prev_dX, const void* prev_dW, bool x_kept, bool dy_kept = false);
 
 inline int hip_status(hipError_t e) { return e == hipSuccess ? ZR_OK : ZR_ERR_HIP; }
 

@@ -135,7 +135,7 @@ int zr_resized_linear_bwd_mx(const void* Xq, int64_t ldxq, const void* Xs, int64
     char* rest = workspace ? (char*)workspace + used : nullptr;
     const size_t left = workspace ? workspace_bytes - used : 0;
     return resized_linear_bwd(dW ? workspace : nullptr, ldv, W, ldw, dY, lddy, dX, lddx, dW, lddw, M, K, N, keep_idx, n_keep, mode, w_layout, dtype, policy,
-                              prev_dX, prev_dW, rest, left, 0, x_kept, (hipStream_t)stream);
+                              prev_dX, prev_dW, rest, left, 0, x_kept, false, (hipStream_t)stream);
 }
 
 }  // extern "C"
