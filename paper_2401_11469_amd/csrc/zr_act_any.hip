@@ -22,4 +22,14 @@ int launch_act_any(const GemmDesc& d, hipStream_t stream)
     return bg ? launch_shape<Plain, true, Gather, true>(a, "P, Pg", stream) : launch_shape<Plain, true, Plain, true>(a, "P, P", stream);
 }
 
+int launch_act_narrow(const GemmDesc& d, int j_base, hipStream_t stream)
+{
+    FinishArgs a;
+    (Args&)a = args_of(d);
+    a.f = *d.finish;
+    a.j_base = j_base;
+    if (d.B.c_contig) return launch_inst<Plain, true, Plain, true, 32, 256>(a, "P, P", stream);
+    return launch_inst<Plain, true, Plain, false, 32, 256>(a, "P, Q", stream);
+}
+
 }  // namespace zr

@@ -7,7 +7,7 @@ namespace zr {
 namespace {
 
 // Threads of a workgroup over groups of eight columns and rows: `across` (a power of two) neighbours along a row.
-constexpr int BACK_BLOCKS = 1536;          // workgroups of act_back_kernel, six to a compute unit
+constexpr int BACK_BLOCKS = 1024;          // workgroups of act_back_kernel, four to a compute unit
 inline int lanes_across(int cols)
 {
     int w = 1;
@@ -25,13 +25,14 @@ __global__ __launch_bounds__(256) void dropout_kernel(const T* x, int64_t ldx, T
     const int lane = threadIdx.x & (across - 1), sub = threadIdx.x / across, down = 256 / across;
     const int group = (int)blockIdx.x * across + lane, col = 8 * group;
     if (col >= cols) return;
-    const uint64_t seed = rng[0], offset = rng[1];
+    uint64_t seed = 0, offset = 0;
+    if (drop) { seed = rng[0]; offset = rng[1]; }          // (no generator where nothing is dropped)
     const int hi = min(8, cols - col);
     const int64_t first = (int64_t)blockIdx.y * rows_each, last = min((int64_t)rows, first + rows_each);
     for (int64_t r = first + sub; r < last; r += down) {
         float v[8];
         load8(x + r * ldx + col, 0, hi, v);
-        Draw(seed, offset, (uint32_t)r, (uint32_t)group).apply(v, drop, factor);
+        if (drop) Draw(seed, offset, (uint32_t)r, (uint32_t)group).apply(v, drop, factor);
         store8(out + r * ldo + col, 0, hi, v);
     }
 }
@@ -44,7 +45,7 @@ __global__ __launch_bounds__(256) void dropout_kernel(const T* x, int64_t ldx, T
 // KEPT (bf16): only the kept columns of dZ are written, side by side: a wavefront has a row's 512 columns, puts the kept
 // ones into LDS at their places and stores 16 bytes a lane; the chunks that panels share go out element by element.
 template <typename T, bool KEPT>
-__global__ __launch_bounds__(256) void act_back_kernel(const ActBack a, int across, int rows_each)
+__global__ __launch_bounds__(256, 4) void act_back_kernel(const ActBack a, int across, int rows_each)
 {
     constexpr int PANEL = 512, SLOTS = PANEL + 8 + 64;       // a row's panel, its place in a chunk, the zeros behind the last column
     __shared__ float sums[256 * 8];

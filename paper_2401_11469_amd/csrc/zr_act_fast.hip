@@ -132,7 +132,7 @@ int launch_tile(const FinishFArgs& a, int i_base, int i_end, int j_base, int j_e
 
 // Tile shapes as for the products without an end of their own (see launch_shape in zr_gemm_fast.hip).
 template <template <int, int> class LA, template <int, int> class LB, template <int, int> class RA, template <int, int> class RB>
-int launch_shape(const FinishFArgs& a, hipStream_t stream)
+int launch_shape(const FinishFArgs& a, const GemmDesc& d, hipStream_t stream)
 {
     constexpr bool rows_of_w = std::is_same<LB<128, 256>, DmaP<128, 256>>::value;
     if (const int f = forced_tiles()) {
@@ -158,6 +158,9 @@ int launch_shape(const FinishFArgs& a, hipStream_t stream)
     if (sc.big_i_end == 0) return launch_tile<LA, LB, RA, RB, 128, 128, 2, 2>(a, 0, a.I, 0, a.J, stream);
     const int st = launch_tile<LA, LB, RA, RB, 256, 256, 2, 4>(a, 0, sc.big_i_end, 0, sc.big_j_end, stream);
     if (st != ZR_OK || (sc.big_i_end >= a.I && sc.big_j_end >= a.J)) return st;
+    // A few columns behind the panel: 32 x 32 tiles that split each stage over their wavefronts, one to a compute unit, instead of 128 x 128
+    // ones in slices (8192 x 4096, 16 columns behind 2048: 27 us in two launches, now 17).
+    if (!sc.cut_rows && a.J - sc.big_j_end <= 64) return launch_act_narrow(d, sc.big_j_end, stream);
     if (sc.cut_rows) return launch_tile<LA, LB, RA, RB, 128, 128, 2, 2>(a, sc.big_i_end, a.I, 0, a.J, stream);
     return launch_tile<LA, LB, RA, RB, 128, 128, 2, 2>(a, 0, a.I, sc.big_j_end, a.J, stream);
 }
@@ -175,8 +178,8 @@ int launch_act_fast(const GemmDesc& d, hipStream_t stream)
     FinishFArgs a;
     (FArgs&)a = fargs_of(d);
     a.f = *d.finish;
-    if (d.B.c_contig) return launch_shape<DmaP, DmaP, RingP, RingP>(a, stream);
-    return d.B.map_strided ? launch_shape<DmaP, DmaQM, RingP, RingQM>(a, stream) : launch_shape<DmaP, DmaQ, RingP, RingQ>(a, stream);
+    if (d.B.c_contig) return launch_shape<DmaP, DmaP, RingP, RingP>(a, d, stream);
+    return d.B.map_strided ? launch_shape<DmaP, DmaQM, RingP, RingQM>(a, d, stream) : launch_shape<DmaP, DmaQ, RingP, RingQ>(a, d, stream);
 }
 
 }  // namespace zr

@@ -87,6 +87,7 @@ struct Args {
 };
 struct FinishArgs : Args {
     Finish f;
+    int j_base = 0;             // first column of D that the launch covers (the other kernels' tiles lie before it)
 };
 
 // element e of the result is element e + sh of v, 0 past its end (sh >= 0)
@@ -405,7 +406,9 @@ __device__ __forceinline__ void gemm_body(const G& g, uint32_t* smem, const int 
     const int grp_sz = 4 * g.tiles_j;
     const int first_i = lin / grp_sz * 4, within = lin % grp_sz;
     const int rows_in = min(4, g.tiles_i - first_i);
-    const int i0 = (first_i + within % rows_in) * R, j0 = within / rows_in * R;
+    int j0 = within / rows_in * R;
+    const int i0 = (first_i + within % rows_in) * R;
+    if constexpr (std::is_same_v<G, FinishArgs>) j0 += g.j_base;
 
     const int wr0 = WPT == 1 ? 0 : ((wave >> 1) & 1) * (R / 2), wc0 = WPT == 1 ? 0 : (wave & 1) * (R / 2);
     const int k0 = wave / WPT * (BK / KG);
@@ -760,6 +763,7 @@ int launch_inst(const G& a, const char* name, hipStream_t stream)
     G k = a;
     k.tiles_i = (a.I + R - 1) / R;
     k.tiles_j = (a.J + R - 1) / R;
+    if constexpr (finishes) k.tiles_j = (a.J - a.j_base + R - 1) / R;
     const int64_t tiles = (int64_t)k.tiles_i * k.tiles_j;
     if (tiles > 0x7ffffff0) return ZR_ERR_LIMIT;
     hipLaunchKernelGGL(fn, dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(NT), smem, stream, k);

@@ -595,7 +595,7 @@ def _vec(t: Optional[torch.Tensor], n: int, dt, here: int, name: str):
     """Pointer of a vector of n values of dtype dt, None: None."""
     if t is None:
         return None
-    if t.dtype is not dt or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous() or t.get_device() != here:
+    if t.dtype is not dt or t.shape != (n,) or not t.is_contiguous() or t.get_device() != here:
         raise ValueError(f"{name}: need a contiguous vector of {n} {dt} on the current GPU")
     return t.data_ptr()
 
@@ -604,9 +604,10 @@ def _like(t: Optional[torch.Tensor], shape, dt, here: int, name: str):
     """(pointer, leading dimension) of a matrix of this shape and dtype, None: (None, 0)."""
     if t is None:
         return None, 0
-    if t.shape != shape or t.dtype is not dt:
-        raise ValueError(f"{name}: need {tuple(shape)} of {dt}")
-    return _grid(t, here, name)
+    ld, one = t.stride() if t.dtype is dt and t.shape == shape else (0, 0)
+    if one != 1 or t.get_device() != here:
+        raise ValueError(f"{name}: need {tuple(shape)} of {dt} with unit column stride, on the current GPU")
+    return t.data_ptr(), ld
 
 
 def _generator(rng: Optional[torch.Tensor], here: int):
@@ -635,7 +636,7 @@ def dropout(x: torch.Tensor, p: float, rng: Optional[torch.Tensor], out: Optiona
     if out is None:
         out = _empty(x.shape, x.dtype, x.device, stream)
     op, ldo = _like(out, x.shape, x.dtype, here, "out")
-    st = _lib.zr_dropout(xp, ldx, op, ldo, x.shape[0], x.shape[1], p, _generator(rng, here), _code(x.dtype), on)
+    st = _lib.zr_dropout(xp, ldx, op, ldo, x.shape[0], x.shape[1], p, _generator(rng, here) if p else None, _code(x.dtype), on)
     if st:
         raise ZrError(st)
     return out
@@ -675,7 +676,7 @@ def resized_linear_act_fwd(X: torch.Tensor, W: torch.Tensor, keep_idx: Optional[
     gp, ldg = _like(gate, (M, N), dt, here, "gate")
     rp, ldr = _like(residual, (M, N), dt, here, "residual")
     st = _lib.zr_resized_linear_act_fwd(xp, ldx, wp, ldw, yp, ldy, M, K, N, kp, nk, mode, w_layout, _code(dt),
-                                        _vec(bias, N, dt, here, "bias"), act, gp, ldg, p, _generator(rng, here), rp, ldr, zp, ldz,
+                                        _vec(bias, N, dt, here, "bias"), act, gp, ldg, p, _generator(rng, here) if p else None, rp, ldr, zp, ldz,
                                         *_scratch(workspace, here), on)
     if st:
         raise ZrError(st)
@@ -717,7 +718,7 @@ def resized_linear_act_bwd(X: Optional[torch.Tensor], W: torch.Tensor, dY: torch
         workspace = _empty(act_workspace_bytes(M, K, N, n_keep, mode, dt, True), torch.uint8, dY.device, stream, returned=False)
     st = _lib.zr_resized_linear_act_bwd(xp, ldx, wp, ldw, gyp, ldgy, zp, ldz, gp, ldg, dxp, lddx, dwp, lddw,
                                         _vec(dbias, N, dt, here, "dbias"), dgp, lddg, M, K, N, kp, nk, mode, w_layout, _code(dt), act, p,
-                                        _generator(rng, here), *_scratch(workspace, here), on)
+                                        _generator(rng, here) if p else None, *_scratch(workspace, here), on)
     if st:
         raise ZrError(st)
     return dX, dW
@@ -748,7 +749,7 @@ def block_join_fwd(y: torch.Tensor, x: torch.Tensor, norm: int = NORM_RMS, post:
     op, ldo = _like(x_out, shape, dt, here, "x_out")
     hp, ldh = _like(h, shape, dt, here, "h")
     st = _lib.zr_block_join_fwd(yp, ldy, xp, ldx, op, ldo, hp, ldh, rows, cols, (1 if post else 0) | (2 if pre else 0), norm, eps, p,
-                                _generator(rng, here), scale, _vec(bias, cols, dt, here, "bias"), _vec(gate, cols, dt, here, "gate"),
+                                _generator(rng, here) if p else None, scale, _vec(bias, cols, dt, here, "bias"), _vec(gate, cols, dt, here, "gate"),
                                 _vec(post_w, cols, dt, here, "post_w"), _vec(post_b, cols, dt, here, "post_b"),
                                 _vec(pre_w, cols, dt, here, "pre_w"), _vec(pre_b, cols, dt, here, "pre_b"), _code(dt), on)
     if st:
@@ -793,7 +794,7 @@ def block_join_bwd(dx_out: Optional[torch.Tensor], dh: Optional[torch.Tensor], x
     if workspace is None and any(s is not None for s in sums):
         workspace = _empty(block_join_workspace_bytes(rows, cols), torch.uint8, first.device, stream, returned=False)
     st = _lib.zr_block_join_bwd(gp, ldg, hp, ldh, xp, ldx, yp, ldy, dxp, lddx, dyp, lddy, rows, cols,
-                                (1 if post else 0) | (2 if pre else 0), norm, eps, p, _generator(rng, here), scale,
+                                (1 if post else 0) | (2 if pre else 0), norm, eps, p, _generator(rng, here) if p else None, scale,
                                 _vec(bias, cols, dt, here, "bias"), _vec(gate, cols, dt, here, "gate"),
                                 _vec(post_w, cols, dt, here, "post_w"), _vec(post_b, cols, dt, here, "post_b"),
                                 _vec(pre_w, cols, dt, here, "pre_w"), *sums, *_scratch(workspace, here), _code(dt), on)

@@ -48,7 +48,7 @@ def keep_of(g, n, ratio):
     return np.sort(g.permutation(n)[:k])
 
 
-def layer(M, K, N, dtype, mode_k, ratio, kn, act, bias, gate, p, residual, pad=0, off=0, workspace=True, seed=0, keep=None):
+def layer(M, K, N, dtype, mode_k, ratio, kn, act, bias, gate, p, residual, pad=0, off=0, workspace=True, seed=0, keep=None, split=False):
     """Forward and backward, checked."""
     from paper_2401_11469_amd import zr
     g = np.random.default_rng(seed + 1000 * M + K + N)
@@ -76,9 +76,9 @@ def layer(M, K, N, dtype, mode_k, ratio, kn, act, bias, gate, p, residual, pad=0
     (y, ey), (z, ez) = au.product(X, W, keep, mode_k, b, act, G, f, R, dtype)
     within(outs["Z"].np(), z, ez, "Z")
     within(outs["Y"].np(), y, ey, "Y")
-    # without Z, and without scratch where there was some: the same bits
+    # without Z, and without scratch where there was some: the same bits, unless kept columns were extracted or the contraction split there
     Y2 = zr.resized_linear_act_fwd(get("X"), get("W"), dev, bias=bv, residual=get("R"), **how)
-    if not (workspace and mode_k and dev is not None):
+    if not (workspace and (split or mode_k and dev is not None)):
         assert torch.equal(Y2, outs["Y"].t)
     else:
         within(Y2.double().cpu().numpy(), y, ey, "Y without scratch")
@@ -128,6 +128,25 @@ def test_pitches_and_alignments(dtype, mode_k, kn, pad, off):
     (0, 0, 2048, 128, 4096, 0.1), (1, 1, 2056, 256, 4104, 0.4), (0, 0, 2304, 328, 4000, 0.5), (0, 1, 768, 256, 768, 0.2), (1, 0, 768, 256, 768, 0.2)])
 def test_many_tiles(mode_k, kn, M, K, N, ratio):
     layer(M, K, N, "bf16", mode_k, ratio, kn, au.GELU, True, True, 0.1, True)
+
+
+@pytest.mark.parametrize("mode_k,kn,M,K,N,ratio", [(0, 0, 8192, 72, 2752, 0.25), (1, 1, 4096, 192, 4128, 0.25), (0, 1, 4096, 64, 4112, 0.0), (0, 0, 2112, 128, 8192, 0.0),
+                                                   (0, 0, 4200, 128, 5120, 0.2), (1, 1, 6144, 136, 3000, 0.0)])
+@pytest.mark.parametrize("workspace", [False, True])
+def test_panels_of_whole_rounds_and_what_they_leave(mode_k, kn, M, K, N, ratio, workspace):
+    layer(M, K, N, "bf16", mode_k, ratio, kn, au.SILU, True, True, 0.1, True, workspace=workspace)
+
+
+@pytest.mark.parametrize("mode_k,kn,M,K,N,ratio", [(0, 0, 200, 4096, 256, 0.25), (1, 1, 384, 2752, 512, 0.25), (0, 0, 130, 1536, 1000, 0.0), (1, 1, 128, 5120, 128, 0.0)])
+def test_split_contractions(mode_k, kn, M, K, N, ratio):
+    layer(M, K, N, "bf16", mode_k, ratio, kn, au.GELU, True, True, 0.1, True, split=True)
+
+
+@pytest.mark.parametrize("M", [1, 2, 4, 5, 8, 9, 16])
+@pytest.mark.parametrize("mode_k,kn,K,N,ratio", [(0, 0, 4096, 2752, 0.0), (0, 0, 1000, 2000, 0.3), (1, 1, 2752, 4096, 0.0), (1, 1, 2752, 1024, 0.25), (1, 1, 1001, 520, 0.0),
+                                                 (0, 0, 8, 4, 0.0), (0, 0, 7168, 40, 0.5), (1, 1, 7000, 8, 0.5)])
+def test_few_rows(M, mode_k, kn, K, N, ratio):
+    layer(M, K, N, "bf16", mode_k, ratio, kn, au.SILU, True, True, 0.1, True, workspace=M % 2 == 0)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
