@@ -29,6 +29,7 @@ struct FewArgs {
     const int32_t* rows;        // [N x K]: the kept rows of W, or nullptr; [K x N]: the kept contraction indices, or nullptr
     int extent;                 // of the axis that they index
     int M, J, C;                // rows of X, features multiplied, contraction
+    int x_extent;               // columns of X that may be read: C, or with zeros behind it a multiple of 64
     int N;                      // features of the output
     Bf* out; int64_t ldo;
     Finish f;
@@ -155,7 +156,8 @@ __global__ __launch_bounds__(64 * ROW_WAVES) void act_few_rows_kernel(const FewA
 }
 
 // ---- W stored [K x N] ----
-// ELEMS: X is read element by element (through the list, or where its rows are not 16-byte aligned).
+// ELEMS: X is read element by element (through the list, or where its rows are not 16-byte aligned); otherwise as it lies, also beside
+// a list, which its columns have been picked by before.
 template <bool ELEMS, int U>
 __global__ __launch_bounds__(1024) void act_few_cols_kernel(const FewArgs g)
 {
@@ -204,7 +206,7 @@ __global__ __launch_bounds__(1024) void act_few_cols_kernel(const FewArgs g)
             for (int h = 0; h < 2; ++h) w[u][h] = *(const u4*)(g.W + (size_t)row[u][h] * (size_t)g.ldw + from);
         if constexpr (!ELEMS) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) x[u] = *(const u4*)(xrow + min((s0 + WAVES * u) * STEP + 8 * q, g.C - 8));       // (C is a multiple of 8)
+            for (int u = 0; u < U; ++u) x[u] = *(const u4*)(xrow + min((s0 + WAVES * u) * STEP + 8 * q, g.x_extent - 8));       // (a multiple of 8)
         } else {
             int at[U][8];
             uint32_t h[U][8];
@@ -331,14 +333,17 @@ int launch_act_few(const GemmDesc& d, hipStream_t stream)
 {
     auto aligned = [](const Operand& o) { return (uintptr_t)o.base % 16 == 0 && o.ld % 8 == 0; };
     if (d.dtype != ZR_BF16 || d.I > ACT_FEW || !d.A.c_contig || d.B.map_contig || !aligned(d.B)) return -1;
-    const bool x_chunks = !d.A.map_contig && aligned(d.A) && d.C % 8 == 0;
+    // (extracted columns have zeros behind them, to a multiple of 64)
+    const int x_extent = d.A.zero_padded ? d.A.n_contig : d.C;
+    const bool x_chunks = !d.A.map_contig && aligned(d.A) && x_extent % 8 == 0;
     FewArgs a;
     a.X = (const Bf*)d.A.base; a.ldx = d.A.ld; a.W = (const Bf*)d.B.base; a.ldw = d.B.ld;
     a.rows = d.B.map_strided; a.extent = d.B.n_strided;
     a.M = d.I; a.J = d.J; a.C = d.C; a.N = d.epilogue == EPI_COL_SCATTER ? d.out_full : d.J;
     a.out = (Bf*)d.out; a.ldo = d.ldo; a.f = *d.finish;
+    a.x_extent = x_extent;
     if (d.B.c_contig) {
-        if (!x_chunks) return -1;
+        if (!x_chunks || d.C % 8 != 0) return -1;
         // Features of a workgroup by measurement (us in a graph, 4 / 8 / 16 of them): one row, 2752 x 4096 7.0 / 8.1 / 7.5, 640 x 2560
         // 4.0 / 4.2 / 5.4, 11008 x 4096 17.3 / 19.0 / 20.0; four rows, 2752 x 4096 8.6 / 9.1 / 8.2, 1728 x 5120 7.7 / 6.8 / 9.5
         // (sixteen wavefronts in place of eight: as fast on 16, 4 to 35 % slower on 4)
@@ -347,9 +352,9 @@ int launch_act_few(const GemmDesc& d, hipStream_t stream)
         return launch_rows<16>(a, stream);
     }
     if (d.J % 8 != 0 || d.epilogue != EPI_PLAIN) return -1;
-    // X through a list must be W's: one contraction for both
-    if (d.A.map_contig != d.B.map_strided) return -1;
-    return x_chunks ? launch_cols<false>(a, stream) : launch_cols<true>(a, stream);
+    if (x_chunks) return launch_cols<false>(a, stream);
+    // element by element through the list that picks rows of W, or where nothing is picked
+    return d.A.map_contig == d.B.map_strided ? launch_cols<true>(a, stream) : -1;
 }
 
 }  // namespace zr
