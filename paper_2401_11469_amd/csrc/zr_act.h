@@ -236,22 +236,29 @@ template <bool EXACT> __device__ __forceinline__ float recip(float x)
 }
 template <bool EXACT> __device__ __forceinline__ float sigmoid_of(float x) { return recip<EXACT>(1.f + exp_of<EXACT>(-x)); }
 
-// The normal distribution function at z, and its density.  bf16 results: half of erfc by formula 7.1.26 of Abramowitz and Stegun
-// (a polynomial of fifth degree in 1 / (1 + 0.3275911 x), times e^(-x^2)), off by 7.5e-8 at most, where a bf16 result is off by
-// 2^-9 of itself; it decays as it should, so that small results keep their size.  fp32 results: the library's erfc.
-template <bool EXACT> __device__ __forceinline__ float normal_cdf(float z, float& density)
+// z Phi(z) and Phi(z) + z phi(z), Phi the normal distribution function and phi its density.
+// bf16 results: half of erfc by formula 7.1.26 of Abramowitz and Stegun (a polynomial of fifth degree in 1 / (1 + 0.3275911 x), times
+// e^(-x^2)), off by 7.5e-8 at most, where a bf16 result is off by 2^-9 of itself; it decays as it should, so that small results keep
+// their size.  With the tail T = Phi(-|z|):  z Phi(z) = max(z, 0) - |z| T.  fp32 results: the library's erfc.
+template <bool EXACT, bool SLOPE> __device__ __forceinline__ void gelu_of(float z, float& a, float& s)
 {
-    const float e = exp_of<EXACT>(-0.5f * z * z);
-    density = 0.39894228f * e;
-    if constexpr (EXACT) return 0.5f * erfcf(-0.70710678f * z);
-    const float t = recip<EXACT>(fmaf(0.3275911f * 0.70710678f, fabsf(z), 1.f));
-    float s = 1.061405429f;
-    s = fmaf(s, t, -1.453152027f);
-    s = fmaf(s, t, 1.421413741f);
-    s = fmaf(s, t, -0.284496736f);
-    s = fmaf(s, t, 0.254829592f);
-    const float tail = 0.5f * s * t * e;
-    return z > 0.f ? 1.f - tail : tail;
+    if constexpr (EXACT) {
+        const float cdf = 0.5f * erfcf(-0.70710678f * z);
+        a = z * cdf;
+        if constexpr (SLOPE) s = fmaf(z, 0.39894228f * expf(-0.5f * z * z), cdf);
+    } else {
+        const float e = __builtin_amdgcn_exp2f(z * (z * -0.72134752f));            // e^(-z^2 / 2)
+        const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678f, fabsf(z), 1.f));
+        float p = 0.5f * 1.061405429f;
+        p = fmaf(p, t, 0.5f * -1.453152027f);
+        p = fmaf(p, t, 0.5f * 1.421413741f);
+        p = fmaf(p, t, 0.5f * -0.284496736f);
+        p = fmaf(p, t, 0.5f * 0.254829592f);
+        const float tail = p * t * e;
+        // (not fmaxf: NaN stays NaN)
+        a = fmaf(-fabsf(z), tail, z < 0.f ? 0.f : z);
+        if constexpr (SLOPE) s = fmaf(z, 0.39894228f * e, z > 0.f ? 1.f - tail : tail);
+    }
 }
 
 // a = act(z), s = act'(z) (SLOPE)
@@ -261,10 +268,7 @@ template <bool EXACT, bool SLOPE> __device__ __forceinline__ void act_one(int ac
         a = z < 0.f ? 0.f : z;          // (NaN stays NaN)
         s = z > 0.f ? 1.f : 0.f;
     } else if (act == ZR_ACT_GELU) {
-        float density;
-        const float cdf = normal_cdf<EXACT>(z, density);
-        a = z * cdf;
-        if constexpr (SLOPE) s = fmaf(z, density, cdf);
+        gelu_of<EXACT, SLOPE>(z, a, s);
     } else if (act == ZR_ACT_GELU_TANH) {
         // (1 + tanh u) / 2 is the sigmoid of 2 u, u = sqrt(2 / pi) (z + 0.044715 z^3)
         const float zz = z * z, t = sigmoid_of<EXACT>(1.59576912f * z * fmaf(0.044715f, zz, 1.f));
