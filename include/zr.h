@@ -345,7 +345,7 @@ typedef enum { ZR_ACT_NONE = 0, ZR_ACT_RELU = 1, ZR_ACT_GELU = 2, ZR_ACT_GELU_TA
  * (dropped columns of DROP_N: P = 0, so they hold what bias, activation and so on make of that).
  *  bias [N]; gate, residual, Z [M x N] with their pitches; all may be NULL: bias and residual add nothing, gate is 1, Z is not
  *  kept.  dtype: of all tensors.  Sums, activation and everything behind them are fp32, each output is rounded once.
- *  keep_idx NULL: nothing is pruned, n_keep is ignored.  Y may be gate or residual (same pitch); Z must not overlap another tensor.
+ *  keep_idx NULL: nothing is pruned, n_keep is ignored.  Y may be gate or residual (same pitch); else no output may overlap another tensor.
  *  workspace: optional, of zr_act_fwd_workspace_bytes bytes, 16-byte aligned (less is used as far as it reaches), for what
  *  zr_resized_linear_fwd extracts and for the slices of a split contraction, by the same rules; its contents are undefined
  *  afterwards, and calls that share one must be ordered on one stream.  Results repeat to the bit for a given size of it.
@@ -366,8 +366,8 @@ int zr_resized_linear_act_fwd(const void* X, int64_t ldx, const void* W, int64_t
  *  pitch); no other output may overlap an input.  X is needed for dW, W for dX.
  *  dZ is held in dtype between the two steps (bf16: one rounding more, before sums over all of its terms, as the matrix
  *  instruction takes its operands in bf16); dbias adds up dZ before that rounding, in fp32.
- *  workspace: of zr_act_bwd_workspace_bytes bytes, 16-byte aligned; needed where dZ is not dY itself (act, gate or p), or dbias is
- *  wanted (else NULL is allowed).  Less will do, down to dZ (M x N values of dtype, N rounded up to 64) and dbias's sums, with fewer ways open
+ *  workspace: of zr_act_bwd_workspace_bytes bytes, 16-byte aligned; needed where dZ is not dY itself (act, gate, p or dgate), or dbias is
+ *  wanted (else NULL is allowed); calls that share one must be ordered on one stream.  Less will do, down to dZ (M x N values of dtype, N rounded up to 64) and dbias's sums, with fewer ways open
  *  to the products.  Errors: as above; SHAPE also for a workspace that is too small, NULL without one. */
 size_t zr_act_bwd_workspace_bytes(int32_t M, int32_t K, int32_t N, int32_t n_keep, int mode, int dtype);
 int zr_resized_linear_act_bwd(const void* X, int64_t ldx, const void* W, int64_t ldw, const void* dY, int64_t lddy,
@@ -398,7 +398,8 @@ int zr_block_join_fwd(const void* y, int64_t ldy, const void* x, int64_t ldx, vo
  *  ZR_JOIN_POST or dgate.  Outputs: each may be NULL, not all; dpost_* need ZR_JOIN_POST, dpre_* ZR_JOIN_PRE (else MODE).  dx may be dx_out, dh or
  *  x_out, dy may be y (same pitch); dx and dy must not overlap.
  *  The norms are taken again, of x_out as it was stored.  fp32 sums over the rows, in a fixed order: results repeat to the bit.
- *  workspace: of zr_block_join_workspace_bytes(rows, cols) bytes, 16-byte aligned, where a vector's gradient is wanted (else NULL is allowed).
+ *  workspace: of zr_block_join_workspace_bytes(rows, cols) bytes, 16-byte aligned, where a vector's gradient is wanted (else NULL is allowed);
+ *  calls that share one must be ordered on one stream.
  *  Launches: 1, +1 for the vectors.  Errors: as for the forward pass; SHAPE also for a workspace that is too small, NULL without one. */
 size_t zr_block_join_workspace_bytes(int32_t rows, int32_t cols);
 int zr_block_join_bwd(const void* dx_out, int64_t lddxo, const void* dh, int64_t lddh, const void* x_out, int64_t ldxo,

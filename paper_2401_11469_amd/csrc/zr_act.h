@@ -255,8 +255,8 @@ template <bool EXACT, bool SLOPE> __device__ __forceinline__ void gelu_of(float 
         p = fmaf(p, t, 0.5f * -0.284496736f);
         p = fmaf(p, t, 0.5f * 0.254829592f);
         const float tail = p * t * e;
-        // (not fmaxf: NaN stays NaN)
-        a = fmaf(-fabsf(z), tail, z < 0.f ? 0.f : z);
+        // (not fmaxf: NaN stays NaN; an infinite z has no tail to be multiplied by)
+        a = fmaf(-fminf(fabsf(z), 3e38f), tail, z < 0.f ? 0.f : z);
         if constexpr (SLOPE) s = fmaf(z, 0.39894228f * e, z > 0.f ? 1.f - tail : tail);
     }
 }

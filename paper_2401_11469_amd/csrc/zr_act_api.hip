@@ -116,7 +116,8 @@ int zr_resized_linear_act_bwd(const void* X, int64_t ldx, const void* W, int64_t
     if (st != ZR_OK) return st;
 
     const bool products = dX || dW;
-    const bool changes = act != ZR_ACT_NONE || gate || a.drop;         // dZ is not dY itself
+    // dZ is not dY itself, or dY may be where dgate goes
+    const bool changes = act != ZR_ACT_NONE || gate || a.drop || dgate;
     const bool holds = products && changes;
     // bf16 products of kept columns read them side by side: dZ is written that way
     const bool kept = holds && dtype == ZR_BF16 && mode == ZR_DROP_N && n_keep < N && N > ACT_KEPT_ABOVE;

@@ -182,6 +182,22 @@ def test_in_place(dtype):
             assert torch.equal(t, dG) and torch.equal(gx, wx) and torch.equal(gw, ww), name
 
 
+def test_the_gate_gradient_of_a_plain_layer_over_dY():
+    """No activation, gate or dropout: dZ is dY, which dgate may replace."""
+    from paper_2401_11469_amd import zr
+    g = np.random.default_rng(16)
+    for dtype in ("bf16", "f32"):
+        M, K, N = 40, 64, 96
+        X, W, Z, dY = (torch.from_numpy(values(g, dtype, *s)).to(TORCH[dtype]).cuda() for s in ((M, K), (K, N), (M, N), (M, N)))
+        wx, ww = zr.resized_linear_act_bwd(X, W, dY)
+        want = torch.empty_like(dY)
+        zr.resized_linear_act_bwd(X, W, dY, Z=Z, dgate=want)
+        t = dY.clone()
+        gx, gw = zr.resized_linear_act_bwd(X, W, t, Z=Z, dgate=t)
+        assert torch.equal(gx, wx) and torch.equal(gw, ww) and torch.equal(t, want)
+        within(t.double().cpu().numpy(), (dY.double() * Z.double()).cpu().numpy(), au.U[dtype] * (dY.double() * Z.double()).abs().cpu().numpy() * 1.01, "dgate")
+
+
 def test_which_outputs_are_wanted_changes_none():
     from paper_2401_11469_amd import zr
     g = np.random.default_rng(6)
@@ -245,6 +261,8 @@ def test_activation_at_its_ends(act, dtype):
         dW = zr.resized_linear_act_bwd(X, t.cuda()[None].contiguous(), torch.ones_like(Y), act=act, Z=t.cuda()[None].contiguous(), need_dX=False)[1]
         ok &= np.abs(z) < 1e3
         within(np.where(ok, dW.double().cpu().numpy(), 0), np.where(ok, s, 0), np.where(np.abs(z) > 30, 1e-30, es) + 2 * 2.0 ** -8 * abs(s) + 1e-37, "slope")
+    up = torch.full((1, 8), float("inf"), dtype=TORCH[dtype], device="cuda")
+    assert torch.equal(zr.resized_linear_act_fwd(X, up, act=act), up)
     nan = torch.full((1, 8), float("nan"), dtype=TORCH[dtype], device="cuda")
     assert zr.resized_linear_act_fwd(X, nan, act=act).isnan().all()
 
