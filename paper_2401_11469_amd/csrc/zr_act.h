@@ -270,8 +270,9 @@ template <bool EXACT, bool SLOPE> __device__ __forceinline__ void act_one(int ac
     } else if (act == ZR_ACT_GELU) {
         gelu_of<EXACT, SLOPE>(z, a, s);
     } else if (act == ZR_ACT_GELU_TANH) {
-        // (1 + tanh u) / 2 is the sigmoid of 2 u, u = sqrt(2 / pi) (z + 0.044715 z^3)
-        const float zz = z * z, t = sigmoid_of<EXACT>(1.59576912f * z * fmaf(0.044715f, zz, 1.f));
+        // (1 + tanh u) / 2 is the sigmoid of 2 u, u = sqrt(2 / pi) (z + 0.044715 z^3), which is 0 or 1 long before z^2 is held at 1e12 (so
+        // that t (1 - t) = 0 has no infinity to meet)
+        const float zz = fminf(z * z, 1e12f), t = sigmoid_of<EXACT>(1.59576912f * z * fmaf(0.044715f, zz, 1.f));
         a = z * t;
         if constexpr (SLOPE) s = fmaf(z * t * (1.f - t), 1.59576912f * fmaf(0.134145f, zz, 1.f), t);
     } else if (act == ZR_ACT_SILU) {

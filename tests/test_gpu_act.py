@@ -267,6 +267,20 @@ def test_activation_at_its_ends(act, dtype):
     assert zr.resized_linear_act_fwd(X, nan, act=act).isnan().all()
 
 
+@pytest.mark.parametrize("act", range(1, 5))
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_slope_of_large_values(act, dtype):
+    """The slope is 1 or 0 there, also where z^2 is past the largest fp32 number."""
+    from paper_2401_11469_amd import zr
+    big = torch.tensor([1e6, 1e19, 1e20, 1e30, 3e38], dtype=TORCH[dtype], device="cuda")
+    z = torch.cat([big, -big])[None]
+    dY, out = torch.ones_like(z), torch.empty_like(z)
+    W = torch.eye(10, dtype=TORCH[dtype], device="cuda")
+    dX, _ = zr.resized_linear_act_bwd(None, W, dY, mode=zr.DROP_N, act=act, Z=z, dgate=out, need_dW=False)
+    assert dX.cpu().tolist() == [[1.0] * 5 + [0.0] * 5]
+    assert torch.equal(out, z.clamp(min=0))
+
+
 def test_another_stream_and_repeatability():
     from paper_2401_11469_amd import zr
     g = np.random.default_rng(8)
