@@ -47,11 +47,8 @@ struct ActBack {
 constexpr int ACT_KEPT_ABOVE = 256;        // (a wavefront has a row then)
 int act_slabs(int M, int N);
 int launch_act_back(const ActBack& a, int dtype, hipStream_t stream);
-// out[v][c] = sum over slabs of partial[(v * slabs + slab) * n + c], in slab order, for `vectors` of them (out[v] nullptr: skipped)
-constexpr int MAX_SUMS = 6;
-struct SumOut { void* out[MAX_SUMS]; };
-enum { SUM_BIAS, SUM_GATE, SUM_POST_W, SUM_POST_B, SUM_PRE_W, SUM_PRE_B };       // of a join's vectors
-int launch_sum_slabs(const float* partial, int slabs, int n, int vectors, const SumOut& out, int dtype, hipStream_t stream);
+// out[c] = sum over slabs of partial[slab * n + c], in slab order
+int launch_sum_slabs(const float* partial, int slabs, int n, void* out, int dtype, hipStream_t stream);
 int launch_dropout(const void* x, int64_t ldx, void* out, int64_t ldo, int rows, int cols, const uint64_t* rng, uint32_t drop,
                    float factor, int dtype, hipStream_t stream);
 
@@ -71,15 +68,18 @@ struct Join {
     const void* dh; int64_t lddh;
     void* dx; int64_t lddx;
     void* dy; int64_t lddy;
-    float* partial;                        // [vectors x slabs x cols]
+    float* partial;                        // [sums x slabs x cols], the sums below; without `biases` the first two
     int slabs;
+    void* vectors[6];                      // gradients of bias, gate, post_w, post_b, pre_w, pre_b; each may be nullptr
     int biases;                            // sums of d, dh or dy are wanted: a gradient of bias, post_b or pre_b, or of the gate beside a post_b
 };
+enum { SUM_DT, SUM_HAT, SUM_D, SUM_DY, SUM_DH, JOIN_SUMS };     // over the rows: of d t, dh times the pre norm's value, d, dy, dh
 int join_max_cols();
 int join_most_slabs(int rows, int cols);                // of any backward call of this size
 int join_slabs(const Join& j);                          // of this one
 int launch_join(const Join& j, int dtype, hipStream_t stream);
 int launch_join_back(const Join& j, int dtype, hipStream_t stream);
+int launch_join_sums(const Join& j, int dtype, hipStream_t stream);
 
 // products with a Finish (GemmDesc::finish set): any alignment, and fp32
 constexpr int ACT_FEW = 16;     // rows of X up to which launch_act_few takes a product
@@ -270,11 +270,11 @@ template <bool EXACT, bool SLOPE> __device__ __forceinline__ void act_one(int ac
     } else if (act == ZR_ACT_GELU) {
         gelu_of<EXACT, SLOPE>(z, a, s);
     } else if (act == ZR_ACT_GELU_TANH) {
-        // (1 + tanh u) / 2 is the sigmoid of 2 u, u = sqrt(2 / pi) (z + 0.044715 z^3), which is 0 or 1 long before z^2 is held at 1e12 (so
-        // that t (1 - t) = 0 has no infinity to meet)
-        const float zz = fminf(z * z, 1e12f), t = sigmoid_of<EXACT>(1.59576912f * z * fmaf(0.044715f, zz, 1.f));
+        // (1 + tanh u) / 2 is the sigmoid of 2 u, u = sqrt(2 / pi) (z + 0.044715 z^3)
+        const float zz = z * z, t = sigmoid_of<EXACT>(1.59576912f * z * fmaf(0.044715f, zz, 1.f));
         a = z * t;
-        if constexpr (SLOPE) s = fmaf(z * t * (1.f - t), 1.59576912f * fmaf(0.134145f, zz, 1.f), t);
+        // (1 - t = 0 or t = 0 long before z^2 is held at 1e12: no infinity to be multiplied by)
+        if constexpr (SLOPE) s = fmaf(z * t * (1.f - t), 1.59576912f * fmaf(0.134145f, fminf(zz, 1e12f), 1.f), t);
     } else if (act == ZR_ACT_SILU) {
         const float t = sigmoid_of<EXACT>(z);
         a = z * t;

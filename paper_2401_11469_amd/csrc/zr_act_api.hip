@@ -137,9 +137,7 @@ int zr_resized_linear_act_bwd(const void* X, int64_t ldx, const void* W, int64_t
         st = launch_act_back(a, dtype, s);
         if (st != ZR_OK) return st;
         if (dbias) {
-            SumOut out = {};
-            out.out[0] = dbias;
-            st = launch_sum_slabs(a.partial, act_slabs(M, N), N, 1, out, dtype, s);
+            st = launch_sum_slabs(a.partial, act_slabs(M, N), N, dbias, dtype, s);
             if (st != ZR_OK) return st;
         }
     }
@@ -184,7 +182,7 @@ int zr_block_join_fwd(const void* y, int64_t ldy, const void* x, int64_t ldx, vo
 size_t zr_block_join_workspace_bytes(int32_t rows, int32_t cols)
 {
     if (rows < 1 || cols < 1 || cols > join_max_cols()) return 0;
-    return (size_t)MAX_SUMS * (size_t)join_most_slabs(rows, cols) * (size_t)cols * 4;
+    return (size_t)JOIN_SUMS * (size_t)join_most_slabs(rows, cols) * (size_t)cols * 4;
 }
 
 int zr_block_join_bwd(const void* dx_out, int64_t lddxo, const void* dh, int64_t lddh, const void* x_out, int64_t ldxo,
@@ -224,8 +222,9 @@ int zr_block_join_bwd(const void* dx_out, int64_t lddxo, const void* dh, int64_t
     hipStream_t s = (hipStream_t)stream;
     st = launch_join_back(j, dtype, s);
     if (st != ZR_OK || !vectors) return st;
-    const SumOut out = {{dbias, dgate, dpost_w, dpost_b, dpre_w, dpre_b}};
-    return launch_sum_slabs(j.partial, j.slabs, cols, MAX_SUMS, out, dtype, s);
+    void* const gradients[6] = {dbias, dgate, dpost_w, dpost_b, dpre_w, dpre_b};
+    std::copy(gradients, gradients + 6, j.vectors);
+    return launch_join_sums(j, dtype, s);
 }
 
 }  // extern "C"

@@ -179,32 +179,72 @@ __global__ __launch_bounds__(256, 4) void act_back_kernel(const ActBack a, int a
 // Sums over slabs: 64 columns to a workgroup, sixteen wavefronts along the slabs, eight loads of each on their way, added in a fixed
 // order.  Latency bound: 2.4 to 5 us.
 // ---------------------------------------------------------------------------
-template <typename T>
-__global__ __launch_bounds__(1024) void sum_slabs_kernel(const float* partial, int slabs, int n, const SumOut out)
+constexpr int SLAB_WAVES = 16;
+// of this wavefront's slabs; column c below n
+__device__ __forceinline__ float slab_sum(const float* p, int slabs, int n, int c, int wave)
 {
-    constexpr int W = 16, U = 8;
-    __shared__ float part[W][64];
-    void* dst = out.out[0];
-#pragma unroll
-    for (int v = 1; v < MAX_SUMS; ++v) dst = (int)blockIdx.y == v ? out.out[v] : dst;
-    if (!dst) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = (int)blockIdx.x * 64 + lane;
-    const float* p = partial + (size_t)blockIdx.y * (size_t)slabs * (size_t)n;
+    constexpr int W = SLAB_WAVES, U = 8;
     float v = 0.f;
-    for (int s = wave; s < slabs && c < n; s += W * U) {
+    for (int s = wave; s < slabs; s += W * U) {
         float x[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) x[u] = p[(size_t)min(s + W * u, slabs - 1) * (size_t)n + c];
 #pragma unroll
         for (int u = 0; u < U; ++u) v += s + W * u < slabs ? x[u] : 0.f;
     }
-    part[wave][lane] = v;
+    return v;
+}
+
+template <typename T>
+__global__ __launch_bounds__(1024) void sum_slabs_kernel(const float* partial, int slabs, int n, T* out)
+{
+    __shared__ float part[SLAB_WAVES][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = (int)blockIdx.x * 64 + lane;
+    part[wave][lane] = slab_sum(partial, slabs, n, min(c, n - 1), wave);
     __syncthreads();
     if (wave == 0 && c < n) {
         float sum = 0.f;
 #pragma unroll
-        for (int w = 0; w < W; ++w) sum += part[w][lane];
-        put_one((T*)dst + c, sum);
+        for (int w = 0; w < SLAB_WAVES; ++w) sum += part[w][lane];
+        put_one(out + c, sum);
+    }
+}
+
+// The gradients of a join's vectors, one to a row of the grid: one of the sums, or of SUM_DT and SUM_D with scale and
+//   dgate = scale (post_w sum d t + post_b sum d),  dpost_w = scale gate sum d t,  dpost_b = scale gate sum d
+template <typename T>
+__global__ __launch_bounds__(1024) void join_sums_kernel(const Join j)
+{
+    __shared__ float part[2][SLAB_WAVES][64];
+    const int which = blockIdx.y;
+    void* out = j.vectors[0];
+    int first = SUM_DY;
+    const void* weight = nullptr;
+    if (which == 1) { out = j.vectors[1]; first = SUM_DT; weight = j.post ? j.post_w : nullptr; }
+    if (which == 2) { out = j.vectors[2]; first = SUM_DT; weight = j.gate; }
+    if (which == 3) { out = j.vectors[3]; first = SUM_D; weight = j.gate; }
+    if (which == 4) { out = j.vectors[4]; first = SUM_HAT; }
+    if (which == 5) { out = j.vectors[5]; first = SUM_DH; }
+    if (!out) return;
+    const bool both = which == 1 && j.post && j.post_b;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = (int)blockIdx.x * 64 + lane, at = min(c, j.cols - 1);
+    const size_t size = (size_t)j.slabs * (size_t)j.cols;
+    float w = which >= 1 && which <= 3 ? j.scale : 1.f, w2 = j.scale;
+    if (weight) w *= one_of((const T*)weight + at);
+    if (both) w2 *= one_of((const T*)j.post_b + at);
+    part[0][wave][lane] = slab_sum(j.partial + size * (size_t)first, j.slabs, j.cols, at, wave);
+    if (both) part[1][wave][lane] = slab_sum(j.partial + size * (size_t)SUM_D, j.slabs, j.cols, at, wave);
+    __syncthreads();
+    if (wave == 0 && c < j.cols) {
+        float sum = 0.f, sum2 = 0.f;
+#pragma unroll
+        for (int i = 0; i < SLAB_WAVES; ++i) {
+            sum += part[0][i][lane];
+            if (both) sum2 += part[1][i][lane];
+        }
+        sum *= w;
+        if (both) sum = fmaf(w2, sum2, sum);
+        put_one((T*)out + c, sum);
     }
 }
 
@@ -251,11 +291,19 @@ int launch_act_back(const ActBack& a, int dtype, hipStream_t stream)
     return hip_status(hipGetLastError());
 }
 
-int launch_sum_slabs(const float* partial, int slabs, int n, int vectors, const SumOut& out, int dtype, hipStream_t stream)
+int launch_sum_slabs(const float* partial, int slabs, int n, void* out, int dtype, hipStream_t stream)
 {
-    const dim3 grid((unsigned)((n + 63) / 64), (unsigned)vectors);
-    if (dtype == ZR_BF16) hipLaunchKernelGGL(sum_slabs_kernel<Bf>, grid, dim3(1024), 0, stream, partial, slabs, n, out);
-    else hipLaunchKernelGGL(sum_slabs_kernel<float>, grid, dim3(1024), 0, stream, partial, slabs, n, out);
+    const dim3 grid((unsigned)((n + 63) / 64));
+    if (dtype == ZR_BF16) hipLaunchKernelGGL(sum_slabs_kernel<Bf>, grid, dim3(64 * SLAB_WAVES), 0, stream, partial, slabs, n, (Bf*)out);
+    else hipLaunchKernelGGL(sum_slabs_kernel<float>, grid, dim3(64 * SLAB_WAVES), 0, stream, partial, slabs, n, (float*)out);
+    return hip_status(hipGetLastError());
+}
+
+int launch_join_sums(const Join& j, int dtype, hipStream_t stream)
+{
+    const dim3 grid((unsigned)((j.cols + 63) / 64), 6);
+    if (dtype == ZR_BF16) hipLaunchKernelGGL(join_sums_kernel<Bf>, grid, dim3(64 * SLAB_WAVES), 0, stream, j);
+    else hipLaunchKernelGGL(join_sums_kernel<float>, grid, dim3(64 * SLAB_WAVES), 0, stream, j);
     return hip_status(hipGetLastError());
 }
 

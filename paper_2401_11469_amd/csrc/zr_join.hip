@@ -5,7 +5,7 @@
 // NT threads take a row, NV groups of eight columns a thread; rows of up to 512 columns run on one wavefront without a barrier.
 // The backward pass normalises again from y and x_out (a few instructions; kept statistics would be read and, of a stored
 // x_out, be slightly off), and every thread adds up the gradients of the vectors for its columns over all rows of its workgroup;
-// a second launch adds the workgroups' sums in their order.
+// a second launch adds the workgroups' sums in their order and makes the vectors' gradients of them.
 // Measured, bf16: 12608 x 1024, layer norm, dropout, bias and gate 20.6 us (5.0 TB/s); backward, 8192 x 4096, two norms 79 to 87 us
 // (4.6 to 5.1 TB/s) and 4.5 for the second launch.
 #include <type_traits>
@@ -492,69 +492,45 @@ __global__ __launch_bounds__(NT * groups_of<NT>(), (back_waves<T, NT, BIASES>())
     }
 
     if (!j.partial) return;
-    // the sums of the G rows that a workgroup takes at a time, in their order
-    __shared__ __align__(16) float all[G > 1 ? BLOCK * 8 : 4];
-    auto joined = [&](float (&x)[NV][8]) {
-        if constexpr (G > 1) {
-#pragma unroll
-            for (int k = 0; k < NV; ++k) {
-                __syncthreads();
-                store8(all + threadIdx.x * 8, 0, 8, x[k]);
-                __syncthreads();
-                if (threadIdx.x < NT)
-#pragma unroll
-                    for (int q = 1; q < G; ++q)
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) x[k][e] += all[(threadIdx.x + NT * q) * 8 + e];
-            }
-        }
-    };
-    auto keep = [&](int which, const float (&x)[NV][8]) {
-        if (G > 1 && threadIdx.x >= NT) return;
-        c.template put<float>(j.partial + ((size_t)which * (size_t)j.slabs + blockIdx.x) * (size_t)j.cols, 0, x);
-    };
-    joined(A);
-    if constexpr (BIASES) {
-        joined(B);
-        joined(D);
-        keep(SUM_BIAS, D);
-    }
-    if constexpr (PRE) {
-        joined(P);
-        keep(SUM_PRE_W, P);
+    const int64_t size = (int64_t)j.slabs * j.cols;
+    float* dst = j.partial + (int64_t)blockIdx.x * j.cols;
+    if constexpr (G == 1) {
+        c.template put<float>(dst, SUM_DT * size, A);
+        if constexpr (PRE) c.template put<float>(dst, SUM_HAT * size, P);
         if constexpr (BIASES) {
-            joined(Q);
-            keep(SUM_PRE_B, Q);
-        }
-    }
-    auto scaled = [&](const float (&x)[NV][8], const void* v, float (&out)[NV][8]) {
-        float w[NV][8];
-        vector_of<T, NV>(w, v, 1.f, c);
-#pragma unroll
-        for (int k = 0; k < NV; ++k)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) out[k][e] = j.scale * w[k][e] * x[k][e];
-    };
-    float v[NV][8];
-    if constexpr (POST) {
-        scaled(A, j.gate, v);
-        keep(SUM_POST_W, v);
-        if constexpr (BIASES) {
-            scaled(B, j.gate, v);
-            keep(SUM_POST_B, v);
-        }
-        scaled(A, j.post_w, v);
-        if constexpr (BIASES) {
-            if (j.post_b) {
-                float w[NV][8];
-                scaled(B, j.post_b, w);
-                add<NV>(v, w);
-            }
+            c.template put<float>(dst, SUM_D * size, B);
+            c.template put<float>(dst, SUM_DY * size, D);
+            if constexpr (PRE) c.template put<float>(dst, SUM_DH * size, Q);
         }
     } else {
-        scaled(A, nullptr, v);
+        // the sums of the G rows that a workgroup takes at a time, added up in their order
+        static_assert(NV == 1, "a group of eight columns a thread");
+        constexpr int COUNT = BIASES ? JOIN_SUMS : 2, WIDTH = NT * 8;
+        __shared__ __align__(16) float all[COUNT][BLOCK * 8];
+        auto keep = [&](int which, const float (&x)[NV][8]) { store8(all[which] + threadIdx.x * 8, 0, 8, x[0]); };
+        keep(SUM_DT, A);
+        keep(SUM_HAT, P);
+        if constexpr (BIASES) {
+            keep(SUM_D, B);
+            keep(SUM_DY, D);
+            keep(SUM_DH, Q);
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < COUNT * (WIDTH / 4); i += BLOCK) {
+            const int which = i / (WIDTH / 4), col = i % (WIDTH / 4) * 4;
+            f4 v = *(const f4*)(all[which] + col);
+#pragma unroll
+            for (int q = 1; q < G; ++q) v += *(const f4*)(all[which] + WIDTH * q + col);
+            float* p = dst + which * size + col;
+            if (col + 4 <= j.cols) {
+                *(f4_any*)p = v;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (col + e < j.cols) p[e] = v[e];
+            }
+        }
     }
-    keep(SUM_GATE, v);
 }
 
 template <typename T, int NT, int NV, bool BACK>
@@ -626,7 +602,7 @@ int join_most_slabs(int rows, int cols) { return blocks_of(rows, shape_of(cols))
 int join_slabs(const Join& j)
 {
     // (two turns at least where there are sums: those of a workgroup with one are as much to write and read as its rows; 985 x 1023
-    // in fp32, all gradients, with 1 / 2 / 4 / 8: 22.6, 20.5, 24.5, 36.7 us)
+    // in fp32, all gradients, with 1 / 2 / 3 / 4: 20.2, 19.7, 22.3, 24.6 us)
     const Shape s = back_shape_of(j);
     const int64_t turns = ((int64_t)j.rows + s.rows_at_once - 1) / s.rows_at_once;
     const int64_t most = std::min<int64_t>(blocks_of(j.rows, s), join_most_slabs(j.rows, j.cols));

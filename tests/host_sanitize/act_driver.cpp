@@ -41,14 +41,23 @@ int launch_act_back(const ActBack& a, int dtype, hipStream_t)
     check_drop(a.rng, a.drop, a.factor);
     return ZR_OK;
 }
-int launch_sum_slabs(const float* partial, int slabs, int n, int vectors, const SumOut& out, int, hipStream_t)
+int launch_sum_slabs(const float* partial, int slabs, int n, void* out, int, hipStream_t)
 {
     ++g_launches;
-    require(vectors >= 1 && vectors <= MAX_SUMS && slabs >= 1 && n >= 1, "sums");
-    require(within(partial, (size_t)vectors * slabs * n * 4), "sums past the workspace");
+    require(slabs >= 1 && n >= 1, "sums");
+    require(within(partial, (size_t)slabs * n * 4), "sums past the workspace");
+    require(out != nullptr, "sums for nobody");
+    return ZR_OK;
+}
+int launch_join_sums(const Join& j, int, hipStream_t)
+{
+    ++g_launches;
+    require(j.slabs >= 1 && within(j.partial, (size_t)(j.biases ? (int)JOIN_SUMS : 2) * j.slabs * j.cols * 4), "sums past the workspace");
     bool any = false;
-    for (int v = 0; v < vectors; ++v) any |= out.out[v] != nullptr;
+    for (void* v : j.vectors) any |= v != nullptr;
     require(any, "sums for nobody");
+    require(j.biases || (!j.vectors[0] && !j.vectors[3] && !j.vectors[5] && !(j.vectors[1] && j.post && j.post_b)), "sums that were not taken");
+    require(j.pre || (!j.vectors[4] && !j.vectors[5]), "a norm's gradients without one");
     return ZR_OK;
 }
 int launch_dropout(const void* x, int64_t ldx, void* out, int64_t ldo, int rows, int cols, const uint64_t* rng, uint32_t drop, float factor, int, hipStream_t)
@@ -83,7 +92,7 @@ int launch_join_back(const Join& j, int, hipStream_t)
     require(!j.post || j.y, "the post norm's input");
     require((!j.y || j.ldy >= j.cols) && (!j.dx_out || j.lddxo >= j.cols) && (!j.dx || j.lddx >= j.cols) && (!j.dy || j.lddy >= j.cols), "pitches");
     require(j.dx || j.dy || j.partial, "a pass for nothing");
-    if (j.partial) require(within(j.partial, (size_t)MAX_SUMS * j.slabs * j.cols * 4), "sums past the workspace");
+    if (j.partial) require(within(j.partial, (size_t)(j.biases ? (int)JOIN_SUMS : 2) * j.slabs * j.cols * 4), "sums past the workspace");
     return ZR_OK;
 }
 }  // namespace zr

@@ -18,7 +18,7 @@ def test_kernels_around_the_products_do_not_spill():
         pytest.skip("no resource table (library not built by build.py here)")
     rows = [l.rstrip("\n").split(" | ") for l in open(build.RESOURCES) if not l.startswith("#")]
     for kind, least in (("act_fast_kernel<", 12), ("act_slice_kernel<", 3), ("act_reduce_kernel", 1), ("act_kernel<", 20), ("f32_act_kernel<", 20),
-                        ("act_few_rows_kernel<", 24), ("act_few_cols_kernel<", 9), ("act_back_kernel<", 3), ("dropout_kernel<", 2), ("sum_slabs_kernel<", 2),
+                        ("act_few_rows_kernel<", 24), ("act_few_cols_kernel<", 9), ("act_back_kernel<", 3), ("dropout_kernel<", 2), ("sum_slabs_kernel<", 2), ("join_sums_kernel<", 2),
                         ("join_kernel<", 40), ("join_back_kernel<", 100)):
         mine = [r for r in rows if r[0].startswith(kind)]
         assert len(mine) >= least, (kind, len(mine))
