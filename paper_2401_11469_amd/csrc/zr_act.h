@@ -86,7 +86,7 @@ constexpr int ACT_FEW = 16;     // rows of X up to which launch_act_few takes a 
 constexpr int ACT_FEW_GATHERED = 4;     // and up to which it is left to gather the kept columns of X
 int launch_act_few(const GemmDesc& d, hipStream_t stream);      // bf16, few rows; -1: not taken
 int launch_act_any(const GemmDesc& d, hipStream_t stream);
-int launch_act_narrow(const GemmDesc& d, int j_base, hipStream_t stream);      // columns j_base .. of a product without lists on a contiguous axis, on 32 x 32 tiles
+int launch_act_narrow(const GemmDesc& d, int j_base, hipStream_t stream);      // columns j_base .. of a product without lists on a contiguous axis, on 32 x 32 tiles; -1: not taken
 int launch_act_fast(const GemmDesc& d, hipStream_t stream);     // bf16, 16-byte aligned rows; -1: not taken
 int launch_act_f32(const GemmDesc& d, hipStream_t stream);
 

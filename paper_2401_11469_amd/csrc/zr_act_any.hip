@@ -24,6 +24,8 @@ int launch_act_any(const GemmDesc& d, hipStream_t stream)
 
 int launch_act_narrow(const GemmDesc& d, int j_base, hipStream_t stream)
 {
+    // (what Plain reads at a time has to be there: extracted columns can be fewer, with their zeros behind them)
+    if (too_short(d, d.A) || too_short(d, d.B)) return -1;
     FinishArgs a;
     (Args&)a = args_of(d);
     a.f = *d.finish;

@@ -162,7 +162,10 @@ int launch_shape(const FinishFArgs& a, const GemmDesc& d, hipStream_t stream)
     if (st != ZR_OK || (sc.big_i_end >= a.I && sc.big_j_end >= a.J)) return st;
     // A few columns behind the panel: 32 x 32 tiles that split each stage over their wavefronts, one to a compute unit, instead of 128 x 128
     // ones in slices (8192 x 4096, 16 columns behind 2048: 27 us in two launches, now 17).
-    if (!sc.cut_rows && a.J - sc.big_j_end <= 64) return launch_act_narrow(d, sc.big_j_end, stream);
+    if (!sc.cut_rows && a.J - sc.big_j_end <= 64) {
+        const int rest = launch_act_narrow(d, sc.big_j_end, stream);
+        if (rest >= 0) return rest;
+    }
     if (sc.cut_rows) return launch_tile<LA, LB, RA, RB, 128, 128, 2, 2>(a, sc.big_i_end, a.I, 0, a.J, stream);
     return launch_tile<LA, LB, RA, RB, 128, 128, 2, 2>(a, 0, a.I, sc.big_j_end, a.J, stream);
 }
