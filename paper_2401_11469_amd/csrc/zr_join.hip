@@ -422,7 +422,7 @@ __global__ __launch_bounds__(NT * groups_of<NT>(), (back_waves<T, NT, BIASES>())
         // the next row's values travel while this one's are used (past the last row: the last one's again)
         if constexpr (!LEAN) fetch(base + step);
         if constexpr (G > 1) {
-            // (a group of threads behind the last row has that row's values again, and adds nothing)
+            // (a group of threads behind the last row has that row's values again, and adds nothing: see below)
             if (!on) { zero(d); zero(g); }
         }
         if (j.bias) {
@@ -449,6 +449,15 @@ __global__ __launch_bounds__(NT * groups_of<NT>(), (back_waves<T, NT, BIASES>())
         if constexpr (POST && PRE) normalise<NV, true>(x, t, rr, rt, c, j.cols, LAYER, j.eps, sums);
         else if constexpr (PRE) normalise<NV, false>(x, x, rr, rt, c, j.cols, LAYER, j.eps, sums);
         else if constexpr (POST) normalise<NV, false>(t, t, rt, rr, c, j.cols, LAYER, j.eps, sums);
+        if constexpr (G > 1) {
+            // (its draws are those of a row that there is not: values that the last row drops, whatever they are, may be kept in t, and
+            // zeros have no deviation with eps 0; 0 times either is no 0)
+            if (!on) {
+                zero(t);
+                if constexpr (PRE) zero(x);
+                rt = rr = 0.f;
+            }
+        }
         if constexpr (PRE) {
             add_product<NV>(P, g, x);
             if constexpr (BIASES) add<NV>(Q, g);
@@ -487,7 +496,10 @@ __global__ __launch_bounds__(NT * groups_of<NT>(), (back_waves<T, NT, BIASES>())
                 for (int e = 0; e < 8; ++e) d[k][e] *= j.scale;
         }
         if (j.drop) drop(d);
-        if constexpr (BIASES) add<NV>(D, d);
+        if constexpr (BIASES) {
+            if constexpr (G > 1) { if (!on) zero(d); }          // (0 times a gate or weight that is no number)
+            add<NV>(D, d);
+        }
         if (j.dy && on) c.template put<T>(j.dy, row * j.lddy, d);
     }
 
