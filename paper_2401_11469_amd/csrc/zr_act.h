@@ -236,10 +236,12 @@ template <bool EXACT> __device__ __forceinline__ float recip(float x)
 }
 template <bool EXACT> __device__ __forceinline__ float sigmoid_of(float x) { return recip<EXACT>(1.f + exp_of<EXACT>(-x)); }
 
-// z Phi(z) and Phi(z) + z phi(z), Phi the normal distribution function and phi its density.
-// bf16 results: half of erfc by formula 7.1.26 of Abramowitz and Stegun (a polynomial of fifth degree in 1 / (1 + 0.3275911 x), times
-// e^(-x^2)), off by 7.5e-8 at most, where a bf16 result is off by 2^-9 of itself; it decays as it should, so that small results keep
-// their size.  With the tail T = Phi(-|z|):  z Phi(z) = max(z, 0) - |z| T.  fp32 results: the library's erfc.
+// z Phi(z) and Phi(z) + z phi(z), Phi the normal distribution function and phi its density, by the tail T = Phi(-|z|):
+//   z Phi(z) = max(z, 0) - |z| T
+// bf16 results: T = t P(t) e^(-z^2 / 2) with t = 1 / (1 + 0.285 |z|), which goes to 0 as T e^(z^2 / 2) does (as 1 / |z|), and P of fifth
+// degree, fitted for the smallest largest error where 7e-8 counts as much as 4.5e-4 of T: off by 6e-8 and by 2.5e-4 of T at most, before
+// the roundings of fp32, where a bf16 result is off by 2^-9 of itself.  So small results keep their size, down to 1e-37 (one degree less: 3.5e-7
+// at these tails).  fp32 results: the library's erfc.
 template <bool EXACT, bool SLOPE> __device__ __forceinline__ void gelu_of(float z, float& a, float& s)
 {
     if constexpr (EXACT) {
@@ -248,12 +250,13 @@ template <bool EXACT, bool SLOPE> __device__ __forceinline__ void gelu_of(float 
         if constexpr (SLOPE) s = fmaf(z, 0.39894228f * expf(-0.5f * z * z), cdf);
     } else {
         const float e = __builtin_amdgcn_exp2f(z * (z * -0.72134752f));            // e^(-z^2 / 2)
-        const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678f, fabsf(z), 1.f));
-        float p = 0.5f * 1.061405429f;
-        p = fmaf(p, t, 0.5f * -1.453152027f);
-        p = fmaf(p, t, 0.5f * 1.421413741f);
-        p = fmaf(p, t, 0.5f * -0.284496736f);
-        p = fmaf(p, t, 0.5f * 0.254829592f);
+        const float t = __builtin_amdgcn_rcpf(fmaf(0.285f, fabsf(z), 1.f));
+        float p = -0.09544432f;
+        p = fmaf(p, t, 0.32764384f);
+        p = fmaf(p, t, -0.14764132f);
+        p = fmaf(p, t, 0.20968573f);
+        p = fmaf(p, t, 0.0899962f);
+        p = fmaf(p, t, 0.115759924f);
         const float tail = p * t * e;
         // (not fmaxf: NaN stays NaN; an infinite z has no tail to be multiplied by)
         a = fmaf(-fminf(fabsf(z), 3e38f), tail, z < 0.f ? 0.f : z);
