@@ -184,15 +184,7 @@ bool gemm_fast_can(const GemmDesc& d)
     return true;
 }
 
-// contractions of whole 64-deep stages, or with an operand that is padded to them
-static bool whole_stages(const GemmDesc& d)
-{
-    return d.C % BK == 0 || (d.A.c_contig && d.A.zero_padded) || (d.B.c_contig && d.B.zero_padded);
-}
-
-// Slices of the contraction that its launch on 128 x 128 tiles will make.  (Two slices of a contraction of no whole stages
-// below 1344 gain nothing: 216 tiles, 1264 deep 26 us in one piece, 30 in two.)
-static bool short_for_slices(const GemmDesc& d) { return !whole_stages(d) && d.C < 1344; }
+// Slices of the contraction that its launch on 128 x 128 tiles will make.
 static int slices_of(const GemmDesc& d, int64_t t128)
 {
     return short_for_slices(d) ? 1 : slices_for(d.C, t128, d.split_scratch, d.split_scratch_bytes, d.accumulate);

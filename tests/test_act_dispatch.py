@@ -27,3 +27,12 @@ def test_no_short_contraction_reaches_loads_of_eight(tmp_path):
              for n in (1, 4, 7) for kn in (True, False) for scratch in (True, False)]
     for c, got in zip(calls, names(tmp_path, calls)):
         assert got and not any("Plain, true" in g for g in got), (c, got)
+
+
+@pytest.mark.parametrize("C,pieces", [(1096, 1), (1264, 1), (1336, 1), (1280, 2), (1344, 2), (1400, 2)])
+def test_slices_by_the_rules_of_the_plain_product(tmp_path, C, pieces):
+    """216 tiles of 128 x 128: the contraction is cut in two with scratch where it is whole stages of 64 or at least 1344 long."""
+    call = dict(M=1536, K=C, N=2304, n_keep=None, mode_k=False, kn=False)
+    one, two = names(tmp_path, [dict(call, scratch=False), dict(call, scratch=True)])
+    assert one == ["act_fast_kernel<DmaP, DmaP, 64, 128, 1, 4>"]
+    assert two == (one if pieces == 1 else ["act_slice_kernel<DmaP, DmaP>", "act_reduce_kernel"])
