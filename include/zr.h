@@ -397,7 +397,8 @@ int zr_block_join_fwd(const void* y, int64_t ldy, const void* x, int64_t ldx, vo
  *  dx_out: NULL stands for zeros (allowed with ZR_JOIN_PRE).  dh, x_out: needed with ZR_JOIN_PRE, else ignored.  y: needed with
  *  ZR_JOIN_POST or dgate.  Outputs: each may be NULL, not all; dpost_* need ZR_JOIN_POST, dpre_* ZR_JOIN_PRE (else MODE).  dx may be dx_out, dh or
  *  x_out, dy may be y (same pitch); dx and dy must not overlap.
- *  The norms are taken again, of x_out as it was stored.  fp32 sums over the rows, in a fixed order: results repeat to the bit.
+ *  The norms are taken again, of x_out as it was stored.  fp32 sums over the rows, in an order that goes by the extents and by which vectors'
+ *  gradients are wanted: calls that are alike in these repeat to the bit, and dx and dy do whatever else is wanted.
  *  workspace: of zr_block_join_workspace_bytes(rows, cols) bytes, 16-byte aligned, where a vector's gradient is wanted (else NULL is allowed);
  *  calls that share one must be ordered on one stream.
  *  Launches: 1, +1 for the vectors.  Errors: as for the forward pass; SHAPE also for a workspace that is too small, NULL without one. */
