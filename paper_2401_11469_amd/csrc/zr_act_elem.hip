@@ -43,7 +43,7 @@ __global__ __launch_bounds__(256) void dropout_kernel(const T* x, int64_t ldx, T
 // ---------------------------------------------------------------------------
 // A workgroup has a panel of columns and rows_each rows; a thread's next row is on its way while it works on one.  What bounds it is
 // HBM and, with an activation, the vector instructions as much: 12608 x 2048, 1638 kept, GELU, 40 to 45 us, where its 145 MB alone take 27 and
-// its 35 instructions an element, two of them at a quarter of the rate, 27 as well.
+// its 36 instructions an element, two of them at a quarter of the rate, 28.
 // KEPT (bf16): only the kept columns of dZ are written, side by side: a wavefront has a row's 512 columns, puts the kept
 // ones into LDS at their places and stores 16 bytes a lane; the chunks that panels share go out element by element.
 template <typename T, bool KEPT>

@@ -1,6 +1,6 @@
 // Forward products with bias, activation, gate, dropout and residual, of bf16 tensors with 16-byte aligned rows: the loops and tile
 // shapes of zr_gemm_fast.h with finish_tile at their end.  MFMA bound up to there, then by the way of the end's tensors, which one of
-// two tiles on a compute unit can overlap and a 256 x 256 one cannot: 8192 x 1024 x 1024 with bias, GELU and Z 24 us (the product alone 20),
+// two tiles on a compute unit can overlap and a 256 x 256 one cannot: 8192 x 1024 x 1024 with bias, GELU and Z 24 to 26 us (the product alone 20),
 // 8192 x 4096 x 2752 of 2064 kept with SiLU, gate and Z 146 to 167 (135 alone; 135 MB more to move, 25 us of HBM).
 #include "zr_gemm_fast.h"
 

@@ -6,8 +6,8 @@
 // The backward pass normalises again from y and x_out (a few instructions; kept statistics would be read and, of a stored
 // x_out, be slightly off), and every thread adds up the gradients of the vectors for its columns over all rows of its workgroup;
 // a second launch adds the workgroups' sums in their order and makes the vectors' gradients of them.
-// Measured, bf16: 12608 x 1024, layer norm, dropout, bias and gate 20.6 us (5.0 TB/s); backward, 8192 x 4096, two norms 79 to 87 us
-// (4.6 to 5.1 TB/s) and 4.5 for the second launch.
+// Measured, bf16, as called: 12608 x 1024, layer norm, dropout, bias and gate 22 us (4.7 TB/s); backward, 8192 x 4096, two RMS norms 81 us
+// (5.0 TB/s; under a profiler 89 and 5 for the second launch), two layer norms with every gradient 109.
 #include <type_traits>
 
 #include "zr_act.h"
@@ -576,6 +576,8 @@ int launch_shape(const Join& j, int blocks, hipStream_t stream)
 // compute unit: a launch is that many, each with its share of the rows, and their number is that of the sums to be added up in the
 // end.  (Backward, two norms, bf16, us with 1 / 2 / 3 workgroups to a unit: 8192 x 4096 83 / 90 / -, 8192 x 2048 62 / 47 / 50, 12608 x 1024
 // 52 / 39 / 40, 8192 x 768 36 / 27 / 24, 8192 x 5120 100 / 112 / -.)
+// Above 5120 columns 1024 threads leave 128 registers each, and rows and sums spill in the backward kernels: 8192 x 8192 forward 99 us (5.4 TB/s),
+// backward 187 (4.3), with layer norms and every gradient 420 (1.9); 4096 x 16384 115 (4.7), 415 (1.9), 897 (0.9).
 struct Shape { int threads, rows_at_once, per_unit; };
 Shape shape_of(int cols)
 {
