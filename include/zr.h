@@ -360,7 +360,7 @@ int zr_resized_linear_act_fwd(const void* X, int64_t ldx, const void* W, int64_t
 
 /* Its backward pass.  With T = D(dY) (the forward's p and rng):
  *   dgate = T * act(Z),  dZ = T * gate * act'(Z),  dbias = column sums of dZ,  dX and dW = zr_resized_linear_bwd at dZ, Zero imputed
- * (the gradient of the residual is dY).  act'(0) of ZR_ACT_RELU is 0.
+ * (the gradient of the residual is dY).  act'(0) of ZR_ACT_RELU is 0.  Where D drops an element dgate and dZ are 0, whatever dY, gate and Z hold there.
  *  Z [M x N]: the forward's, needed unless act is ZR_ACT_NONE and dgate is NULL.  gate: the forward's or NULL.
  *  dX [M x K], dW (stored like W), dbias [N], dgate [M x N]: outputs, each may be NULL, not all.  dgate may be gate, Z or dY (same
  *  pitch); no other output may overlap an input.  X is needed for dW, W for dX.

@@ -119,7 +119,18 @@ __global__ __launch_bounds__(256, 4) void act_back_kernel(const ActBack a, int a
         if (a.Z) rz.values(z);
         if (a.gate) rg.values(g);
         fetch(r + down);
-        if (a.drop) Draw(seed, offset, (uint32_t)r, (uint32_t)group).apply(t, a.drop, a.factor);
+        // (the dropped ones become 0 last: nothing of dY, Z or gate at their places reaches a gradient)
+        uint32_t kept = 0xffu;
+        if (a.drop) {
+            kept = Draw(seed, offset, (uint32_t)r, (uint32_t)group).bits(a.drop);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) t[e] *= a.factor;
+        }
+        auto drop = [&](float (&x)[8]) {
+            if (!a.drop) return;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = kept >> e & 1 ? x[e] : 0.f;
+        };
         if (a.Z) {
             act8<EXACT, true>(a.act, z, v, s);
         } else {
@@ -133,13 +144,14 @@ __global__ __launch_bounds__(256, 4) void act_back_kernel(const ActBack a, int a
         if (a.dgate && hi > 0) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] *= t[e];
+            drop(v);
             store8((T*)a.dgate + r * a.lddg + col, 0, hi, v);
         }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            t[e] *= s[e];
-            total[e] += t[e];
-        }
+        for (int e = 0; e < 8; ++e) t[e] *= s[e];
+        drop(t);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) total[e] += t[e];
         if constexpr (KEPT) {
             Bf* slots = turn[sub];
             Bf* row = (Bf*)a.dz + r * a.lddz + (begin & ~7);
