@@ -7,7 +7,7 @@
 // x_out, be slightly off), and every thread adds up the gradients of the vectors for its columns over all rows of its workgroup;
 // a second launch adds the workgroups' sums in their order and makes the vectors' gradients of them.
 // Measured, bf16, as called: 12608 x 1024, layer norm, dropout, bias and gate 22 us (4.7 TB/s); backward, 8192 x 4096, two RMS norms 81 us
-// (5.0 TB/s; under a profiler 89 and 5 for the second launch), two layer norms with every gradient 109.
+// (5.0 TB/s; under a profiler 84 to 89 and 5 for the second launch), two layer norms with every gradient 109.
 #include <type_traits>
 
 #include "zr_act.h"
